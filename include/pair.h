@@ -74,7 +74,11 @@ typedef enum {
   PAIR_ERR_DEVICE_TIMEOUT = 7,        /* a bounded on-device wait gave up;
                                          outputs of that call are invalid  */
   PAIR_ERR_ALLOC_INPUT = 8,           /* pair_allocate: invalid input value */
-  PAIR_ERR_ALLOC_INFEASIBLE = 9       /* pair_allocate: budget < pi_min sum c */
+  PAIR_ERR_ALLOC_INFEASIBLE = 9,      /* pair_allocate: budget < pi_min sum c */
+  PAIR_ERR_PAGES = 10,                /* paged cache: lengths, pages or slots
+                                         that do not fit together          */
+  PAIR_ERR_PROBABILITY = 11           /* pair_verify_drafts: no probability
+                                         left to draw a token from         */
 } pair_status;
 
 typedef enum { PAIR_F32 = 0, PAIR_BF16 = 1 } pair_dtype;
@@ -85,6 +89,8 @@ typedef enum { PAIR_F32 = 0, PAIR_BF16 = 1 } pair_dtype;
 #define PAIR_DEV_ERR_TIMEOUT 4 /* a pipeline wait exceeded its limit (~2 s) */
 #define PAIR_DEV_ERR_ALLOC_INPUT 8       /* pair_allocate: invalid input value */
 #define PAIR_DEV_ERR_ALLOC_INFEASIBLE 16 /* pair_allocate: budget < pi_min sum c */
+#define PAIR_DEV_ERR_PAGES 32            /* paged cache: lengths, pages or slots misfit */
+#define PAIR_DEV_ERR_PROBABILITY 64      /* pair_verify_drafts: nothing to draw from */
 
 /* pair_coeffs flags. */
 #define PAIR_CENTER 1u /* subtract the mean of a over completed vertices
@@ -499,10 +505,170 @@ PAIR_API pair_status pair_grad_noalloc(int64_t T, int32_t d, int32_t V,
                                        int32_t *dev_err, pair_stream_t stream);
 
 /*
+ * Generating the continued rollouts. A rollout that the design continues is
+ * generated in steps of a chunk of new tokens per request (one token, or the
+ * last token and the drafts behind it, or a prompt's piece). A step is
+ *     pair_pages_extend   cache pages and slots for the chunk,
+ *     pair_cache_append   the chunk's keys and values into those slots,
+ *     pair_attend_paged   the chunk's queries over the request's cache,
+ *     pair_verify_drafts  the drafts against the target's probabilities.
+ * Requests are packed: request i owns the rows [cu_new[i], cu_new[i+1]) of
+ * the step's arrays (none for a request that the design stopped). All lengths
+ * stay on the device, so a step needs no host synchronisation and can be
+ * captured in a CUDA graph; T is the capacity of the packed arrays, and rows
+ * from cu_new[R] on belong to nobody.
+ *
+ * The cache: num_pages pages of page_size >= 1 tokens; token p of request i
+ * lies in page block_table[i][p / page_size] at p % page_size. Its slot is
+ * page * page_size + p % page_size (int64). Requests may share pages (a
+ * group's rollouts their prompt's). Keys and values are two arrays with
+ * strides of their own, in elements: for_page, for_token, for_head; the head
+ * dimension is contiguous. Every order of the three is accepted.
+ */
+typedef struct {
+  int64_t for_page, for_token, for_head;
+} pair_cache_strides;
+
+/*
+ * pair_pages_extend -- block tables and slot map of a step from the requests'
+ * lengths. With kv_i = len_i + n_new_i, request i needs
+ * max(0, ceil(kv_i / page_size) - held_i) new pages; requests take them from
+ * the free list in their order, and they follow the held ones in the
+ * request's table row.
+ * In:  R >= 1 requests; page_size >= 1; table_width = columns of block_table;
+ *      len [R] tokens cached, held [R] pages held (at least ceil(len /
+ *      page_size): rejected drafts leave a request with more), n_new [R] new
+ *      tokens, each >= 0; free_pages [free_capacity] page ids and free_count
+ *      [1] how many of them are free. All int32 on the device.
+ *      T >= 1: capacity of slots.
+ * Out: block_table [R][table_width] int32: the new pages' entries (others are
+ *      left as they are); kv_len [R], held_out [R], cu_new [R+1] int32;
+ *      slots [T] int64, slot of every new token in packed order, -1 from
+ *      cu_new[R] on; taken [1] int32: pages used from the front of the list.
+ *      No output may overlap an input.
+ * Errors: host PAIR_ERR_INVALID_ARG; device PAIR_DEV_ERR_PAGES: a request
+ *      with a negative length or more tokens than its pages hold, one whose
+ *      pages run out (of the list or of its table row), or a chunk that does
+ *      not fit in T. Such a request gets no pages, its slots are -1 and its
+ *      kv_len is len (0 if negative); the others are served. cu_new counts a
+ *      negative n_new as 0 and stops at T.
+ * Deterministic. One launch, no workspace.
+ */
+PAIR_API pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t table_width,
+                                       const int32_t *len, const int32_t *held,
+                                       const int32_t *n_new, const int32_t *free_pages,
+                                       int32_t free_capacity, const int32_t *free_count,
+                                       int64_t T, int32_t *block_table, int32_t *kv_len,
+                                       int32_t *held_out, int32_t *cu_new, int64_t *slots,
+                                       int32_t *taken, int32_t *dev_err, pair_stream_t stream);
+
+/*
+ * pair_cache_append -- the keys and values of T new tokens into their slots;
+ * rows with slot -1 are left out.
+ * In:  dt type of all four arrays; Hkv >= 1 heads; D head size, D elements a
+ *      multiple of 16 bytes; k, v with element strides k_row, v_row per token
+ *      and k_head, v_head per head; slots [T] int64. Row and head strides,
+ *      cache strides and base pointers are multiples of 16 bytes.
+ * Out: k_cache, v_cache (strides ks, vs).
+ * Errors: PAIR_ERR_INVALID_ARG; device PAIR_DEV_ERR_PAGES: a slot below -1 or
+ *      from num_pages * page_size on (that row is left out). Two rows with the
+ *      same slot leave one of them there, which one is not defined.
+ */
+PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt,
+                                       const void *k, int64_t k_row, int64_t k_head,
+                                       const void *v, int64_t v_row, int64_t v_head,
+                                       const int64_t *slots, int32_t num_pages,
+                                       int32_t page_size, void *k_cache, pair_cache_strides ks,
+                                       void *v_cache, pair_cache_strides vs, int32_t *dev_err,
+                                       pair_stream_t stream);
+
+/*
+ * pair_attend_paged -- attention of each request's chunk of new tokens over
+ * its paged cache, which already holds the chunk itself (kv_len counts it).
+ * Row j of a chunk of n tokens sees the keys k < kv_len - n + j + 1:
+ *     s_k = scale <q, key_k>,  lse = log sum_k exp(s_k),
+ *     out = sum_k exp(s_k - lse) value_k.
+ * A row that sees no key (kv_len - n + j < 0) and a row that no request owns
+ * get out = 0, lse = -inf.
+ * In:  q [T][Hq][D] (dt) with element strides q_row, q_head; Hq a multiple of
+ *      Hkv (query head h reads key head h / (Hq / Hkv)); D 64, 128 or 256;
+ *      block_table [R][table_width] int32, kv_len [R], cu_new [R+1] int32
+ *      (cu_new[0] = 0) on the device. Strides and base pointers are multiples
+ *      of 16 bytes. max_new: the longest chunk if the host knows it, else 0; it
+ *      leaves out launches that no chunk needs and changes no result (a longer
+ *      chunk than it says is computed all the same, more slowly).
+ * Out: out [T][Hq][D] (dt), lse [T][Hq] float32 (nullable).
+ * Arithmetic: scores, softmax statistics and output sums in fp32. PAIR_BF16:
+ *      the weights exp(s - max) go to the tensor cores in bf16, and out is
+ *      rounded once. PAIR_F32: CUDA cores, fp32 throughout. Keys from kv_len
+ *      on are never used, whatever their pages hold, and a key that a row does
+ *      not see has no part in it, NaN and infinity included.
+ * Workspace: pair_attend_workspace_size bytes, 256-byte aligned, any contents.
+ * Errors: PAIR_ERR_INVALID_ARG, PAIR_ERR_UNSUPPORTED (another D),
+ *      PAIR_ERR_WORKSPACE; device PAIR_DEV_ERR_PAGES: a page id outside
+ *      [0, num_pages) or a kv_len that is negative or beyond the table row
+ *      (that request's rows are unspecified), or offsets cu_new that decrease
+ *      or pass T (all rows are). Nothing outside the arrays is read or written.
+ * Deterministic for the same arguments on the same device.
+ */
+PAIR_API size_t pair_attend_workspace_size(int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                           pair_dtype dt);
+PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                       pair_dtype dt, const void *q, int64_t q_row,
+                                       int64_t q_head, const void *k_cache,
+                                       pair_cache_strides ks, const void *v_cache,
+                                       pair_cache_strides vs, int32_t num_pages,
+                                       int32_t page_size, const int32_t *block_table,
+                                       int32_t table_width, const int32_t *kv_len,
+                                       const int32_t *cu_new, float scale, int32_t max_new,
+                                       void *out, float *lse, void *ws, size_t ws_bytes,
+                                       int32_t *dev_err, pair_stream_t stream);
+
+/*
+ * pair_verify_drafts -- verification of drafted tokens against the target's
+ * probabilities, from given random numbers, and the token that follows them.
+ * A chunk of n = cu_new[i+1] - cu_new[i] rows holds the request's last token
+ * and n - 1 drafts: row j of p predicts ids[cu_new[i] + j + 1]. With y that
+ * draft, it is accepted iff u[row] * q(y) < p(y) (one fp32 product). At the
+ * first draft that is not, the token is drawn from max(p - q, 0) of that row;
+ * if all are accepted, from p of the last row. The emitted tokens are then
+ * distributed as the target's own (speculative sampling).
+ * The draw: weights w_v = floor(2^40 max(p_v - q_v, 0)) (the difference in
+ * fp32; NaN counts as 0, more than 1 as 1), C_v = w_0 + .. + w_v, the lowest
+ * v with C_v > floor(u_draw[i] * C_{V-1}) (an fp64 product, at most
+ * C_{V-1} - 1). The sums are integers, so the token depends on no order. If
+ * every weight of the difference is 0, p alone is drawn from.
+ * In:  p [T][V], q [T][V] (dt; row strides p_row, q_row in elements; a
+ *      chunk's last row of q is not read); q may be null: drafts that were
+ *      looked up, q(y) = 1 at the draft and 0 elsewhere. ids [T], cu_new [R+1]
+ *      int32; u [T], u_draw [R] float32 in [0, 1). V <= 2^22.
+ * Out: out_ids [T] int32: at row cu_new[i] + j the j-th emitted token, -1
+ *      behind the last one and at rows no request owns; logp [T] float32
+ *      (nullable): log p of that token under its row of p, 0 where out_ids is
+ *      -1: summed over a rollout, pair_grad_clipped's logp_old; n_emit [R]
+ *      int32: tokens emitted, 0 for an empty chunk. After the step the
+ *      request's cache holds len + n_emit valid tokens.
+ * Errors: PAIR_ERR_INVALID_ARG; device PAIR_DEV_ERR_TARGET_RANGE: a draft
+ *      outside [0, V) (rejected, the draw is from p - q, from p without q);
+ *      PAIR_DEV_ERR_PROBABILITY: all weights of p are 0 (the token is -1 and
+ *      not counted); PAIR_DEV_ERR_PAGES: offsets that decrease or pass T (the
+ *      request is left out).
+ * Deterministic. One launch, no workspace.
+ */
+PAIR_API pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_dtype dt,
+                                        const void *p, int64_t p_row, const void *q,
+                                        int64_t q_row, const int32_t *ids,
+                                        const int32_t *cu_new, const float *u,
+                                        const float *u_draw, int32_t *out_ids, float *logp,
+                                        int32_t *n_emit, int32_t *dev_err,
+                                        pair_stream_t stream);
+
+/*
  * pair_status_sync -- synchronise `stream`, read the device error word
  * (if non-null), reset it to 0, and return the status it encodes
  * (PAIR_ERR_DEVICE_TIMEOUT, then PAIR_ERR_NONPOSITIVE_INCLUSION, then
- * PAIR_ERR_TARGET_RANGE), or
+ * PAIR_ERR_TARGET_RANGE, the allocation errors, PAIR_ERR_PAGES and
+ * PAIR_ERR_PROBABILITY), or
  * PAIR_ERR_CUDA if the stream reports an error. Not for hot loops.
  */
 PAIR_API pair_status pair_status_sync(pair_stream_t stream, int32_t *dev_err);

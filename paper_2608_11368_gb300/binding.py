@@ -26,7 +26,9 @@ PAIR_STANDARDIZE = 2
 STATUS_NAMES = {0: "PAIR_OK", 1: "PAIR_ERR_INVALID_ARG", 2: "PAIR_ERR_UNSUPPORTED",
                 3: "PAIR_ERR_WORKSPACE", 4: "PAIR_ERR_NONPOSITIVE_INCLUSION",
                 5: "PAIR_ERR_TARGET_RANGE", 6: "PAIR_ERR_CUDA",
-                7: "PAIR_ERR_DEVICE_TIMEOUT"}
+                7: "PAIR_ERR_DEVICE_TIMEOUT", 8: "PAIR_ERR_ALLOC_INPUT",
+                9: "PAIR_ERR_ALLOC_INFEASIBLE", 10: "PAIR_ERR_PAGES",
+                11: "PAIR_ERR_PROBABILITY"}
 
 
 class PairError(RuntimeError):
@@ -34,6 +36,12 @@ class PairError(RuntimeError):
         self.status = status
         super().__init__("%s: %s (%s)" % (where, STATUS_NAMES.get(status, status),
                                           pair_status_string(status)))
+
+
+class CacheStrides(ctypes.Structure):
+    """pair_cache_strides (include/pair.h), in elements."""
+    _fields_ = [("for_page", ctypes.c_int64), ("for_token", ctypes.c_int64),
+                ("for_head", ctypes.c_int64)]
 
 
 _lib = None
@@ -90,6 +98,21 @@ def lib() -> ctypes.CDLL:
     L.pair_allocate.restype = ctypes.c_int
     L.pair_grad_token_logp.argtypes = [I64, I32, I32, I32, ctypes.c_int, P, SZ, P, P]
     L.pair_grad_token_logp.restype = ctypes.c_int
+    L.pair_pages_extend.argtypes = [I32, I32, I32, P, P, P, P, I32, P, I64, P, P, P, P, P, P, P,
+                                    P]
+    L.pair_pages_extend.restype = ctypes.c_int
+    L.pair_cache_append.argtypes = [I64, I32, I32, ctypes.c_int, P, I64, I64, P, I64, I64, P, I32,
+                                    I32, P, CacheStrides, P, CacheStrides, P, P]
+    L.pair_cache_append.restype = ctypes.c_int
+    L.pair_attend_workspace_size.argtypes = [I32, I32, I32, I32, ctypes.c_int]
+    L.pair_attend_workspace_size.restype = SZ
+    L.pair_attend_paged.argtypes = [I64, I32, I32, I32, I32, ctypes.c_int, P, I64, I64, P,
+                                    CacheStrides, P, CacheStrides, I32, I32, P, I32, P, P, F32,
+                                    I32, P, P, P, SZ, P, P]
+    L.pair_attend_paged.restype = ctypes.c_int
+    L.pair_verify_drafts.argtypes = [I64, I32, I32, ctypes.c_int, P, I64, P, I64, P, P, P, P, P,
+                                     P, P, P, P]
+    L.pair_verify_drafts.restype = ctypes.c_int
     L.pair_selftest_wait_timeout.argtypes = [I64, P, P, P]
     L.pair_selftest_wait_timeout.restype = ctypes.c_int
     _lib = L
@@ -333,12 +356,12 @@ def pair_grad_workspace_min_size(T, d, V, R, dtype) -> int:
                                                   int(dtype)))
 
 
-def _pair_dtype(t):
+def _pair_dtype(t, name="H/W"):
     if t.dtype == torch.bfloat16:
         return PAIR_BF16
     if t.dtype == torch.float32:
         return PAIR_F32
-    raise TypeError("H/W must be bfloat16 or float32")
+    raise TypeError("%s must be bfloat16 or float32" % name)
 
 
 def _grad_inputs(H, W, y, mask, cu_seqlens, a):
@@ -427,6 +450,150 @@ def pair_grad_noalloc(H, W, y, mask, cu_seqlens, a, dH=None, dW=None,
     _call("pair_grad_noalloc", H, stream, T, d, V, dt, _p(H), _p(W), _p(y), _p(mask),
           _p(cu_seqlens), R, _p(a), _p(dH), _p(dW), _p(Jobj), _p(logp_seq), _p(dev_err))
     return Jobj, dH, dW, logp_seq
+
+
+def _strided(t, name, dtype, shape, like):
+    """A CUDA tensor on like's device whose last dimension is contiguous (rows
+    of a wider array are fine); the library checks alignment."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.device != like.device:
+        raise ValueError("%s must be on %s, got %s" % (name, like.device, t.device))
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+
+
+def _same_device(like, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != like.device:
+            raise ValueError("%s must be on %s, got %s" % (name, like.device, t.device))
+
+
+def _cache(k_cache, v_cache, dtype, like):
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be [num_pages, page_size, Hkv, D]")
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _strided(t, name, dtype, k_cache.shape, like)
+    return (CacheStrides(*k_cache.stride()[:3]), CacheStrides(*v_cache.stride()[:3]))
+
+
+def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, page_size, T,
+                      kv_len=None, held_out=None, cu_new=None, slots=None, taken=None,
+                      dev_err=None, stream=None):
+    """Pages and slots of a step's new tokens (see pair.h). lens, held, n_new
+    [R], free_pages [F], free_count [1], block_table [R, width], all int32;
+    block_table gets the new pages in place. Returns (kv_len [R], held_out
+    [R], cu_new [R+1], slots [T] int64, taken [1])."""
+    R, width = block_table.shape
+    dev, i32 = lens.device, torch.int32
+    _need(lens, "lens", i32, (R,))
+    _need(held, "held", i32, (R,))
+    _need(n_new, "n_new", i32, (R,))
+    _need(free_pages, "free_pages", i32)
+    _need(free_count, "free_count", i32, (1,))
+    _need(block_table, "block_table", i32)
+    _same_device(lens, held=held, n_new=n_new, free_pages=free_pages, free_count=free_count,
+                 block_table=block_table, dev_err=dev_err)
+    kv_len = _out(kv_len, "kv_len", (R,), i32, dev)
+    held_out = _out(held_out, "held_out", (R,), i32, dev)
+    cu_new = _out(cu_new, "cu_new", (R + 1,), i32, dev)
+    slots = _out(slots, "slots", (int(T),), torch.int64, dev)
+    taken = _out(taken, "taken", (1,), i32, dev)
+    _call("pair_pages_extend", lens, stream, R, int(page_size), width, _p(lens), _p(held),
+          _p(n_new), _p(free_pages), free_pages.numel(), _p(free_count), int(T), _p(block_table),
+          _p(kv_len), _p(held_out), _p(cu_new), _p(slots), _p(taken), _p(dev_err))
+    return kv_len, held_out, cu_new, slots, taken
+
+
+def pair_cache_append(k, v, slots, k_cache, v_cache, dev_err=None, stream=None):
+    """Keys and values k, v [T, Hkv, D] into their slots [T] (int64, -1: left
+    out) of the caches [num_pages, page_size, Hkv, D] (see pair.h). k, v and
+    the caches may be views with other strides. Returns (k_cache, v_cache)."""
+    T, H, D = k.shape
+    dt = _pair_dtype(k, "k")
+    for t, name in ((k, "k"), (v, "v")):
+        _strided(t, name, k.dtype, (T, H, D), k)
+    _need(slots, "slots", torch.int64, (T,))
+    _same_device(k, slots=slots, dev_err=dev_err)
+    ks, vs = _cache(k_cache, v_cache, k.dtype, k)
+    if k_cache.shape[2:] != (H, D):
+        raise ValueError("k_cache must have %d heads of %d, got %s" % (H, D,
+                                                                       tuple(k_cache.shape)))
+    _call("pair_cache_append", k, stream, T, H, D, dt, _p(k), k.stride(0), k.stride(1), _p(v),
+          v.stride(0), v.stride(1), _p(slots), k_cache.shape[0], k_cache.shape[1], _p(k_cache),
+          ks, _p(v_cache), vs, _p(dev_err))
+    return k_cache, v_cache
+
+
+def pair_attend_workspace_size(R, Hq, Hkv, D, dtype) -> int:
+    return int(lib().pair_attend_workspace_size(int(R), int(Hq), int(Hkv), int(D), int(dtype)))
+
+
+def pair_attend_paged(q, k_cache, v_cache, block_table, kv_len, cu_new, scale=None, max_new=0,
+                      out=None, lse=None, ws=None, dev_err=None, stream=None):
+    """Attention of every request's chunk of new tokens over its paged cache
+    (see pair.h). q [T, Hq, D], caches [num_pages, page_size, Hkv, D] (views
+    with other strides too), block_table [R, width], kv_len [R], cu_new [R+1]
+    int32; scale is D ** -0.5 by default; max_new is the longest chunk if the
+    host knows it. Returns (out [T, Hq, D], lse [T, Hq]
+    float32)."""
+    T, Hq, D = q.shape
+    dt = _pair_dtype(q, "q")
+    _strided(q, "q", q.dtype, (T, Hq, D), q)
+    ks, vs = _cache(k_cache, v_cache, q.dtype, q)
+    Hkv = k_cache.shape[2]
+    if k_cache.shape[3] != D:
+        raise ValueError("k_cache must have heads of %d, got %s" % (D, tuple(k_cache.shape)))
+    R, width = block_table.shape
+    _need(block_table, "block_table", torch.int32)
+    _need(kv_len, "kv_len", torch.int32, (R,))
+    _need(cu_new, "cu_new", torch.int32, (R + 1,))
+    _same_device(q, block_table=block_table, kv_len=kv_len, cu_new=cu_new, ws=ws,
+                 dev_err=dev_err)
+    dev = q.device
+    out = _out(out, "out", (T, Hq, D), q.dtype, dev)
+    lse = _out(lse, "lse", (T, Hq), torch.float32, dev)
+    if ws is None:
+        need = pair_attend_workspace_size(R, Hq, Hkv, D, dt)
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", torch.uint8)
+    _call("pair_attend_paged", q, stream, T, R, Hq, Hkv, D, dt, _p(q), q.stride(0), q.stride(1),
+          _p(k_cache), ks, _p(v_cache), vs, k_cache.shape[0], k_cache.shape[1], _p(block_table),
+          width, _p(kv_len), _p(cu_new), float(D ** -0.5 if scale is None else scale),
+          int(max_new), _p(out), _p(lse), _p(ws), ws.numel(), _p(dev_err))
+    return out, lse
+
+
+def pair_verify_drafts(p, ids, cu_new, u, u_draw, q=None, out_ids=None, logp=None, n_emit=None,
+                       dev_err=None, stream=None):
+    """Drafted tokens against the target's probabilities p [T, V], and the
+    token that follows (see pair.h). ids [T], cu_new [R+1] int32; u [T], u_draw
+    [R] float32; q [T, V] the drafter's probabilities, or None for drafts that
+    were looked up. Returns (out_ids [T] int32, logp [T] float32, n_emit [R]
+    int32)."""
+    T, V = p.shape
+    dt = _pair_dtype(p, "p")
+    _strided(p, "p", p.dtype, (T, V), p)
+    if q is not None:
+        _strided(q, "q", p.dtype, (T, V), p)
+    R = cu_new.numel() - 1
+    _need(ids, "ids", torch.int32, (T,))
+    _need(cu_new, "cu_new", torch.int32, (R + 1,))
+    _need(u, "u", torch.float32, (T,))
+    _need(u_draw, "u_draw", torch.float32, (R,))
+    _same_device(p, ids=ids, cu_new=cu_new, u=u, u_draw=u_draw, dev_err=dev_err)
+    dev = p.device
+    out_ids = _out(out_ids, "out_ids", (T,), torch.int32, dev)
+    logp = _out(logp, "logp", (T,), torch.float32, dev)
+    n_emit = _out(n_emit, "n_emit", (R,), torch.int32, dev)
+    _call("pair_verify_drafts", p, stream, T, R, V, dt, _p(p), p.stride(0), _p(q),
+          0 if q is None else q.stride(0), _p(ids), _p(cu_new), _p(u), _p(u_draw), _p(out_ids),
+          _p(logp), _p(n_emit), _p(dev_err))
+    return out_ids, logp, n_emit
 
 
 def pair_selftest_wait_timeout(limit_cycles, dev_err, seen, stream=None):

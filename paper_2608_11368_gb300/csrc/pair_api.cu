@@ -273,6 +273,8 @@ pair_status pair_status_sync(pair_stream_t stream, int32_t *dev_err) {
   if (h & PAIR_DEV_ERR_TARGET_RANGE) return PAIR_ERR_TARGET_RANGE;
   if (h & PAIR_DEV_ERR_ALLOC_INPUT) return PAIR_ERR_ALLOC_INPUT;
   if (h & PAIR_DEV_ERR_ALLOC_INFEASIBLE) return PAIR_ERR_ALLOC_INFEASIBLE;
+  if (h & PAIR_DEV_ERR_PAGES) return PAIR_ERR_PAGES;
+  if (h & PAIR_DEV_ERR_PROBABILITY) return PAIR_ERR_PROBABILITY;
   return PAIR_OK;
 }
 
@@ -289,6 +291,8 @@ const char *pair_status_string(pair_status st) {
     case PAIR_ERR_DEVICE_TIMEOUT: return "device pipeline wait timed out";
     case PAIR_ERR_ALLOC_INPUT: return "allocation input out of range or not finite";
     case PAIR_ERR_ALLOC_INFEASIBLE: return "allocation budget below pi_min times the summed cost";
+    case PAIR_ERR_PAGES: return "lengths, pages or slots of the paged cache do not fit together";
+    case PAIR_ERR_PROBABILITY: return "no probability left to draw a token from";
   }
   return "unknown status";
 }

@@ -1,0 +1,270 @@
+// Paged cache of the rollouts being generated: pair_pages_extend (block
+// tables, chunk offsets and slots from request lengths) and
+// pair_cache_append (keys and values into their slots).
+#include "pair_common.cuh"
+
+namespace pairk {
+namespace {
+
+constexpr int kExtendThreads = 1024;
+constexpr int kExtendTokens = 1024;  // slots a block fills
+
+struct ExtendArgs {
+  int32_t R, page, width;
+  const int32_t *len, *held, *n_new, *free_pages;
+  int32_t free_capacity;
+  const int32_t *free_count;
+  int64_t T;
+  int32_t *table, *kv_len, *held_out, *cu;
+  int64_t *slots;
+  int32_t *taken, *dev_err;
+};
+
+// One request's needs. `bad`: its entries do not fit together or its table
+// row is too short; it then needs no pages (its rows still count in cu).
+struct Need {
+  int32_t len, held, n, pages;
+  bool bad;
+};
+__device__ __forceinline__ Need request_need(const ExtendArgs &a, int i) {
+  Need r;
+  r.len = a.len[i];
+  r.held = a.held[i];
+  const int32_t n = a.n_new[i];
+  r.n = n > 0 ? n : 0;
+  const int64_t kv = (int64_t)r.len + r.n;
+  const int64_t total = (kv + a.page - 1) / a.page;
+  r.bad = r.len < 0 || r.held < 0 || n < 0 || r.held > a.width || kv > INT32_MAX ||
+          (int64_t)r.held * a.page < r.len || total > a.width;
+  r.pages = r.bad ? 0 : (int32_t)(total > r.held ? total - r.held : 0);
+  return r;
+}
+
+// A request whose tokens a block fills: first row, pages taken before it.
+struct Filled {
+  int32_t i, len, held, n, ok;
+  int64_t row, first;
+};
+
+// The prefix sums of tokens and of pages over all requests are formed by
+// every block for itself (12 bytes per request, from L2 after the first), so
+// one launch does: block b writes the requests of its share and the slots
+// [b kExtendTokens, (b+1) kExtendTokens). A slot's page is read from the old
+// table entries or from the free list, never from entries this launch writes.
+// Bound by latency: loads of the lengths, one block scan, dependent page
+// reads, stores.
+__global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs a) {
+  __shared__ int64_t warp_n[32], warp_p[32];
+  __shared__ Filled list[kExtendTokens];
+  __shared__ int n_list, last_page;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (a.R + kExtendThreads - 1) / kExtendThreads;
+  const int i0 = min((int64_t)tid * per, (int64_t)a.R), i1 = min(i0 + per, a.R);
+  int64_t sn = 0, sp = 0;
+  for (int i = i0; i < i1; ++i) {
+    const Need r = request_need(a, i);
+    sn += r.n;
+    sp += r.pages;
+  }
+  int64_t xn = sn, xp = sp;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t yn = __shfl_up_sync(0xffffffffu, xn, o);
+    const int64_t yp = __shfl_up_sync(0xffffffffu, xp, o);
+    if (lane >= o) {
+      xn += yn;
+      xp += yp;
+    }
+  }
+  if (lane == 31) {
+    warp_n[warp] = xn;
+    warp_p[warp] = xp;
+  }
+  if (tid == 0) {
+    n_list = 0;
+    last_page = 0;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    int64_t yn = warp_n[lane], yp = warp_p[lane];
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t zn = __shfl_up_sync(0xffffffffu, yn, o);
+      const int64_t zp = __shfl_up_sync(0xffffffffu, yp, o);
+      if (lane >= o) {
+        yn += zn;
+        yp += zp;
+      }
+    }
+    warp_n[lane] = yn;
+    warp_p[lane] = yp;
+  }
+  __syncthreads();
+  const int64_t total_n = warp_n[31];
+  xn += (warp ? warp_n[warp - 1] : 0) - sn;  // exclusive
+  xp += (warp ? warp_p[warp - 1] : 0) - sp;
+  const int32_t avail = min(max(a.free_count[0], 0), a.free_capacity);
+  const int64_t t0 = (int64_t)blockIdx.x * kExtendTokens;
+  const int64_t t1 = min(t0 + kExtendTokens, a.T);
+  const int share = (a.R + gridDim.x - 1) / gridDim.x;
+  const int r0 = blockIdx.x * share, r1 = min(r0 + share, a.R);
+  for (int i = i0; i < i1; ++i) {
+    const Need r = request_need(a, i);
+    const bool ok = !r.bad && xp + r.pages <= avail && xn + r.n <= a.T;
+    if (ok && r.pages && blockIdx.x == 0) atomicMax(&last_page, (int32_t)(xp + r.pages));
+    if (i >= r0 && i < r1) {
+      a.kv_len[i] = ok ? r.len + r.n : max(r.len, 0);
+      a.held_out[i] = r.held + (ok ? r.pages : 0);
+      a.cu[i + 1] = (int32_t)min(xn + r.n, a.T);
+      if (i == 0) a.cu[0] = 0;
+      if (ok) {
+        int32_t *row = a.table + (int64_t)i * a.width + r.held;
+        for (int j = 0; j < r.pages; ++j) row[j] = a.free_pages[xp + j];
+      } else {
+        flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+      }
+    }
+    if (r.n > 0 && xn < t1 && xn + r.n > t0)
+      list[atomicAdd(&n_list, 1)] = {i, r.len, r.held, r.n, ok, xn, xp};
+    xn += r.n;
+    xp += r.pages;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0 && tid == 0) a.taken[0] = last_page;
+  for (int e = warp; e < n_list; e += kExtendThreads / 32) {
+    const Filled f = list[e];
+    const int64_t lo = max(f.row, t0), hi = min(f.row + f.n, t1);
+    for (int64_t t = lo + lane; t < hi; t += 32) {
+      int64_t slot = -1;
+      if (f.ok) {
+        const int64_t pos = f.len + (t - f.row);
+        const int32_t at = (int32_t)(pos / a.page);
+        const int32_t id = at < f.held ? a.table[(int64_t)f.i * a.width + at]
+                                       : a.free_pages[f.first + at - f.held];
+        slot = (int64_t)id * a.page + (pos - (int64_t)at * a.page);
+      }
+      a.slots[t] = slot;
+    }
+  }
+  for (int64_t t = max(t0, total_n) + tid; t < t1; t += kExtendThreads) a.slots[t] = -1;
+}
+
+struct AppendArgs {
+  int64_t T;
+  int32_t vecs_per_head, vecs;  // 16-byte pieces of a head, of a row
+  const uint4 *k, *v;
+  int64_t k_row, k_head, v_row, v_head;  // strides in 16-byte pieces, as below
+  const int64_t *slots;
+  int64_t n_slots;
+  int32_t page;
+  uint4 *kc, *vc;
+  pair_cache_strides ks, vs;
+  int32_t *dev_err;
+};
+
+constexpr int kAppendThreads = 256;
+
+// A thread moves one 16-byte piece of a token's keys and the same piece of its
+// values. Bound by HBM: every byte is read and written once.
+__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs a) {
+  const int64_t total = a.T * a.vecs;
+  for (int64_t x = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x; x < total;
+       x += (int64_t)gridDim.x * kAppendThreads) {
+    const int64_t t = x / a.vecs;
+    const int piece = (int)(x - t * a.vecs);
+    const int64_t slot = a.slots[t];
+    if (slot == -1) continue;
+    if (slot < 0 || slot >= a.n_slots) {
+      flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+      continue;
+    }
+    const int h = piece / a.vecs_per_head, c = piece - h * a.vecs_per_head;
+    const uint4 kx = a.k[t * a.k_row + h * a.k_head + c];
+    const uint4 vx = a.v[t * a.v_row + h * a.v_head + c];
+    const int64_t pg = slot / a.page, off = slot - pg * a.page;
+    a.kc[pg * a.ks.for_page + off * a.ks.for_token + h * a.ks.for_head + c] = kx;
+    a.vc[pg * a.vs.for_page + off * a.vs.for_token + h * a.vs.for_head + c] = vx;
+  }
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace
+}  // namespace pairk
+
+using namespace pairk;
+
+extern "C" {
+
+pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t table_width,
+                              const int32_t *len, const int32_t *held, const int32_t *n_new,
+                              const int32_t *free_pages, int32_t free_capacity,
+                              const int32_t *free_count, int64_t T, int32_t *block_table,
+                              int32_t *kv_len, int32_t *held_out, int32_t *cu_new,
+                              int64_t *slots, int32_t *taken, int32_t *dev_err,
+                              pair_stream_t stream) {
+  reset_launches();
+  if (R < 1 || page_size < 1 || table_width < 1 || T < 1 || T > INT32_MAX ||
+      free_capacity < 0 || !len || !held || !n_new || (!free_pages && free_capacity > 0) ||
+      !free_count || !block_table || !kv_len || !held_out || !cu_new || !slots || !taken)
+    return PAIR_ERR_INVALID_ARG;
+  const pair_status dv = check_device();
+  if (dv != PAIR_OK) return dv;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const ExtendArgs a{R,    page_size, table_width, len,    held, n_new, free_pages, free_capacity,
+                     free_count, T,   block_table, kv_len, held_out, cu_new, slots, taken,
+                     dev_err};
+  PAIR_BEGIN("pages_extend", s);
+  pages_extend_kernel<<<(unsigned)ceil_div(T, kExtendTokens), kExtendThreads, 0, s>>>(a);
+  PAIR_LAUNCH_CHECK(s);
+  return PAIR_OK;
+}
+
+pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt, const void *k,
+                              int64_t k_row, int64_t k_head, const void *v, int64_t v_row,
+                              int64_t v_head, const int64_t *slots, int32_t num_pages,
+                              int32_t page_size, void *k_cache, pair_cache_strides ks,
+                              void *v_cache, pair_cache_strides vs, int32_t *dev_err,
+                              pair_stream_t stream) {
+  reset_launches();
+  if (T < 1 || T > INT32_MAX || Hkv < 1 || D < 1 || (dt != PAIR_F32 && dt != PAIR_BF16) || !k ||
+      !v || !slots || num_pages < 1 || page_size < 1 || !k_cache || !v_cache)
+    return PAIR_ERR_INVALID_ARG;
+  const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
+  const int64_t strides[] = {k_row, k_head, v_row, v_head, ks.for_page, ks.for_token,
+                             ks.for_head, vs.for_page, vs.for_token, vs.for_head};
+  for (const int64_t x : strides)
+    if (x % per != 0) return PAIR_ERR_INVALID_ARG;
+  if (D % per != 0 || (int64_t)Hkv * D > INT32_MAX || !aligned16(k) || !aligned16(v) ||
+      !aligned16(k_cache) || !aligned16(v_cache))
+    return PAIR_ERR_INVALID_ARG;
+  const pair_status dv = check_device();
+  if (dv != PAIR_OK) return dv;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const auto cut = [per](pair_cache_strides x) {
+    return pair_cache_strides{x.for_page / per, x.for_token / per, x.for_head / per};
+  };
+  const AppendArgs a{T,
+                     D / per,
+                     Hkv * (D / per),
+                     static_cast<const uint4 *>(k),
+                     static_cast<const uint4 *>(v),
+                     k_row / per,
+                     k_head / per,
+                     v_row / per,
+                     v_head / per,
+                     slots,
+                     (int64_t)num_pages * page_size,
+                     page_size,
+                     static_cast<uint4 *>(k_cache),
+                     static_cast<uint4 *>(v_cache),
+                     cut(ks),
+                     cut(vs),
+                     dev_err};
+  const int64_t blocks = ceil_div(T * a.vecs, kAppendThreads);
+  PAIR_BEGIN("cache_append", s);
+  cache_append_kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), kAppendThreads, 0,
+                        s>>>(a);
+  PAIR_LAUNCH_CHECK(s);
+  return PAIR_OK;
+}
+
+}  // extern "C"
