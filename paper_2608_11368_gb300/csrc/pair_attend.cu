@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   clear_notes(a, cta);
   clear_spare_rows<T, D, kSimtThreads>(a, cta, ctas);
   if (cta == 0)
-    for (int i = tid; i < a.R; i += kSimtThreads) request(a, i, true);
+    report_requests(a);
   Walk<M, BN> walk{find_share<kSimtThreads>(a, M, cta, ctas, sm.scratch)};
   const T *q = static_cast<const T *>(a.q);
   const T *kc = static_cast<const T *>(a.kc), *vc = static_cast<const T *>(a.vc);
@@ -357,6 +357,8 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                Hq,
                Hkv,
                Hq / Hkv,
+               -1,
+               INT32_MAX,
                q,
                q_row,
                q_head,
@@ -376,7 +378,18 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                static_cast<Desc *>(ws),
                reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + desc_bytes()),
                dev_err};
-  return launch_simt(a, D, dt, reinterpret_cast<cudaStream_t>(stream));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (dt == PAIR_F32) return launch_simt(a, D, dt, s);
+  // Which kernel a chunk goes to is decided by its rows, on the device; a
+  // launch is left out where the host knows that no chunk can be its.
+  const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
+  if (most_rows <= kFewRows || !many_applies(a, D)) return launch_few(a, D, s);
+  if (R == 1) return launch_many(a, D, s);
+  Args few = a, many = a;
+  few.rows_upto = kFewRows;
+  many.rows_over = kFewRows;
+  const pair_status st = launch_few(few, D, s);
+  return st != PAIR_OK ? st : launch_many(many, D, s);
 }
 
 }  // extern "C"

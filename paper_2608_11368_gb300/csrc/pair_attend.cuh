@@ -28,6 +28,7 @@ namespace attend {
 
 constexpr int kMaxCtas = 320;    // of one call, at most
 constexpr int kMaxRows = 256;    // rows of a unit, at most
+constexpr int kManyRows = 256;   // rows of a unit of the kernel for many rows
 constexpr int kFewRows = 64;     // rows of a unit of the kernel for few rows
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kUnitCost = 48;    // a unit's fixed cost, in keys
@@ -36,6 +37,7 @@ constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its o
 struct Args {
   int64_t T;
   int32_t R, Hq, Hkv, g;
+  int32_t rows_over, rows_upto;  // requests with rows in (rows_over, rows_upto] are this launch's
   const void *q;
   int64_t q_row, q_head;
   const void *kc, *vc;
@@ -65,14 +67,25 @@ struct Request {
   int32_t n, kv;  // tokens of the chunk, keys in the cache (they include it)
 };
 
-// Request i with what does not fit together cut down to what does.
-__device__ __forceinline__ Request request(const Args &a, int i, bool report = false) {
+// Request i with what does not fit together cut down to what does; without
+// rows if they are another launch's.
+__device__ __forceinline__ Request request(const Args &a, int i) {
   const int lo = a.cu[i], hi = a.cu[i + 1], len = a.kv_len[i];
   const bool sane = lo >= 0 && hi >= lo && hi <= a.T;
   const int64_t most = (int64_t)a.width * a.page;
   Request r{lo, sane ? hi - lo : 0, len < 0 ? 0 : (int32_t)(len > most ? most : len)};
-  if (report && (!sane || len < 0 || len > most)) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+  const int rows = r.n * a.g;
+  if (rows <= a.rows_over || rows > a.rows_upto) r.n = 0;
   return r;
+}
+// By a whole block: requests whose entries do not fit together.
+__device__ __forceinline__ void report_requests(const Args &a) {
+  bool bad = false;
+  for (int i = threadIdx.x; i < a.R; i += blockDim.x) {
+    const int lo = a.cu[i], hi = a.cu[i + 1], len = a.kv_len[i];
+    bad |= lo < 0 || hi < lo || hi > a.T || len < 0 || len > (int64_t)a.width * a.page;
+  }
+  if (bad || (threadIdx.x == 0 && a.cu[0] != 0)) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
 }
 
 // The line of units of one request.
@@ -287,6 +300,9 @@ __device__ __noinline__ void add_not_finite(const Args &a, const Segment &s, int
 
 // Host side: the kernels and the pass that joins their partial sums.
 pair_status launch_simt(const Args &a, int D, pair_dtype dt, cudaStream_t s);
+pair_status launch_few(const Args &a, int D, cudaStream_t s);
+bool many_applies(const Args &a, int D);
+pair_status launch_many(const Args &a, int D, cudaStream_t s);
 pair_status launch_join(const Args &a, int D, int M, int ctas, pair_dtype dt, cudaStream_t s);
 int sm_count();
 

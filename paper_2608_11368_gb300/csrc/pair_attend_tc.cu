@@ -1,0 +1,559 @@
+// pair_attend_paged for chunks with many rows, bf16: scores and output sums on
+// the 5th-generation tensor cores.
+#include "pair_attend.cuh"
+#include "tc_kernels.cuh"
+
+namespace pairk {
+namespace attend {
+namespace {
+
+using namespace tc;
+
+// CTA: warps 0-3 and 4-7 the softmax of one tile of 128 rows each (a row per
+// thread), warp 8 the TMA producer, warp 9 the MMA issuer.
+constexpr int kThreads = 320;
+constexpr int M = kManyRows;  // two tiles of 128
+constexpr int BN = 128;       // keys of a tile
+
+template <int D>
+struct Tc {
+  static constexpr int kStages = D == 64 ? 8 : 5;  // ring of key and value tiles
+  static constexpr int kAtoms = D / 64;            // 128 rows x 64 columns, 128-byte swizzle
+  static constexpr uint32_t kAtom = 128 * 128;
+  static constexpr uint32_t kTile = kAtoms * kAtom;
+  static constexpr uint32_t kIdescS = idesc_bf16(128, 128, 0, 0);
+  static constexpr uint32_t kIdescO = idesc_bf16(128, D, 0, 1);
+};
+
+template <int D>
+struct Smem {
+  uint8_t q[2][Tc<D>::kTile];
+  uint8_t kv[Tc<D>::kStages][Tc<D>::kTile];
+  uint64_t full[Tc<D>::kStages], empty[Tc<D>::kStages];
+  uint64_t done, q_full[2], s_full[2], p_ready[2], pv_done[2];
+  int64_t scratch[kThreads / 32 + 2];
+  uint32_t tmem;
+  int abort, any_bad;
+};
+
+struct Maps {
+  CUtensorMap k, v;
+  int8_t k_at[3], v_at[3];  // dimension (1 to 3) of page, token, head
+  int box;                  // tokens of a box
+};
+
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
+                                            uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(
+          taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+      "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+      "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x,
+                                            int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+
+// Place in the ring of key and value tiles.
+template <int ST>
+struct Ring {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int n = 1) {
+    stage += n;
+    if (stage >= ST) {
+      stage -= ST;
+      phase ^= 1;
+    }
+  }
+};
+
+// Tiles with keys that some row does not see: their scores are masked and
+// their values looked over.
+__device__ __forceinline__ bool edge_tile(const Segment &s, int g, int t) {
+  return (t + 1) * BN > min(s.seen(0, g), s.kv);
+}
+
+template <int D>
+__device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN> walk) {
+  using C = Tc<D>;
+  const int lane = threadIdx.x & 31;
+  volatile int *abort = &sm.abort;
+  Ring<C::kStages> ring;
+  int issued = 0;
+  const int box = maps.box, boxes = BN / box;
+  bool ok = true;
+  Segment s;
+  while (ok && walk.next(a, &s)) {
+    int off = 0, id = -1;
+    auto find = [&](int t) {
+      const int key = t * BN + lane * box;
+      id = t < s.t1 && lane < boxes && key < s.keys ? page_of(a, s.i, key, &off) : -1;
+    };
+    find(s.t0);
+    for (int t = s.t0; t < s.t1 && ok; ++t) {
+      const int cur = id, cur_off = off;
+      find(t + 1);
+      const unsigned some = __ballot_sync(0xffffffffu, cur >= 0);
+      const uint32_t bytes = __popc(some) * box * D * 2;
+      for (int kv = 0; kv < 2; ++kv) {
+        if (!(ok = wait(&sm.empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
+        uint64_t *bar = &sm.full[ring.stage];
+        if (lane == 0) mbar_expect_tx(bar, bytes);
+        __syncwarp();
+        if (cur >= 0) {
+          const int8_t *at = kv ? maps.v_at : maps.k_at;
+          const int c1 = at[0] == 1 ? cur : at[1] == 1 ? cur_off : s.h;
+          const int c2 = at[0] == 2 ? cur : at[1] == 2 ? cur_off : s.h;
+          const int c3 = at[0] == 3 ? cur : at[1] == 3 ? cur_off : s.h;
+#pragma unroll
+          for (int x = 0; x < C::kAtoms; ++x)
+            tma_load_4d(sm.kv[ring.stage] + x * C::kAtom + lane * box * 128,
+                        kv ? &maps.v : &maps.k, bar, x * 64, c1, c2, c3);
+        }
+        ++issued;
+        ring.step();
+      }
+    }
+  }
+  // Nothing may still be on its way into shared memory when the CTA ends: on
+  // the regular path every tile has been consumed; after an abort the last
+  // ones are waited for here (the barrier of a stage completes once per use).
+  if (!ok) {
+    volatile int never = 0;
+    Ring<C::kStages> r;
+    for (int x = 0; x < issued; ++x, r.step())
+      if (x >= issued - C::kStages) wait_limit(&sm.full[r.stage], r.phase, &never, a.dev_err, 10000000);
+  }
+}
+
+template <int D>
+__device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
+  using C = Tc<D>;
+  volatile int *abort = &sm.abort;
+  const uint32_t tmem = sm.tmem;
+  const uint32_t tS[2] = {tmem, tmem + 128}, tO[2] = {tmem + 256, tmem + 256 + D};
+  const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
+  const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, 1024);
+  const uint64_t dv = sdesc_sw128(smem_u32(sm.kv[0]), C::kAtom, 1024);
+  Ring<C::kStages> ring;
+  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0};
+  bool ok = true;
+  auto scores = [&](int w, int stage) {  // S_w = Q_w K^T
+    if (elect_one()) {
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t at = (kk >> 2) * (C::kAtom >> 4) + (kk & 3) * 2;
+        mma_bf16(tS[w], dq + w * (C::kTile >> 4) + at, dk + stage * (C::kTile >> 4) + at,
+                 C::kIdescS, kk != 0);
+      }
+      mma_commit(&sm.s_full[w]);
+    }
+    __syncwarp();
+  };
+  auto sums = [&](int w, int stage, bool first) {  // O_w += P_w V
+    if (elect_one()) {
+#pragma unroll
+      for (int kk = 0; kk < BN / 16; ++kk)
+        mma_bf16_ts(tO[w], tS[w] + kk * 8, dv + stage * (C::kTile >> 4) + kk * 128, C::kIdescO,
+                    !first || kk != 0);
+      mma_commit(&sm.pv_done[w]);
+    }
+    __syncwarp();
+  };
+  Segment s;
+  while (ok && walk.next(a, &s)) {
+    if (s.t0 == s.t1) continue;
+    const bool two = s.rows > 128;
+    if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+    for (int w = 0; w <= (int)two && ok; ++w) {
+      if (!(ok = wait(&sm.q_full[w], q_ph[w], abort, a.dev_err))) break;
+      q_ph[w] ^= 1;
+      tc_fence_after();
+      scores(w, ring.stage);
+    }
+    if (!ok) break;
+    if (elect_one()) mma_commit(&sm.empty[ring.stage]);
+    __syncwarp();
+    ring.step();
+    for (int t = s.t0; t < s.t1 && ok; ++t) {
+      const int v_stage = ring.stage;
+      if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+      const bool edge = edge_tile(s, a.g, t);
+      ring.step();
+      const bool more = t + 1 < s.t1;
+      const Ring<C::kStages> next = ring;
+      for (int w = 0; w <= (int)two && ok; ++w) {
+        // The threads that wrote the weights looked over an edge tile's values,
+        // each its part: all have to be through.
+        for (int y = w; y <= (edge && w == 0 ? (int)two : w) && ok; ++y)
+          if (!(edge && w == 1)) ok = wait(&sm.p_ready[y], p_ph[y], abort, a.dev_err);
+        if (!ok) break;
+        p_ph[w] ^= 1;
+        tc_fence_after();
+        sums(w, v_stage, t == s.t0);
+        if (more) {
+          // In the tensor pipe's order behind the sums, which read the weights
+          // in the place of these scores.
+          if (w == 0) {
+            if (!(ok = wait(&sm.full[next.stage], next.phase, abort, a.dev_err))) break;
+            tc_fence_after();
+          }
+          scores(w, next.stage);
+        }
+      }
+      if (!ok) break;
+      if (elect_one()) {
+        mma_commit(&sm.empty[v_stage]);
+        if (more) mma_commit(&sm.empty[next.stage]);
+      }
+      __syncwarp();
+      if (more) ring.step();
+    }
+  }
+  if (elect_one()) mma_commit(&sm.done);
+  __syncwarp();
+  volatile int never = 0;
+  wait(&sm.done, 0, &never, a.dev_err);
+}
+
+// Values of an edge tile, by the threads of the active tiles: keys from `nk` on become 0, what is not finite too
+// (add_not_finite brings it back for the rows that see it).
+template <int D>
+__device__ __forceinline__ void look_over(uint8_t *tile, int nk, int threads, int *any_bad) {
+  using C = Tc<D>;
+  bool bad = false;
+  for (int x = threadIdx.x; x < (int)C::kTile / 16; x += threads) {
+    uint4 *at = reinterpret_cast<uint4 *>(tile) + x;
+    uint4 u = *at;
+    bool change = false;
+    if (((x >> 3) & 127) >= nk) {
+      u = make_uint4(0, 0, 0, 0);
+      change = true;
+    } else {
+      uint32_t *w = reinterpret_cast<uint32_t *>(&u);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u, bad = change = true;
+        if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu, bad = change = true;
+      }
+    }
+    if (change) *at = u;
+  }
+  if (bad) *any_bad = 1;
+}
+
+template <int D>
+__device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
+  using C = Tc<D>;
+  const int tid = threadIdx.x, w = tid >> 7, row = tid & 127, warp = tid >> 5;
+  volatile int *abort = &sm.abort;
+  const uint32_t lane_at = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t tS = sm.tmem + w * 128 + lane_at, tO = sm.tmem + 256 + w * D + lane_at;
+  const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q);
+  // A negative scale goes into the queries' sign, a zero one makes them zero.
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
+  Ring<C::kStages> ring;
+  uint32_t s_ph = 0, pv_ph = 0;
+  bool ok = true;
+  Segment s;
+  for (int seg = 0; ok && walk.next(a, &s); ++seg) {
+    const int r = w * 128 + row;
+    const bool active = w == 0 || s.rows > 128, mine = r < s.rows;
+    const RowAt at = row_at(a, s.row0, s.r0, s.h, mine ? r : 0);
+    float m = -INFINITY, l = 0.f;
+    if (!active) {
+      for (int t = s.t0; t < s.t1; ++t) ring.step(2);
+    } else if (s.t0 < s.t1) {
+      // This row's query, in the K-major swizzled layout of the A operand. The
+      // scores of the segment before have all been read, so its queries have.
+      const __nv_bfloat16 *src = q + at.token * a.q_row + at.head * a.q_head;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (mine && a.scale != 0.f) u = *reinterpret_cast<const uint4 *>(src + c * 8);
+        u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
+        *reinterpret_cast<uint4 *>(sm.q[w] + (c >> 3) * C::kAtom + row * 128 +
+                                   (((c & 7) ^ (row & 7)) << 4)) = u;
+      }
+      fence_async_smem();
+      mbar_arrive(&sm.q_full[w]);
+      const int seen = min(s.seen(mine ? r : 0, a.g), s.kv);
+      for (int t = s.t0; t < s.t1; ++t) {
+        ring.step();  // the values' place
+        const bool edge = edge_tile(s, a.g, t);
+        const int key0 = t * BN;
+        if (edge) {
+          if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+          look_over<D>(sm.kv[ring.stage], min(BN, s.keys - key0), s.rows > 128 ? 256 : 128,
+                       &sm.any_bad);
+          fence_async_smem();
+        }
+        ring.step();
+        if (!(ok = wait(&sm.s_full[w], s_ph, abort, a.dev_err))) break;
+        s_ph ^= 1;
+        tc_fence_after();
+        float x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, x[c]);
+        if (edge) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (key0 + c * 32 + k >= seen) x[c][k] = -INFINITY;
+        }
+        float mx = m;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(x[c][k], x[c][k + 1]));
+        // The reference of the exponentials stays while no row's maximum has
+        // grown by more than 2^8 over it: weights up to 256 are as good as
+        // weights up to 1, and the sums need not be rescaled.
+        if (t == s.t0) {
+          m = mx;
+        } else if (__any_sync(0xffffffffu, (mx - m) * scale > 8.f)) {
+          const float fix = ex2_approx(mx == -INFINITY ? 0.f : (m - mx) * scale);
+          m = mx;
+          l *= fix;
+          if (!(ok = wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            uint32_t u[32];
+            tmem_ld32(tO + c * 32, o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) u[k] = __float_as_uint(o[k] * fix);
+            tmem_st32(tO + c * 32, u);
+          }
+        }
+        pv_ph ^= 1;
+        const float ref = m == -INFINITY ? 0.f : -m * scale;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) {
+              const float y = ex2_approx(fmaf(x[c + e][k], scale, ref));
+              const float z = ex2_approx(fmaf(x[c + e][k + 1], scale, ref));
+              sum[(k >> 1) & 3] += y + z;
+              const __nv_bfloat162 b = __floats2bfloat162_rn(y, z);
+              p[e * 16 + (k >> 1)] = *reinterpret_cast<const uint32_t *>(&b);
+            }
+          tmem_st32(tS + c * 16, p);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&sm.p_ready[w]);
+      }
+      if (!ok) break;
+      if (!(ok = wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
+      tc_fence_after();
+    }
+    const bool whole = s.whole();
+    float *part = nullptr;
+    if (!whole) part = a.part + note_partial(a, s, cta, seg) * part_floats(M, D);
+    if (!active) continue;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float m2 = m == -INFINITY ? m : m * scale;
+    const bool bad = s.t0 < s.t1 && *reinterpret_cast<volatile int *>(&sm.any_bad) != 0;
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      float o[32];
+      if (s.t0 < s.t1) {
+        tmem_ld32(tO + c * 32, o);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = 0.f;
+      }
+      if (!mine) continue;
+#pragma unroll
+      for (int k = 0; k < 32; k += 8) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = o[k + e];
+        if (bad) add_not_finite<D>(a, s, BN, r, c * 32 + k, v);
+        if (whole) {
+          uint4 u;
+          uint32_t *u4 = reinterpret_cast<uint32_t *>(&u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
+            u4[e] = *reinterpret_cast<const uint32_t *>(&b);
+          }
+          *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
+                                     (at.token * a.Hq + at.head) * D + c * 32 + k) = u;
+        } else {
+          float4 *dst = reinterpret_cast<float4 *>(part + 2 * M + r * D + c * 32 + k);
+          dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+          dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      }
+    }
+    tc_fence_before();
+    if (!mine) continue;
+    if (!whole) {
+      part[r] = m2;
+      part[M + r] = l;
+    } else if (a.lse) {
+      a.lse[at.token * a.Hq + at.head] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
+    }
+  }
+}
+
+// Two tiles of 128 rows share every key and value tile. While the softmax of
+// one tile runs, the tensor cores have the other's products: S_w = Q_w K^T into
+// TMEM, the weights back into TMEM in the place of the scores (bf16, the A
+// operand of the second product), O_w += P_w V in TMEM throughout. Keys and
+// values come by TMA, one box per page piece, into the layout the products
+// read. Bound by the tensor cores and, close behind, by the exponentials.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_many_kernel(Args a, const __grid_constant__ Maps maps) {
+  extern __shared__ uint8_t raw[];
+  Smem<D> &sm = *reinterpret_cast<Smem<D> *>(tck::align1k(raw));
+  const int tid = threadIdx.x, warp = tid >> 5;
+  const int cta = blockIdx.x, ctas = gridDim.x;
+  clear_notes(a, cta);
+  if (a.rows_over < 0) {
+    clear_spare_rows<__nv_bfloat16, D, kThreads>(a, cta, ctas);
+    if (cta == ctas - 1) report_requests(a);
+  }
+  if (tid == 0) {
+    for (int x = 0; x < Tc<D>::kStages; ++x) {
+      mbar_init(&sm.full[x], 1);
+      mbar_init(&sm.empty[x], 1);
+    }
+    mbar_init(&sm.done, 1);
+    for (int w = 0; w < 2; ++w) {
+      mbar_init(&sm.q_full[w], 128);
+      mbar_init(&sm.s_full[w], 1);
+      mbar_init(&sm.p_ready[w], 128);
+      mbar_init(&sm.pv_done[w], 1);
+    }
+    sm.abort = 0;
+    sm.any_bad = 0;
+    fence_mbar_init();
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
+  }
+  if (warp == 9) tmem_alloc(&sm.tmem, 512);
+  const Walk<M, BN> walk{find_share<kThreads>(a, M, cta, ctas, sm.scratch)};
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8)
+    produce<D>(a, maps, sm, walk);
+  else if (warp == 9)
+    issue<D>(a, sm, walk);
+  else
+    softmax<D>(a, sm, walk, cta);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_relinquish();
+    tmem_dealloc(sm.tmem, 512);
+  }
+}
+
+// 4-D map of a cache, dimensions in the order of their strides: boxes of `box`
+// tokens x 64 columns of one page and head. False where no such map exists.
+bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args &a, int D, int box,
+               const pair_cache_strides &st) {
+  const auto fn = tck::encode_fn();
+  if (!fn) return false;
+  const int64_t stride[3] = {st.for_page * 2, st.for_token * 2, st.for_head * 2};
+  const cuuint64_t size[3] = {(cuuint64_t)a.num_pages, (cuuint64_t)a.page, (cuuint64_t)a.Hkv};
+  const cuuint32_t want[3] = {1, (cuuint32_t)box, 1};
+  int order[3] = {0, 1, 2};
+  for (int x = 0; x < 3; ++x)
+    for (int y = 0; y < 2; ++y)
+      if (stride[order[y + 1]] < stride[order[y]]) {
+        const int z = order[y];
+        order[y] = order[y + 1];
+        order[y + 1] = z;
+      }
+  cuuint64_t dims[4] = {(cuuint64_t)D}, strides[3];
+  cuuint32_t boxes[4] = {64}, ones[4] = {1, 1, 1, 1};
+  for (int x = 0; x < 3; ++x) {
+    const int64_t b = stride[order[x]];
+    if (b < 16 || b >= ((int64_t)1 << 40)) return false;
+    strides[x] = (cuuint64_t)b;
+    dims[x + 1] = size[order[x]];
+    boxes[x + 1] = want[order[x]];
+    at[order[x]] = (int8_t)(x + 1);
+  }
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(p), dims, strides, boxes,
+            ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+pair_status run_many(const Args &a, const Maps &maps, cudaStream_t s) {
+  constexpr int smem = sizeof(Smem<D>) + 1024;
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_many_kernel<D>,
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  const int ctas = min(kMaxCtas, sm_count());
+  PAIR_BEGIN("attend_many", s);
+  attend_many_kernel<D><<<ctas, kThreads, smem, s>>>(a, maps);
+  PAIR_LAUNCH_CHECK(s);
+  return launch_join(a, D, M, ctas, PAIR_BF16, s);
+}
+
+bool many_maps(const Args &a, int D, Maps *maps) {
+  // A box is the largest power of two of tokens, up to a tile, that divides
+  // the page; the swizzle's period is 8 rows.
+  int box = 128;
+  while (a.page % box != 0) box /= 2;
+  if (D > 128 || box < 8) return false;
+  maps->box = box;
+  return cache_map(&maps->k, maps->k_at, a.kc, a, D, box, a.ks) &&
+         cache_map(&maps->v, maps->v_at, a.vc, a, D, box, a.vs);
+}
+
+}  // namespace
+
+bool many_applies(const Args &a, int D) {
+  Maps maps;
+  return many_maps(a, D, &maps);
+}
+
+pair_status launch_many(const Args &a, int D, cudaStream_t s) {
+  Maps maps;
+  if (!many_maps(a, D, &maps)) return PAIR_ERR_CUDA;
+  return D == 64 ? run_many<64>(a, maps, s) : run_many<128>(a, maps, s);
+}
+
+}  // namespace attend
+}  // namespace pairk
