@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         for (int c = 0; c < CPT; ++c) o[r][c] *= sm.fix[rg * RPT + r];
       // A value that a row does not see must not reach its sums, not even
       // times zero: it may be NaN.
-      const bool edge = key0 + nk > min(s.seen(0, a.g), s.kv);
+      const bool edge = key0 + nk > s.least;
       for (int k = 0; k < nk; ++k) {
         float v[CPT];
 #pragma unroll

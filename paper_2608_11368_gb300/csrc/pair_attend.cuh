@@ -88,19 +88,19 @@ __device__ __forceinline__ void report_requests(const Args &a) {
   if (bad || (threadIdx.x == 0 && a.cu[0] != 0)) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
 }
 
-// The line of units of one request.
+// The line of units of one request, in 1 / (2 g) keys (so that nothing is
+// divided): unit k sees about (k + 1) M / g tokens of the chunk.
 struct Line {
-  int64_t base;  // cost of a unit without its rows' own tokens
-  int32_t units; // row tiles per key head
-  int32_t M, g;
-  __device__ __forceinline__ Line(const Request &r, int M_, int g_) : M(M_), g(g_) {
-    base = kUnitCost + max(0, r.kv - r.n);
+  int64_t base;   // of a unit, without its rows' own tokens
+  int32_t units;  // row tiles per key head
+  int32_t M;
+  __device__ __forceinline__ Line(const Request &r, int M_, int g) : M(M_) {
+    base = (int64_t)2 * g * (kUnitCost + max(0, r.kv - r.n));
     units = (int32_t)(((int64_t)r.n * g + M - 1) / M);
   }
-  // Length of the first k units: unit k sees about (k + 1) M / g tokens of the chunk.
-  __device__ __forceinline__ int64_t upto(int64_t k) const {
-    return k * base + (int64_t)M * k * (k + 1) / (2 * g);
-  }
+  // Length of the first k units, and of unit k.
+  __device__ __forceinline__ int64_t upto(int64_t k) const { return k * base + M * k * (k + 1); }
+  __device__ __forceinline__ int64_t of(int64_t k) const { return base + 2 * M * (k + 1); }
 };
 
 __device__ __forceinline__ int64_t request_cost(const Args &a, int i, int M) {
@@ -138,7 +138,7 @@ __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *sc
     total += scratch[w];
   }
   x += before - sum;  // exclusive
-  const int64_t n = max((int64_t)1, min((int64_t)ctas, total / kMinKeys));
+  const int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * kMinKeys)));
   Share s{0, 0, 0, 0};
   if (cta < n) {
     s.from = (int64_t)((__int128)total * cta / n);
@@ -171,6 +171,7 @@ struct Segment {
   int32_t r0, rows;       // first row of the tile in the chunk, rows in use
   int32_t first_seen;     // keys that row 0 of the chunk's first token sees (may be < 0)
   int32_t keys;           // keys that the tile's last row sees
+  int32_t least;          // keys that every row of the tile sees
   int32_t kv;
   bool head;              // holds the unit's beginning
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
@@ -184,39 +185,59 @@ struct Segment {
 template <int M, int BN>
 struct Walk {
   Share s;
+  Request r;
+  int32_t h, k, units;
+  int64_t begin;  // where the unit begins
+  bool started;
+
+  __device__ __forceinline__ explicit Walk(const Share &share) : s(share), started(false) {}
+
   __device__ __forceinline__ bool next(const Args &a, Segment *g) {
     while (s.from < s.to) {
-      const Request r = request(a, s.i);
-      const Line l(r, M, a.g);
-      const int64_t per_head = l.upto(l.units);
-      const int64_t off = s.from - s.at;
-      if (off >= per_head * a.Hkv) {
-        s.at += per_head * a.Hkv;
-        ++s.i;
-        continue;
+      if (!started) {  // the only search: the unit that the share begins in
+        r = request(a, s.i);
+        const Line l(r, M, a.g);
+        const int64_t per_head = l.upto(l.units), off = s.from - s.at;
+        h = (int)(off / per_head);
+        const int64_t x = off - h * per_head;
+        int lo = 0, hi = l.units;  // upto(lo) <= x < upto(hi)
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (l.upto(mid) <= x) lo = mid; else hi = mid;
+        }
+        k = lo;
+        units = l.units;
+        begin = s.at + h * per_head + l.upto(lo);
+        started = true;
+      } else {
+        if (++k == units) {
+          k = 0;
+          if (++h == a.Hkv) {
+            h = 0;
+            do {
+              if (++s.i >= a.R) return false;
+              r = request(a, s.i);
+            } while (r.n == 0);
+            units = Line(r, M, a.g).units;
+          }
+        }
+        begin = s.from;
       }
-      const int h = (int)(off / per_head);
-      const int64_t x = off - h * per_head;
-      int lo = 0, hi = l.units;  // upto(lo) <= x < upto(hi)
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (l.upto(mid) <= x) lo = mid; else hi = mid;
-      }
-      const int64_t begin = l.upto(lo), cost = l.upto(lo + 1) - begin;
-      const int64_t x0 = x - begin;
-      const int64_t x1 = min(cost, x0 + (s.to - s.from));
+      const int64_t cost = Line(r, M, a.g).of(k);
+      const int64_t x0 = s.from - begin, x1 = min(cost, x0 + (s.to - s.from));
       g->i = s.i;
       g->h = h;
-      g->rt = lo;
+      g->rt = k;
       g->row0 = r.row0;
-      g->r0 = lo * M;
-      g->rows = min(M, r.n * a.g - lo * M);
+      g->r0 = k * M;
+      g->rows = min(M, r.n * a.g - k * M);
       g->first_seen = r.kv - r.n + 1;
       g->kv = r.kv;
+      g->least = min(r.kv, g->seen(0, a.g));
       g->keys = min(r.kv, g->seen(g->rows - 1, a.g));
       g->tiles = (g->keys + BN - 1) / BN;
-      g->t0 = (int)((x0 * g->tiles + cost / 2) / cost);
-      g->t1 = (int)((x1 * g->tiles + cost / 2) / cost);
+      g->t0 = cut(x0, cost, g->tiles);
+      g->t1 = cut(x1, cost, g->tiles);
       g->head = x0 == 0;
       s.from += x1 - x0;
       // A unit without keys is worked on (zeros are written) by whoever has
@@ -224,6 +245,14 @@ struct Walk {
       if (g->t0 < g->t1 || (g->tiles == 0 && g->head)) return true;
     }
     return false;
+  }
+
+  // The key tile at which x of a unit's `cost` falls: the same for the CTA that
+  // ends there and the one that begins there.
+  static __device__ __forceinline__ int cut(int64_t x, int64_t cost, int tiles) {
+    if (x == 0) return 0;
+    if (x == cost) return tiles;
+    return min(tiles, (int)__float2int_rn(__fdiv_rn((float)x, (float)cost) * (float)tiles));
   }
 };
 
@@ -283,14 +312,16 @@ __device__ __forceinline__ void clear_notes(const Args &a, int cta) {
 // not every row sees whole (key tiles of BN keys from the first row's limit
 // on), where they would meet weights of 0.
 template <int D>
-__device__ __noinline__ void add_not_finite(const Args &a, const Segment &s, int BN, int r, int col,
-                                            float (&v)[8]) {
+__device__ __forceinline__ void add_not_finite(const Args &a, const Segment &s, int BN, int r,
+                                               int col, float (&v)[8]) {
   const __nv_bfloat16 *vc = static_cast<const __nv_bfloat16 *>(a.vc);
-  const int least = min(s.seen(0, a.g), s.kv), most = min(s.seen(r, a.g), s.kv);
-  for (int key = max(s.t0 * BN, least / BN * BN); key < min(most, s.t1 * BN); ++key) {
+  const int most = min(s.seen(r, a.g), s.kv);
+#pragma unroll 1
+  for (int key = max(s.t0 * BN, s.least / BN * BN); key < min(most, s.t1 * BN); ++key) {
     int off;
     const int id = page_of(a, s.i, key, &off);
     const __nv_bfloat16 *row = vc + cache_row(a, a.vs, id, off, s.h) + col;
+#pragma unroll
     for (int c = 0; c < 8; ++c) {
       const float x = __bfloat162float(row[c]);
       if (!(fabsf(x) <= 3.4e38f)) v[c] += x;

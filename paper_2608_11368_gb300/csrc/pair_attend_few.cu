@@ -153,7 +153,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
   const bool working = wr * 16 < s.rows;
   const int ra = wr * 16 + (lane >> 2);
   const int seen[2] = {min(s.seen(ra, a.g), s.kv), min(s.seen(ra + 8, a.g), s.kv)};
-  const int least = min(s.seen(0, a.g), s.kv);  // keys below are seen by every row
+  const int least = s.least;
 
   for (int t = s.t0; t < s.t1; ++t) {
     const int it = t - s.t0, stage = it % NST;

@@ -10,8 +10,10 @@ namespace {
 using namespace tc;
 
 // CTA: warps 0-3 and 4-7 the softmax of one tile of 128 rows each (a row per
-// thread), warp 8 the TMA producer, warp 9 the MMA issuer.
-constexpr int kThreads = 320;
+// thread), warp 8 the TMA producer, warp 9 the MMA issuer. A row's 128 scores
+// stay in registers: the third warpgroup gives up registers to the other two
+// (208 x 256 + 80 x 128 of the 168 x 384 that the block is launched with).
+constexpr int kThreads = 384;
 constexpr int M = kManyRows;  // two tiles of 128
 constexpr int BN = 128;       // keys of a tile
 
@@ -30,7 +32,8 @@ struct Smem {
   uint8_t q[2][Tc<D>::kTile];
   uint8_t kv[Tc<D>::kStages][Tc<D>::kTile];
   uint64_t full[Tc<D>::kStages], empty[Tc<D>::kStages];
-  uint64_t done, q_full[2], s_full[2], p_ready[2], pv_done[2];
+  uint64_t looked[Tc<D>::kStages];  // an edge tile's values have been looked over
+  uint64_t done, q_full[2], s_full[2], p_ready[2][2], pv_done[2];
   int64_t scratch[kThreads / 32 + 2];
   uint32_t tmem;
   int abort, any_bad;
@@ -64,6 +67,47 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
+// tmem_ld32 without its wait, and the wait, which names the registers.
+__device__ __forceinline__ void tmem_ld32_async(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, "
+      "%30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
+        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]),
+                 "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                 "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                 "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+// (x0, x1) * (s, s) + (r, r) and (a0, a1) + (x0, x1), two lanes per instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 r) {
+  float2 o;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t &>(o))
+      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(s)),
+        "l"(reinterpret_cast<uint64_t &>(r)));
+  return o;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 o;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t &>(o))
+      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+  return o;
+}
 __device__ __forceinline__ void tmem_st_wait() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
@@ -92,8 +136,8 @@ struct Ring {
 
 // Tiles with keys that some row does not see: their scores are masked and
 // their values looked over.
-__device__ __forceinline__ bool edge_tile(const Segment &s, int g, int t) {
-  return (t + 1) * BN > min(s.seen(0, g), s.kv);
+__device__ __forceinline__ bool edge_tile(const Segment &s, int t) {
+  return (t + 1) * BN > s.least;
 }
 
 template <int D>
@@ -153,83 +197,78 @@ template <int D>
 __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   using C = Tc<D>;
   volatile int *abort = &sm.abort;
-  const uint32_t tmem = sm.tmem;
-  const uint32_t tS[2] = {tmem, tmem + 128}, tO[2] = {tmem + 256, tmem + 256 + D};
   const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
   const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, 1024);
   const uint64_t dv = sdesc_sw128(smem_u32(sm.kv[0]), C::kAtom, 1024);
+  const uint32_t tmem = sm.tmem;
   Ring<C::kStages> ring;
-  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0};
+  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0}, looked_ph = 0;
   bool ok = true;
-  auto scores = [&](int w, int stage) {  // S_w = Q_w K^T
+  auto scores = [&](int w, int stage, bool last) {  // S_w = Q_w K^T
     if (elect_one()) {
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         const uint32_t at = (kk >> 2) * (C::kAtom >> 4) + (kk & 3) * 2;
-        mma_bf16(tS[w], dq + w * (C::kTile >> 4) + at, dk + stage * (C::kTile >> 4) + at,
+        mma_bf16(tmem + w * 128, dq + w * (C::kTile >> 4) + at, dk + stage * (C::kTile >> 4) + at,
                  C::kIdescS, kk != 0);
       }
       mma_commit(&sm.s_full[w]);
+      if (last) mma_commit(&sm.empty[stage]);
     }
     __syncwarp();
   };
-  auto sums = [&](int w, int stage, bool first) {  // O_w += P_w V
+  // O_w += P_w V, by halves of the tile's keys.
+  auto sums = [&](int w, int stage, int half, bool first, bool last) {
     if (elect_one()) {
 #pragma unroll
-      for (int kk = 0; kk < BN / 16; ++kk)
-        mma_bf16_ts(tO[w], tS[w] + kk * 8, dv + stage * (C::kTile >> 4) + kk * 128, C::kIdescO,
-                    !first || kk != 0);
-      mma_commit(&sm.pv_done[w]);
+      for (int kk = 0; kk < BN / 32; ++kk) {
+        const int at = half * (BN / 32) + kk;
+        mma_bf16_ts(tmem + 256 + w * D, tmem + w * 128 + at * 8,
+                    dv + stage * (C::kTile >> 4) + at * 128, C::kIdescO, !first || at != 0);
+      }
+      if (half) {
+        mma_commit(&sm.pv_done[w]);
+        if (last) mma_commit(&sm.empty[stage]);
+      }
     }
     __syncwarp();
   };
   Segment s;
   while (ok && walk.next(a, &s)) {
     if (s.t0 == s.t1) continue;
-    const bool two = s.rows > 128;
+    const int top = s.rows > 128;  // the last active tile
     if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
-    for (int w = 0; w <= (int)two && ok; ++w) {
+    for (int w = 0; w <= top && ok; ++w) {
       if (!(ok = wait(&sm.q_full[w], q_ph[w], abort, a.dev_err))) break;
       q_ph[w] ^= 1;
       tc_fence_after();
-      scores(w, ring.stage);
+      scores(w, ring.stage, w == top);
     }
-    if (!ok) break;
-    if (elect_one()) mma_commit(&sm.empty[ring.stage]);
-    __syncwarp();
     ring.step();
     for (int t = s.t0; t < s.t1 && ok; ++t) {
       const int v_stage = ring.stage;
-      if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
-      const bool edge = edge_tile(s, a.g, t);
-      ring.step();
       const bool more = t + 1 < s.t1;
-      const Ring<C::kStages> next = ring;
-      for (int w = 0; w <= (int)two && ok; ++w) {
-        // The threads that wrote the weights looked over an edge tile's values,
-        // each its part: all have to be through.
-        for (int y = w; y <= (edge && w == 0 ? (int)two : w) && ok; ++y)
-          if (!(edge && w == 1)) ok = wait(&sm.p_ready[y], p_ph[y], abort, a.dev_err);
-        if (!ok) break;
+      if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+      if (edge_tile(s, t)) {
+        if (!(ok = wait(&sm.looked[v_stage], (looked_ph >> v_stage) & 1, abort, a.dev_err))) break;
+        looked_ph ^= 1u << v_stage;
+      }
+      ring.step();
+      if (more && !(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (w > top) break;
+        if (!(ok = wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err))) break;
+        tc_fence_after();
+        sums(w, v_stage, 0, t == s.t0, false);
+        if (!(ok = wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err))) break;
         p_ph[w] ^= 1;
         tc_fence_after();
-        sums(w, v_stage, t == s.t0);
-        if (more) {
-          // In the tensor pipe's order behind the sums, which read the weights
-          // in the place of these scores.
-          if (w == 0) {
-            if (!(ok = wait(&sm.full[next.stage], next.phase, abort, a.dev_err))) break;
-            tc_fence_after();
-          }
-          scores(w, next.stage);
-        }
+        sums(w, v_stage, 1, false, w == top);
+        // In the tensor pipe's order behind the sums, which read the weights in
+        // the place of these scores.
+        if (more) scores(w, ring.stage, w == top);
       }
-      if (!ok) break;
-      if (elect_one()) {
-        mma_commit(&sm.empty[v_stage]);
-        if (more) mma_commit(&sm.empty[next.stage]);
-      }
-      __syncwarp();
       if (more) ring.step();
     }
   }
@@ -239,30 +278,40 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   wait(&sm.done, 0, &never, a.dev_err);
 }
 
-// Values of an edge tile, by the threads of the active tiles: keys from `nk` on become 0, what is not finite too
-// (add_not_finite brings it back for the rows that see it).
+// Values of an edge tile, by the threads of the active tiles: keys from `nk` on
+// become 0, what is not finite among those that some row does not see (from
+// `from` on) too (add_not_finite brings it back for the rows that see it).
 template <int D>
-__device__ __forceinline__ void look_over(uint8_t *tile, int nk, int threads, int *any_bad) {
+__device__ __forceinline__ void look_over(uint8_t *tile, int from, int nk, int threads,
+                                          int *any_bad) {
   using C = Tc<D>;
-  bool bad = false;
-  for (int x = threadIdx.x; x < (int)C::kTile / 16; x += threads) {
-    uint4 *at = reinterpret_cast<uint4 *>(tile) + x;
-    uint4 u = *at;
-    bool change = false;
-    if (((x >> 3) & 127) >= nk) {
-      u = make_uint4(0, 0, 0, 0);
-      change = true;
-    } else {
-      uint32_t *w = reinterpret_cast<uint32_t *>(&u);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u, bad = change = true;
-        if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu, bad = change = true;
+  for (int atom = 0; atom < C::kAtoms; ++atom) {
+    uint4 *base = reinterpret_cast<uint4 *>(tile + atom * C::kAtom);
+#pragma unroll 4
+    for (int x = from * 8 + threadIdx.x; x < 1024; x += threads) {
+      if ((x >> 3) >= nk) {
+        base[x] = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      uint4 u = base[x];
+      // Zero times what is not finite is NaN.
+      const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+      const __nv_bfloat162 *v = reinterpret_cast<const __nv_bfloat162 *>(&u);
+      const __nv_bfloat162 t = __hfma2(v[0], zero, __hfma2(v[1], zero, __hfma2(v[2], zero,
+                                                                            __hmul2(v[3], zero))));
+      if (__hisnan(t.x) || __hisnan(t.y)) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+          if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
+        }
+        base[x] = u;
+        *any_bad = 1;
       }
     }
-    if (change) *at = u;
   }
-  if (bad) *any_bad = 1;
 }
 
 template <int D>
@@ -279,58 +328,77 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
   Ring<C::kStages> ring;
   uint32_t s_ph = 0, pv_ph = 0;
   bool ok = true;
-  Segment s;
-  for (int seg = 0; ok && walk.next(a, &s); ++seg) {
-    const int r = w * 128 + row;
+  const int r = w * 128 + row;
+  // This row's query, in the K-major swizzled layout of the A operand.
+  auto put_query = [&](const Segment &g) {
+    if (g.t0 == g.t1 || (w == 1 && g.rows <= 128)) return;
+    const bool there = r < g.rows && a.scale != 0.f;
+    const RowAt at = row_at(a, g.row0, g.r0, g.h, r < g.rows ? r : 0);
+    const __nv_bfloat16 *src = q + at.token * a.q_row + at.head * a.q_head;
+    uint4 u[D / 8];
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c)
+      u[c] = there ? *reinterpret_cast<const uint4 *>(src + c * 8) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < D / 8; ++c) {
+      u[c].x ^= flip, u[c].y ^= flip, u[c].z ^= flip, u[c].w ^= flip;
+      *reinterpret_cast<uint4 *>(sm.q[w] + (c >> 3) * C::kAtom + row * 128 +
+                                 (((c & 7) ^ (row & 7)) << 4)) = u[c];
+    }
+    fence_async_smem();
+    mbar_arrive(&sm.q_full[w]);
+  };
+  Segment s, ahead;
+  bool more = walk.next(a, &ahead);
+  if (more) put_query(ahead);
+  for (int seg = 0; ok && more; ++seg) {
+    s = ahead;
     const bool active = w == 0 || s.rows > 128, mine = r < s.rows;
-    const RowAt at = row_at(a, s.row0, s.r0, s.h, mine ? r : 0);
     float m = -INFINITY, l = 0.f;
     if (!active) {
       for (int t = s.t0; t < s.t1; ++t) ring.step(2);
     } else if (s.t0 < s.t1) {
-      // This row's query, in the K-major swizzled layout of the A operand. The
-      // scores of the segment before have all been read, so its queries have.
-      const __nv_bfloat16 *src = q + at.token * a.q_row + at.head * a.q_head;
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (mine && a.scale != 0.f) u = *reinterpret_cast<const uint4 *>(src + c * 8);
-        u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
-        *reinterpret_cast<uint4 *>(sm.q[w] + (c >> 3) * C::kAtom + row * 128 +
-                                   (((c & 7) ^ (row & 7)) << 4)) = u;
-      }
-      fence_async_smem();
-      mbar_arrive(&sm.q_full[w]);
       const int seen = min(s.seen(mine ? r : 0, a.g), s.kv);
       for (int t = s.t0; t < s.t1; ++t) {
         ring.step();  // the values' place
-        const bool edge = edge_tile(s, a.g, t);
+        const bool edge = edge_tile(s, t);
         const int key0 = t * BN;
         if (edge) {
           if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
-          look_over<D>(sm.kv[ring.stage], min(BN, s.keys - key0), s.rows > 128 ? 256 : 128,
-                       &sm.any_bad);
+          look_over<D>(sm.kv[ring.stage], max(0, s.least - key0), min(BN, s.keys - key0),
+                       s.rows > 128 ? 256 : 128, &sm.any_bad);
           fence_async_smem();
+          mbar_arrive(&sm.looked[ring.stage]);
+          if (s.rows <= 128) mbar_arrive(&sm.looked[ring.stage]);  // for the other tile's threads
         }
         ring.step();
         if (!(ok = wait(&sm.s_full[w], s_ph, abort, a.dev_err))) break;
         s_ph ^= 1;
         tc_fence_after();
-        float x[4][32];
+        uint32_t x[4][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, x[c]);
+        for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + c * 32, x[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld_wait(x[c]);
         if (edge) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c) {
+            const int upto = seen - key0 - c * 32;
+            if (upto < 32) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (key0 + c * 32 + k >= seen) x[c][k] = -INFINITY;
+              for (int k = 0; k < 32; ++k)
+                if (k >= upto) x[c][k] = 0xff800000u;  // -inf
+            }
+          }
         }
-        float mx = m;
+        float mx4[4] = {m, m, m, m};
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(x[c][k], x[c][k + 1]));
+          for (int k = 0; k < 32; k += 2)
+            mx4[(k >> 1) & 3] = fmaxf(mx4[(k >> 1) & 3], fmaxf(__uint_as_float(x[c][k]),
+                                                               __uint_as_float(x[c][k + 1])));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
         // The reference of the exponentials stays while no row's maximum has
         // grown by more than 2^8 over it: weights up to 256 are as good as
         // weights up to 1, and the sums need not be rescaled.
@@ -354,7 +422,8 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
         }
         pv_ph ^= 1;
         const float ref = m == -INFINITY ? 0.f : -m * scale;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
+        const float2 scale2 = {scale, scale}, ref2 = {ref, ref};
 #pragma unroll
         for (int c = 0; c < 4; c += 2) {
           uint32_t p[32];
@@ -362,20 +431,29 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
           for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
-              const float y = ex2_approx(fmaf(x[c + e][k], scale, ref));
-              const float z = ex2_approx(fmaf(x[c + e][k + 1], scale, ref));
-              sum[(k >> 1) & 3] += y + z;
-              const __nv_bfloat162 b = __floats2bfloat162_rn(y, z);
+              float2 y = fma2({__uint_as_float(x[c + e][k]), __uint_as_float(x[c + e][k + 1])},
+                              scale2, ref2);
+              y.x = ex2_approx(y.x);
+              y.y = ex2_approx(y.y);
+              sum[(k >> 1) & 1] = add2(sum[(k >> 1) & 1], y);
+              const __nv_bfloat162 b = __floats2bfloat162_rn(y.x, y.y);
               p[e * 16 + (k >> 1)] = *reinterpret_cast<const uint32_t *>(&b);
             }
           tmem_st32(tS + c * 16, p);
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&sm.p_ready[w][c >> 1]);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(&sm.p_ready[w]);
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
       if (!ok) break;
+    }
+    // All scores of this segment have been read, so its queries have: the next
+    // segment's go in their place, and its first scores are formed while this
+    // one's sums are brought out.
+    more = walk.next(a, &ahead);
+    if (more) put_query(ahead);
+    if (active && s.t0 < s.t1) {
       if (!(ok = wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
       tc_fence_after();
     }
@@ -383,6 +461,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
     float *part = nullptr;
     if (!whole) part = a.part + note_partial(a, s, cta, seg) * part_floats(M, D);
     if (!active) continue;
+    const RowAt at = row_at(a, s.row0, s.r0, s.h, mine ? r : 0);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float m2 = m == -INFINITY ? m : m * scale;
     const bool bad = s.t0 < s.t1 && *reinterpret_cast<volatile int *>(&sm.any_bad) != 0;
@@ -452,12 +531,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int x = 0; x < Tc<D>::kStages; ++x) {
       mbar_init(&sm.full[x], 1);
       mbar_init(&sm.empty[x], 1);
+      mbar_init(&sm.looked[x], 256);
     }
     mbar_init(&sm.done, 1);
     for (int w = 0; w < 2; ++w) {
       mbar_init(&sm.q_full[w], 128);
       mbar_init(&sm.s_full[w], 1);
-      mbar_init(&sm.p_ready[w], 128);
+      mbar_init(&sm.p_ready[w][0], 128);
+      mbar_init(&sm.p_ready[w][1], 128);
       mbar_init(&sm.pv_done[w], 1);
     }
     sm.abort = 0;
@@ -471,12 +552,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8)
-    produce<D>(a, maps, sm, walk);
-  else if (warp == 9)
-    issue<D>(a, sm, walk);
-  else
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 8)
+      produce<D>(a, maps, sm, walk);
+    else if (warp == 9)
+      issue<D>(a, sm, walk);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     softmax<D>(a, sm, walk, cta);
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {
