@@ -10,132 +10,167 @@ namespace {
 
 constexpr int kSimtThreads = 128;
 constexpr int kSimtRows = 16;
-constexpr int kSimtKeys = 64;
 
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_float(float *o, float x) { *o = x; }
 __device__ __forceinline__ void from_float(__nv_bfloat16 *o, float x) { *o = __float2bfloat16_rn(x); }
 
-// One 16-byte piece as floats.
-template <typename T>
-__device__ __forceinline__ void widen(const uint4 &u, float *o) {
-  const T *t = reinterpret_cast<const T *>(&u);
-#pragma unroll
-  for (int k = 0; k < 16 / (int)sizeof(T); ++k) o[k] = to_float(t[k]);
-}
-
 template <int D>
 struct SimtSmem {
+  static constexpr int kKeys = D == 64 ? 64 : 32;
+  static constexpr int kStages = 3;
+  float k[kStages][kKeys][D + 4];
+  float v[kStages][kKeys][D];
   float q[kSimtRows][D];
-  float k[kSimtKeys][D + 4];
-  float v[kSimtKeys][D];
-  float p[kSimtRows][kSimtKeys];
+  float p[kSimtRows][kKeys];
   float m[kSimtRows], l[kSimtRows], fix[kSimtRows];
-  int64_t krow[kSimtKeys], vrow[kSimtKeys];
+  int64_t row[2][2][kKeys];  // offsets of a tile's keys and values
   int seen[kSimtRows];
   int64_t scratch[kSimtThreads / 32 + 2];
 };
 
-// fp32 products on the CUDA cores: a tile of 64 keys and values in shared
-// memory, 16 rows against it. A thread forms the scores of one key with 8
-// rows, then the output sums of its columns for 16 rows (8 at D = 64).
-template <typename T, int D>
+// fp32 products on the CUDA cores, 16 rows against tiles of keys and values
+// that arrive two tiles ahead (asynchronous copies into shared memory). A
+// thread forms the scores of one key with its group's rows (the queries are
+// broadcast reads), then the output sums of its columns for 16 rows (8 at D =
+// 64), four keys at a time. Bound by latency at small sizes (four barriers and
+// two exchanges per tile), else by shared-memory reads.
+template <int D>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   extern __shared__ __align__(16) uint8_t raw[];
-  SimtSmem<D> &sm = *reinterpret_cast<SimtSmem<D> *>(raw);
-  constexpr int M = kSimtRows, BN = kSimtKeys, VEC = 16 / sizeof(T);
+  using S = SimtSmem<D>;
+  S &sm = *reinterpret_cast<S *>(raw);
+  constexpr int M = kSimtRows, BN = S::kKeys, NST = S::kStages, V4 = D / 4;
+  constexpr int QR = M * BN / kSimtThreads;                      // rows of a thread's scores
   constexpr int CPT = D >= kSimtThreads ? D / kSimtThreads : 1;  // columns per thread
   constexpr int RG = D >= kSimtThreads ? 1 : kSimtThreads / D;   // row groups
   constexpr int RPT = M / RG;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cta = blockIdx.x, ctas = gridDim.x;
   clear_notes(a, cta);
-  clear_spare_rows<T, D, kSimtThreads>(a, cta, ctas);
-  if (cta == 0)
-    report_requests(a);
+  clear_spare_rows<float, D, kSimtThreads>(a, cta, ctas);
+  if (cta == ctas - 1) report_requests(a);
   Walk<M, BN> walk{find_share<kSimtThreads>(a, M, cta, ctas, sm.scratch)};
-  const T *q = static_cast<const T *>(a.q);
-  const T *kc = static_cast<const T *>(a.kc), *vc = static_cast<const T *>(a.vc);
+  const float *q = static_cast<const float *>(a.q);
+  const float *kc = static_cast<const float *>(a.kc), *vc = static_cast<const float *>(a.vc);
   const float scale = a.scale * kLog2e;
-  const int col = (tid % (kSimtThreads / RG)), rg = tid / (kSimtThreads / RG);
+  const int col = tid % (kSimtThreads / RG), rg = tid / (kSimtThreads / RG);
   Segment s;
   for (int seg = 0; walk.next(a, &s); ++seg) {
     __syncthreads();
-    for (int x = tid; x < M * (D / VEC); x += kSimtThreads) {
-      const int r = x / (D / VEC), c = x % (D / VEC);
-      uint4 u = make_uint4(0, 0, 0, 0);
+    // Offsets of a tile's rows, by the first BN threads, one tile before its
+    // copies are started.
+    auto put_offsets = [&](int t) {
+      const int key = t * BN + tid;
+      if (tid < BN && t < s.t1) {
+        int off = 0;
+        const int id = key < s.keys ? page_of(a, s.i, key, &off) : -1;
+        sm.row[t & 1][0][tid] = id < 0 ? -1 : cache_row(a, a.ks, id, off, s.h);
+        sm.row[t & 1][1][tid] = id < 0 ? -1 : cache_row(a, a.vs, id, off, s.h);
+      }
+    };
+    auto fetch = [&](int t) {
+      if (t < s.t1) {
+        const int st = (t - s.t0) % NST;
+#pragma unroll 4
+        for (int x = tid; x < BN * V4; x += kSimtThreads) {
+          const int k = x / V4, c = x % V4 * 4;
+          const int64_t ko = sm.row[t & 1][0][k], vo = sm.row[t & 1][1][k];
+          cp_async16(tc::smem_u32(&sm.k[st][k][c]), kc + (ko < 0 ? 0 : ko + c), ko >= 0);
+          cp_async16(tc::smem_u32(&sm.v[st][k][c]), vc + (vo < 0 ? 0 : vo + c), vo >= 0);
+        }
+      }
+      cp_async_commit();
+    };
+    put_offsets(s.t0);
+    put_offsets(s.t0 + 1);
+    for (int x = tid; x < M * V4; x += kSimtThreads) {
+      const int r = x / V4, c = x % V4 * 4;
+      float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < s.rows) {
         const RowAt at = row_at(a, s.row0, s.r0, s.h, r);
-        u = *reinterpret_cast<const uint4 *>(q + at.token * a.q_row + at.head * a.q_head + c * VEC);
+        u = *reinterpret_cast<const float4 *>(q + at.token * a.q_row + at.head * a.q_head + c);
       }
-      widen<T>(u, &sm.q[r][c * VEC]);
+      *reinterpret_cast<float4 *>(&sm.q[r][c]) = u;
     }
     if (tid < M) {
       sm.m[tid] = -INFINITY;
       sm.l[tid] = 0.f;
       sm.seen[tid] = min(s.seen(tid, a.g), s.kv);
     }
+    __syncthreads();
+    fetch(s.t0);
+    fetch(s.t0 + 1);
     float o[RPT][CPT];
+    int seen[RPT];
 #pragma unroll
-    for (int r = 0; r < RPT; ++r)
+    for (int r = 0; r < RPT; ++r) {
+      seen[r] = sm.seen[rg * RPT + r];
 #pragma unroll
       for (int c = 0; c < CPT; ++c) o[r][c] = 0.f;
+    }
     for (int t = s.t0; t < s.t1; ++t) {
-      const int key0 = t * BN, nk = min(BN, s.keys - key0);
-      __syncthreads();
-      if (tid < nk) {
-        int off;
-        const int id = page_of(a, s.i, key0 + tid, &off);
-        sm.krow[tid] = cache_row(a, a.ks, id, off, s.h);
-        sm.vrow[tid] = cache_row(a, a.vs, id, off, s.h);
-      }
-      __syncthreads();
-      for (int x = tid; x < BN * (D / VEC); x += kSimtThreads) {
-        const int k = x / (D / VEC), c = x % (D / VEC);
-        uint4 ku = make_uint4(0, 0, 0, 0), vu = ku;
-        if (k < nk) {
-          ku = *reinterpret_cast<const uint4 *>(kc + sm.krow[k] + c * VEC);
-          vu = *reinterpret_cast<const uint4 *>(vc + sm.vrow[k] + c * VEC);
-        }
-        widen<T>(ku, &sm.k[k][c * VEC]);
-        widen<T>(vu, &sm.v[k][c * VEC]);
-      }
-      __syncthreads();
+      const int key0 = t * BN, st = (t - s.t0) % NST;
+      cp_async_wait<1>();
+      __syncthreads();  // tile t is there, tile t - 1's stage free
+      put_offsets(t + 2);
       {
-        const int k = tid % BN, r0 = (tid / BN) * (M / 2);
-        float acc[M / 2] = {};
+        const int k = tid % BN, r0 = tid / BN * QR;
+        float acc[QR] = {};
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {
-          const float4 x = *reinterpret_cast<const float4 *>(&sm.k[k][d]);
+          const float4 x = *reinterpret_cast<const float4 *>(&sm.k[st][k][d]);
 #pragma unroll
-          for (int r = 0; r < M / 2; ++r) {
+          for (int r = 0; r < QR; ++r) {
             const float4 y = *reinterpret_cast<const float4 *>(&sm.q[r0 + r][d]);
             acc[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc[r]))));
           }
         }
 #pragma unroll
-        for (int r = 0; r < M / 2; ++r)
+        for (int r = 0; r < QR; ++r)
           sm.p[r0 + r][k] = key0 + k < sm.seen[r0 + r] ? acc[r] * scale : -INFINITY;
       }
       __syncthreads();
-      // Running maximum and sum: a warp has four rows, two keys per lane.
-      for (int r = warp; r < M; r += kSimtThreads / 32) {
-        const float x = sm.p[r][lane], y = sm.p[r][lane + 32];
-        float mx = fmaxf(x, y);
-        for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-        const float old = sm.m[r], m = fmaxf(old, mx), ref = m == -INFINITY ? 0.f : m;
-        const float px = exp2f(x - ref), py = exp2f(y - ref);
-        float sum = px + py;
-        for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-        sm.p[r][lane] = px;
-        sm.p[r][lane + 32] = py;
-        __syncwarp();
-        if (lane == 0) {
-          const float fix = exp2f(old - ref);
-          sm.m[r] = m;
-          sm.l[r] = fmaf(sm.l[r], fix, sum);
-          sm.fix[r] = fix;
+      fetch(t + 2);
+      // Running maximum and sum: a warp has four rows.
+      float sc[M / 4][BN / 32], mx[M / 4], sum[M / 4];
+#pragma unroll
+      for (int r = 0; r < M / 4; ++r) {
+        mx[r] = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < BN / 32; ++x) {
+          sc[r][x] = sm.p[warp * (M / 4) + r][lane + 32 * x];
+          mx[r] = fmaxf(mx[r], sc[r][x]);
+        }
+      }
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1)
+#pragma unroll
+        for (int r = 0; r < M / 4; ++r)
+          mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], w));
+#pragma unroll
+      for (int r = 0; r < M / 4; ++r) {
+        mx[r] = fmaxf(mx[r], sm.m[warp * (M / 4) + r]);
+        const float ref = mx[r] == -INFINITY ? 0.f : mx[r];
+        sum[r] = 0.f;
+#pragma unroll
+        for (int x = 0; x < BN / 32; ++x) {
+          sc[r][x] = exp2f(sc[r][x] - ref);
+          sum[r] += sc[r][x];
+          sm.p[warp * (M / 4) + r][lane + 32 * x] = sc[r][x];
+        }
+      }
+#pragma unroll
+      for (int w = 16; w > 0; w >>= 1)
+#pragma unroll
+        for (int r = 0; r < M / 4; ++r) sum[r] += __shfl_xor_sync(0xffffffffu, sum[r], w);
+      if (lane == 0) {
+#pragma unroll
+        for (int r = 0; r < M / 4; ++r) {
+          const int rr = warp * (M / 4) + r;
+          const float fix = exp2f(sm.m[rr] - (mx[r] == -INFINITY ? 0.f : mx[r]));
+          sm.m[rr] = mx[r];
+          sm.l[rr] = fmaf(sm.l[rr], fix, sum[r]);
+          sm.fix[rr] = fix;
         }
       }
       __syncthreads();
@@ -144,21 +179,30 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
 #pragma unroll
         for (int c = 0; c < CPT; ++c) o[r][c] *= sm.fix[rg * RPT + r];
       // A value that a row does not see must not reach its sums, not even
-      // times zero: it may be NaN.
-      const bool edge = key0 + nk > s.least;
-      for (int k = 0; k < nk; ++k) {
-        float v[CPT];
+      // times zero: it may be NaN. Behind the last key the values are zeros.
+      const bool edge = key0 + BN > s.least;
+#pragma unroll 2
+      for (int k = 0; k < BN; k += 4) {
+        float v[4][CPT];
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) v[c] = sm.v[k][col + c * kSimtThreads];
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[st][k + y][col + c * kSimtThreads];
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
-          if (edge && key0 + k >= sm.seen[rg * RPT + r]) continue;
-          const float p = sm.p[rg * RPT + r][k];
+          const float4 p4 = *reinterpret_cast<const float4 *>(&sm.p[rg * RPT + r][k]);
+          const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-          for (int c = 0; c < CPT; ++c) o[r][c] = fmaf(p, v[c], o[r][c]);
+          for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int c = 0; c < CPT; ++c) {
+              const float n = fmaf(p[y], v[y][c], o[r][c]);
+              o[r][c] = edge && key0 + k + y >= seen[r] ? o[r][c] : n;
+            }
         }
       }
     }
+    cp_async_wait<0>();
     __syncthreads();
     if (s.whole()) {
 #pragma unroll
@@ -167,9 +211,9 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         if (rr >= s.rows) continue;
         const RowAt at = row_at(a, s.row0, s.r0, s.h, rr);
         const float l = sm.l[rr], inv = l == 0.f ? 0.f : 1.f / l;
-        T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D;
+        float *out = static_cast<float *>(a.out) + (at.token * a.Hq + at.head) * D;
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) from_float(out + col + c * kSimtThreads, o[r][c] * inv);
+        for (int c = 0; c < CPT; ++c) out[col + c * kSimtThreads] = o[r][c] * inv;
         if (col == 0 && a.lse)
           a.lse[at.token * a.Hq + at.head] =
               l == 0.f ? -INFINITY : (sm.m[rr] + log2f(l)) * kLn2;
@@ -187,6 +231,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
           part[2 * M + (rg * RPT + r) * D + col + c * kSimtThreads] = o[r][c];
     }
   }
+  let_next_start();
 }
 
 constexpr int kJoinThreads = 256;
@@ -199,6 +244,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
   __shared__ int slots[kMaxCtas];
   __shared__ int n_slots;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  wait_for_previous();
   for (int which = 0; which < 2; ++which) {
     const int mine = blockIdx.x * 2 + which;
     const Desc d = a.desc[mine];
@@ -253,23 +299,35 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
   }
 }
 
-template <typename T, int D>
+template <int D>
 pair_status run_simt(const Args &a, cudaStream_t s) {
-  const int smem = sizeof(SimtSmem<D>);
-  PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<T, D>,
+  constexpr int smem = sizeof(SimtSmem<D>);
+  static_assert(smem <= 232448, "shared memory of a CTA");
+  PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int per_sm = D <= 128 ? 2 : 1;
-  const int ctas = min(kMaxCtas, per_sm * sm_count());
+  const int ctas = min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count());
   PAIR_BEGIN("attend_simt", s);
-  attend_simt_kernel<T, D><<<ctas, kSimtThreads, smem, s>>>(a);
+  attend_simt_kernel<D><<<ctas, kSimtThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
-  return launch_join(a, D, kSimtRows, ctas, sizeof(T) == 2 ? PAIR_BF16 : PAIR_F32, s);
+  return launch_join(a, D, kSimtRows, ctas, PAIR_F32, s);
 }
 
 template <typename T, int D>
 pair_status run_join(const Args &a, int M, int ctas, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, M / 16, 1);
+  cfg.blockDim = dim3(kJoinThreads, 1, 1);
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
   PAIR_BEGIN("attend_join", s);
-  attend_join_kernel<T, D><<<dim3(ctas, M / 16), kJoinThreads, 0, s>>>(a, M, ctas);
+  if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, a, M, ctas) != cudaSuccess) {
+    cudaGetLastError();
+    return PAIR_ERR_CUDA;
+  }
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
 }
@@ -297,11 +355,8 @@ int sm_count() {
   return n;
 }
 
-pair_status launch_simt(const Args &a, int D, pair_dtype dt, cudaStream_t s) {
-  return by_size(D, [&](auto d) {
-    return dt == PAIR_BF16 ? run_simt<__nv_bfloat16, decltype(d)::value>(a, s)
-                           : run_simt<float, decltype(d)::value>(a, s);
-  });
+pair_status launch_simt(const Args &a, int D, cudaStream_t s) {
+  return by_size(D, [&](auto d) { return run_simt<decltype(d)::value>(a, s); });
 }
 
 pair_status launch_join(const Args &a, int D, int M, int ctas, pair_dtype dt, cudaStream_t s) {
@@ -379,7 +434,7 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + desc_bytes()),
                dev_err};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (dt == PAIR_F32) return launch_simt(a, D, dt, s);
+  if (dt == PAIR_F32) return launch_simt(a, D, s);
   // Which kernel a chunk goes to is decided by its rows, on the device; a
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;

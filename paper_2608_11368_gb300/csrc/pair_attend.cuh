@@ -26,7 +26,7 @@
 namespace pairk {
 namespace attend {
 
-constexpr int kMaxCtas = 320;    // of one call, at most
+constexpr int kMaxCtas = 480;    // of one call, at most
 constexpr int kMaxRows = 256;    // rows of a unit, at most
 constexpr int kManyRows = 256;   // rows of a unit of the kernel for many rows
 constexpr int kFewRows = 64;     // rows of a unit of the kernel for few rows
@@ -329,8 +329,32 @@ __device__ __forceinline__ void add_not_finite(const Args &a, const Segment &s, 
   }
 }
 
+// Asynchronous 16-byte copy into shared memory, zeros where nothing is there.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there) {
+  const int bytes = there ? 16 : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// The pass that joins the partial sums is launched while the kernel before it
+// still runs (programmatic dependent launch): that kernel's blocks say when
+// they have no more work, the joining ones wait for its end.
+__device__ __forceinline__ void let_next_start() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // Host side: the kernels and the pass that joins their partial sums.
-pair_status launch_simt(const Args &a, int D, pair_dtype dt, cudaStream_t s);
+pair_status launch_simt(const Args &a, int D, cudaStream_t s);
 pair_status launch_few(const Args &a, int D, cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(const Args &a, int D, cudaStream_t s);

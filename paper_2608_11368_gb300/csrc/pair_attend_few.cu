@@ -13,18 +13,6 @@ constexpr int kWarps = kThreads / 32;
 constexpr int M = kFewRows;
 constexpr int BN = 64;  // keys of a tile
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there) {
-  const int bytes = there ? 16 : 0;  // the rest is zero-filled
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() {
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -52,7 +40,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 template <int D>
 struct Few {
-  static constexpr int kStages = D == 64 ? 5 : D == 128 ? 3 : 2;
+  static constexpr int kStages = D == 64 ? 4 : 2;
   static constexpr int kTile = BN * D * 2;          // bytes of a tile of keys or values
   static constexpr int kChunks = D / 8;             // 16-byte pieces of a row
   static constexpr int kRowsPerPass = kThreads / kChunks;
@@ -318,7 +306,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) attend_few_kernel(Args a) {
+__global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   const int cta = blockIdx.x, ctas = gridDim.x;
   clear_notes(a, cta);
@@ -335,6 +323,7 @@ __global__ void __launch_bounds__(kThreads) attend_few_kernel(Args a) {
     else
       few_segment<D, 4>(a, s, smem, cta, seg);
   }
+  let_next_start();
 }
 
 template <int D>
@@ -342,7 +331,7 @@ pair_status run_few(const Args &a, cudaStream_t s) {
   constexpr int smem = Few<D>::kBytes;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_few_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count());
+  const int ctas = min(kMaxCtas, (D <= 128 ? 3 : 1) * sm_count());
   PAIR_BEGIN("attend_few", s);
   attend_few_kernel<D><<<ctas, kThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);

@@ -562,6 +562,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     softmax<D>(a, sm, walk, cta);
   }
+  let_next_start();
   tc_fence_before();
   __syncthreads();
   if (warp == 9) {

@@ -6,8 +6,8 @@
 namespace pairk {
 namespace {
 
-constexpr int kExtendThreads = 1024;
-constexpr int kExtendTokens = 1024;  // slots a block fills
+constexpr int kExtendThreads = 512;
+constexpr int kExtendTokens = 2048;  // slots a block fills
 
 struct ExtendArgs {
   int32_t R, page, width;
@@ -33,39 +33,38 @@ __device__ __forceinline__ Need request_need(const ExtendArgs &a, int i) {
   const int32_t n = a.n_new[i];
   r.n = n > 0 ? n : 0;
   const int64_t kv = (int64_t)r.len + r.n;
-  const int64_t total = (kv + a.page - 1) / a.page;
+  // (32 bits: a division of 64 costs some hundred instructions.)
+  const uint32_t total = kv <= 0 ? 0 : (uint32_t)(kv - 1) / (uint32_t)a.page + 1;
   r.bad = r.len < 0 || r.held < 0 || n < 0 || r.held > a.width || kv > INT32_MAX ||
-          (int64_t)r.held * a.page < r.len || total > a.width;
-  r.pages = r.bad ? 0 : (int32_t)(total > r.held ? total - r.held : 0);
+          (int64_t)r.held * a.page < r.len || total > (uint32_t)a.width;
+  r.pages = r.bad || total <= (uint32_t)r.held ? 0 : (int32_t)(total - r.held);
   return r;
 }
 
-// A request whose tokens a block fills: first row, pages taken before it.
-struct Filled {
-  int32_t i, len, held, n, ok;
-  int64_t row, first;
-};
-
 // The prefix sums of tokens and of pages over all requests are formed by
-// every block for itself (12 bytes per request, from L2 after the first), so
-// one launch does: block b writes the requests of its share and the slots
-// [b kExtendTokens, (b+1) kExtendTokens). A slot's page is read from the old
-// table entries or from the free list, never from entries this launch writes.
-// Bound by latency: loads of the lengths, one block scan, dependent page
-// reads, stores.
+// every block for itself (12 bytes per request, from L2 after the first), a
+// run of consecutive requests per thread, so one launch does. Block b writes
+// the requests of its share and the slots [b kExtendTokens, (b+1)
+// kExtendTokens): a thread finds its token's request by bisection over the
+// runs and a walk along the run. A slot's page is read from the old table
+// entries or from the free list, never from entries this launch writes. Bound
+// by latency: loads of the lengths, one block scan, the bisection, two
+// dependent loads, stores (64 requests of one token 5 us with the launch,
+// 4096 of 128 on average 9; a list of requests per block, a warp to each, took 38).
 __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs a) {
   __shared__ int64_t warp_n[32], warp_p[32];
-  __shared__ Filled list[kExtendTokens];
-  __shared__ int n_list, last_page;
+  __shared__ int64_t run_n[kExtendThreads], run_p[kExtendThreads];  // sums before a run
+  __shared__ int last_page;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.R + kExtendThreads - 1) / kExtendThreads;
-  const int i0 = min((int64_t)tid * per, (int64_t)a.R), i1 = min(i0 + per, a.R);
+  const int i0 = (int)min((int64_t)tid * per, (int64_t)a.R), i1 = min(i0 + per, a.R);
   int64_t sn = 0, sp = 0;
   for (int i = i0; i < i1; ++i) {
     const Need r = request_need(a, i);
     sn += r.n;
     sp += r.pages;
   }
+  const int32_t avail = min(max(a.free_count[0], 0), a.free_capacity);
   int64_t xn = sn, xp = sp;
   for (int o = 1; o < 32; o <<= 1) {
     const int64_t yn = __shfl_up_sync(0xffffffffu, xn, o);
@@ -79,13 +78,11 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
     warp_n[warp] = xn;
     warp_p[warp] = xp;
   }
-  if (tid == 0) {
-    n_list = 0;
-    last_page = 0;
-  }
+  if (tid == 0) last_page = 0;
   __syncthreads();
   if (warp == 0) {
-    int64_t yn = warp_n[lane], yp = warp_p[lane];
+    const bool there = lane < kExtendThreads / 32;
+    int64_t yn = there ? warp_n[lane] : 0, yp = there ? warp_p[lane] : 0;
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t zn = __shfl_up_sync(0xffffffffu, yn, o);
       const int64_t zp = __shfl_up_sync(0xffffffffu, yp, o);
@@ -101,50 +98,66 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
   const int64_t total_n = warp_n[31];
   xn += (warp ? warp_n[warp - 1] : 0) - sn;  // exclusive
   xp += (warp ? warp_p[warp - 1] : 0) - sp;
-  const int32_t avail = min(max(a.free_count[0], 0), a.free_capacity);
+  run_n[tid] = xn;
+  run_p[tid] = xp;
+  __syncthreads();
+
   const int64_t t0 = (int64_t)blockIdx.x * kExtendTokens;
   const int64_t t1 = min(t0 + kExtendTokens, a.T);
+  for (int64_t t = t0 + tid; t < t1; t += kExtendThreads) {
+    int64_t slot = -1;
+    if (t < total_n) {
+      int lo = 0, hi = kExtendThreads;  // run_n[lo] <= t < run_n[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (run_n[mid] <= t) lo = mid; else hi = mid;
+      }
+      int i = lo * per;
+      int64_t row = run_n[lo], first = run_p[lo];
+      Need r = request_need(a, i);
+      while (row + r.n <= t) {
+        row += r.n;
+        first += r.pages;
+        r = request_need(a, ++i);
+      }
+      if (!r.bad && first + r.pages <= avail && row + r.n <= a.T) {
+        const uint32_t pos = r.len + (uint32_t)(t - row);
+        const uint32_t at = pos / (uint32_t)a.page;
+        const uint32_t off = pos - at * (uint32_t)a.page;
+        int32_t *entry = a.table + (int64_t)i * a.width + at;
+        const bool fresh = (int32_t)at >= r.held;
+        const int32_t id = fresh ? a.free_pages[first + at - r.held] : *entry;
+        // The held pages cover the cached tokens, so a new one begins with a
+        // new token, whose thread enters it.
+        if (fresh && off == 0) *entry = id;
+        slot = (int64_t)id * a.page + off;
+      }
+    }
+    a.slots[t] = slot;
+  }
+
   const int share = (a.R + gridDim.x - 1) / gridDim.x;
-  const int r0 = blockIdx.x * share, r1 = min(r0 + share, a.R);
+  const int r0 = (int)min((int64_t)blockIdx.x * share, (int64_t)a.R), r1 = min(r0 + share, a.R);
   for (int i = i0; i < i1; ++i) {
+    // Another block's requests count as far as this block's lie behind them in
+    // the run (in block 0, which looks for the last page taken, all do).
+    if (blockIdx.x != 0 && (i1 <= r0 || i >= r1)) break;
+    const bool mine = i >= r0 && i < r1;
     const Need r = request_need(a, i);
     const bool ok = !r.bad && xp + r.pages <= avail && xn + r.n <= a.T;
     if (ok && r.pages && blockIdx.x == 0) atomicMax(&last_page, (int32_t)(xp + r.pages));
-    if (i >= r0 && i < r1) {
+    if (mine) {
       a.kv_len[i] = ok ? r.len + r.n : max(r.len, 0);
       a.held_out[i] = r.held + (ok ? r.pages : 0);
       a.cu[i + 1] = (int32_t)min(xn + r.n, a.T);
       if (i == 0) a.cu[0] = 0;
-      if (ok) {
-        int32_t *row = a.table + (int64_t)i * a.width + r.held;
-        for (int j = 0; j < r.pages; ++j) row[j] = a.free_pages[xp + j];
-      } else {
-        flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
-      }
+      if (!ok) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
     }
-    if (r.n > 0 && xn < t1 && xn + r.n > t0)
-      list[atomicAdd(&n_list, 1)] = {i, r.len, r.held, r.n, ok, xn, xp};
     xn += r.n;
     xp += r.pages;
   }
   __syncthreads();
   if (blockIdx.x == 0 && tid == 0) a.taken[0] = last_page;
-  for (int e = warp; e < n_list; e += kExtendThreads / 32) {
-    const Filled f = list[e];
-    const int64_t lo = max(f.row, t0), hi = min(f.row + f.n, t1);
-    for (int64_t t = lo + lane; t < hi; t += 32) {
-      int64_t slot = -1;
-      if (f.ok) {
-        const int64_t pos = f.len + (t - f.row);
-        const int32_t at = (int32_t)(pos / a.page);
-        const int32_t id = at < f.held ? a.table[(int64_t)f.i * a.width + at]
-                                       : a.free_pages[f.first + at - f.held];
-        slot = (int64_t)id * a.page + (pos - (int64_t)at * a.page);
-      }
-      a.slots[t] = slot;
-    }
-  }
-  for (int64_t t = max(t0, total_n) + tid; t < t1; t += kExtendThreads) a.slots[t] = -1;
 }
 
 struct AppendArgs {

@@ -30,11 +30,29 @@ struct VerifyArgs {
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// A weight in units of 2^-40. The scaling is exact, so the truncation is the
-// only rounding; sums of up to 2^22 weights fit 63 bits and, being integers,
-// do not depend on their order.
-__device__ __forceinline__ long long fixed_weight(float x) {
-  return (long long)(fminf(fmaxf(x, 0.f), 1.f) * 1099511627776.f);
+// Weights in units of 2^-40, w = floor(2^40 x) for x in [0, 1], summed over a
+// vector: fp32 additions that round towards zero leave the upper and the lower
+// 20 bits in the significand (8 + x in steps of 2^-20, then what is left of x
+// plus 2^-17 in steps of 2^-40), where integer additions read them off. The
+// sums of up to 2^22 weights fit 63 bits and, being integers, do not depend on
+// their order. (Conversions to 64-bit integers go through the fp64 pipe: 80 %
+// busy with them, 256 rows of p and q took 104 us.)
+struct Weight {
+  uint32_t hi, lo;  // bits of the two sums, without their constants
+  __device__ __forceinline__ long long value() const {
+    return ((long long)hi << 20) + lo;
+  }
+};
+__device__ __forceinline__ Weight fixed_weight(float x) {
+  const float t = __fadd_rz(x, 8.f);
+  const float rest = x - (t - 8.f);
+  return {__float_as_uint(t) - 0x41000000u, __float_as_uint(__fadd_rz(rest, 0x1p-17f)) - 0x37000000u};
+}
+// a - b held to [0, 1]; NaN gives 0.
+__device__ __forceinline__ float sub_sat(float a, float b) {
+  float o;
+  asm("sub.sat.f32 %0, %1, %2;" : "=f"(o) : "f"(a), "f"(b));
+  return o;
 }
 
 // VEC consecutive values from element e of a row of V (elements outside it
@@ -59,17 +77,29 @@ struct Source {
   const T *p, *q;
   int V, skip;
   static constexpr int VEC = 16 / sizeof(T);
-  __device__ __forceinline__ void weights(int e, long long (&w)[VEC]) const {
-    float a[VEC];
-    load_vec<T, VEC>(p, e, V, a);
+  __device__ __forceinline__ void load(int e, float (&x)[VEC]) const {
+    load_vec<T, VEC>(p, e, V, x);
     if (q) {
-      float b[VEC];
-      load_vec<T, VEC>(q, e, V, b);
+      float y[VEC];
+      load_vec<T, VEC>(q, e, V, y);
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) a[k] -= b[k];
+      for (int k = 0; k < VEC; ++k) x[k] = sub_sat(x[k], y[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) x[k] = e + k == skip ? 0.f : __saturatef(x[k]);
     }
+  }
+  __device__ __forceinline__ long long sum(int e) const {
+    float x[VEC];
+    load(e, x);
+    Weight s{0, 0};
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) w[k] = e + k == skip ? 0 : fixed_weight(a[k]);
+    for (int k = 0; k < VEC; ++k) {
+      const Weight w = fixed_weight(x[k]);
+      s.hi += w.hi;
+      s.lo += w.lo;
+    }
+    return s.value();
   }
 };
 
@@ -157,12 +187,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
   for (int pass = 0; pass < 2; ++pass) {
     long long sum = 0;
 #pragma unroll 4
-    for (int v = v0 + lane; v < v1; v += 32) {
-      long long w[VEC];
-      src.weights(v * VEC - mis, w);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) sum += w[k];
-    }
+    for (int v = v0 + lane; v < v1; v += 32) sum += src.sum(v * VEC - mis);
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();
@@ -199,33 +224,48 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
     at = max(min(at, total - 1), 0ll);
     for (int k = 0; k < warp; ++k) before += s_warp[k];
     if (at < before || at >= before + s_warp[warp]) return;
-    for (int vb = v0; vb < v1; vb += 32) {
-      const int v = vb + lane;
-      long long w[VEC] = {}, mine = 0;
-      if (v < v1) src.weights(v * VEC - mis, w);
+    // This warp's segment again, kAhead pieces of 32 vectors in flight.
+    constexpr int kAhead = 8;
+    for (int vb = v0; vb < v1; vb += 32 * kAhead) {
+      long long mine[kAhead], all[kAhead];
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) mine += w[k];
-      long long incl = mine;
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
+      for (int x = 0; x < kAhead; ++x) {
+        const int v = vb + x * 32 + lane;
+        mine[x] = v < v1 ? src.sum(v * VEC - mis) : 0;
+        all[x] = mine[x];
       }
-      long long c = before + incl - mine;
-      if (at >= c && at < c + mine) {
-        int tok = 0;
 #pragma unroll
-        for (int k = VEC - 1; k >= 0; --k) {  // the lowest k whose sum passes `at`
-          long long upto = c;
+      for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-          for (int j = 0; j <= k; ++j) upto += w[j];
-          if (upto > at) tok = v * VEC - mis + k;
+        for (int x = 0; x < kAhead; ++x) all[x] += __shfl_xor_sync(0xffffffffu, all[x], o);
+#pragma unroll
+      for (int x = 0; x < kAhead; ++x) {
+        if (at >= before + all[x]) {
+          before += all[x];
+          continue;
         }
-        a.out_ids[row] = tok;
-        if (a.logp) a.logp[row] = logf(as_float(prow[tok]));
-        a.n_emit[i] = first + 1;
+        long long incl = mine[x];
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += y;
+        }
+        long long c = before + incl - mine[x];
+        if (at >= c && at < c + mine[x]) {
+          const int e = (vb + x * 32 + lane) * VEC - mis;
+          float f[VEC];
+          src.load(e, f);
+          int tok = e;
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) {  // the first k whose sum passes `at`
+            c += fixed_weight(f[k]).value();
+            if (c <= at) tok = e + k + 1;
+          }
+          a.out_ids[row] = tok;
+          if (a.logp) a.logp[row] = logf(as_float(prow[tok]));
+          a.n_emit[i] = first + 1;
+        }
+        return;
       }
-      before += __shfl_sync(0xffffffffu, incl, 31);
-      if (before > at) return;
     }
     return;
   }
