@@ -6,7 +6,7 @@
 namespace pairk {
 namespace {
 
-constexpr int kExtendThreads = 512;
+constexpr int kExtendThreads = 1024;
 constexpr int kExtendTokens = 2048;  // slots a block fills
 
 struct ExtendArgs {
@@ -51,7 +51,7 @@ __device__ __forceinline__ Need request_need(const ExtendArgs &a, int i) {
 // by latency: loads of the lengths, one block scan, the bisection, two
 // dependent loads, stores (64 requests of one token 5 us with the launch,
 // 4096 of 128 on average 9; a list of requests per block, a warp to each, took 38).
-__global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs a) {
+__global__ void __launch_bounds__(kExtendThreads, 2) pages_extend_kernel(ExtendArgs a) {
   __shared__ int64_t warp_n[32], warp_p[32];
   __shared__ int64_t run_n[kExtendThreads], run_p[kExtendThreads];  // sums before a run
   __shared__ int last_page;
@@ -138,6 +138,7 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
 
   const int share = (a.R + gridDim.x - 1) / gridDim.x;
   const int r0 = (int)min((int64_t)blockIdx.x * share, (int64_t)a.R), r1 = min(r0 + share, a.R);
+  int top = 0;
   for (int i = i0; i < i1; ++i) {
     // Another block's requests count as far as this block's lie behind them in
     // the run (in block 0, which looks for the last page taken, all do).
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
     const bool mine = i >= r0 && i < r1;
     const Need r = request_need(a, i);
     const bool ok = !r.bad && xp + r.pages <= avail && xn + r.n <= a.T;
-    if (ok && r.pages && blockIdx.x == 0) atomicMax(&last_page, (int32_t)(xp + r.pages));
+    if (ok && r.pages) top = (int32_t)(xp + r.pages);
     if (mine) {
       a.kv_len[i] = ok ? r.len + r.n : max(r.len, 0);
       a.held_out[i] = r.held + (ok ? r.pages : 0);
@@ -156,8 +157,11 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
     xn += r.n;
     xp += r.pages;
   }
+  if (blockIdx.x != 0) return;
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (lane == 0 && top) atomicMax(&last_page, top);
   __syncthreads();
-  if (blockIdx.x == 0 && tid == 0) a.taken[0] = last_page;
+  if (tid == 0) a.taken[0] = last_page;
 }
 
 struct AppendArgs {
@@ -173,28 +177,44 @@ struct AppendArgs {
   int32_t *dev_err;
 };
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 128;
+constexpr int kAppendAhead = 4;  // 16-byte pieces of keys and of values in flight per lane
 
-// A thread moves one 16-byte piece of a token's keys and the same piece of its
-// values. Bound by HBM: every byte is read and written once.
+// A warp moves a token's keys and values; its slot is taken apart once. Bound by
+// HBM: every byte is read and written once.
 __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs a) {
-  const int64_t total = a.T * a.vecs;
-  for (int64_t x = (int64_t)blockIdx.x * kAppendThreads + threadIdx.x; x < total;
-       x += (int64_t)gridDim.x * kAppendThreads) {
-    const int64_t t = x / a.vecs;
-    const int piece = (int)(x - t * a.vecs);
-    const int64_t slot = a.slots[t];
-    if (slot == -1) continue;
-    if (slot < 0 || slot >= a.n_slots) {
-      flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
-      continue;
+  const int lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
+  if (t >= a.T) return;
+  const int64_t slot = a.slots[t];
+  if (slot == -1) return;
+  if (slot < 0 || slot >= a.n_slots) {
+    if (lane == 0) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+    return;
+  }
+  const int64_t pg = a.n_slots <= INT32_MAX ? (uint32_t)slot / (uint32_t)a.page : slot / a.page;
+  const int64_t off = slot - pg * a.page;
+  const uint4 *k = a.k + t * a.k_row, *v = a.v + t * a.v_row;
+  uint4 *kc = a.kc + pg * a.ks.for_page + off * a.ks.for_token;
+  uint4 *vc = a.vc + pg * a.vs.for_page + off * a.vs.for_token;
+  for (int x0 = lane; x0 < a.vecs; x0 += 32 * kAppendAhead) {
+    uint4 kx[kAppendAhead], vx[kAppendAhead];
+#pragma unroll
+    for (int y = 0; y < kAppendAhead; ++y) {
+      const int x = x0 + 32 * y, h = x / a.vecs_per_head, c = x - h * a.vecs_per_head;
+      if (x < a.vecs) {
+        kx[y] = __ldg(k + h * a.k_head + c);
+        vx[y] = __ldg(v + h * a.v_head + c);
+      }
     }
-    const int h = piece / a.vecs_per_head, c = piece - h * a.vecs_per_head;
-    const uint4 kx = a.k[t * a.k_row + h * a.k_head + c];
-    const uint4 vx = a.v[t * a.v_row + h * a.v_head + c];
-    const int64_t pg = slot / a.page, off = slot - pg * a.page;
-    a.kc[pg * a.ks.for_page + off * a.ks.for_token + h * a.ks.for_head + c] = kx;
-    a.vc[pg * a.vs.for_page + off * a.vs.for_token + h * a.vs.for_head + c] = vx;
+#pragma unroll
+    for (int y = 0; y < kAppendAhead; ++y) {
+      const int x = x0 + 32 * y, h = x / a.vecs_per_head, c = x - h * a.vecs_per_head;
+      if (x < a.vecs) {
+        kc[h * a.ks.for_head + c] = kx[y];
+        vc[h * a.vs.for_head + c] = vx[y];
+      }
+    }
   }
 }
 
@@ -272,10 +292,8 @@ pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt, 
                      cut(ks),
                      cut(vs),
                      dev_err};
-  const int64_t blocks = ceil_div(T * a.vecs, kAppendThreads);
   PAIR_BEGIN("cache_append", s);
-  cache_append_kernel<<<(unsigned)(blocks < (1 << 30) ? blocks : (1 << 30)), kAppendThreads, 0,
-                        s>>>(a);
+  cache_append_kernel<<<(unsigned)ceil_div(T, kAppendThreads / 32), kAppendThreads, 0, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
 }

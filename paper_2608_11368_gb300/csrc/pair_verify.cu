@@ -2,6 +2,8 @@
 // the token that follows the accepted ones (speculative sampling).
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "pair_common.cuh"
 #include "tc_ptx.cuh"
 
@@ -10,14 +12,15 @@ namespace {
 
 using namespace tc;
 
-constexpr int kVerifyThreads = 512;
-constexpr int kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifyMaxCluster = 8;
+constexpr int kVerifyWarps = 8;  // that read probabilities; one more controls
+constexpr int kVerifyThreads = (kVerifyWarps + 1) * 32;
+constexpr int kVerifyMaxCluster = 16;
+constexpr int kVerifyLeast = 2048;  // values of a row worth a CTA of its own
 
 template <typename T>
 struct VerifyArgs {
   int64_t T_rows;
-  int32_t R, V, C;  // C: CTAs per request
+  int32_t R, V, C, clusters;  // C: CTAs of a cluster
   const T *p, *q;
   int64_t p_row, q_row;
   const int32_t *ids, *cu;
@@ -55,43 +58,38 @@ __device__ __forceinline__ float sub_sat(float a, float b) {
   return o;
 }
 
-// VEC consecutive values from element e of a row of V (elements outside it
-// are 0): one 16-byte load where the address allows it.
-template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T *row, int e, int V, float (&x)[VEC]) {
-  const T *at = row + e;
-  if (e >= 0 && e + VEC <= V && (reinterpret_cast<uintptr_t>(at) & 15u) == 0) {
-    const uint4 r = __ldg(reinterpret_cast<const uint4 *>(at));
-    const T *t = reinterpret_cast<const T *>(&r);
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = as_float(t[k]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) x[k] = e + k >= 0 && e + k < V ? as_float(at[k]) : 0.f;
-  }
-}
-
-// What a draw is made from: p alone, p - q, or p without the draft.
+// What a draw is made from: p alone, p - q, or p without the draft. The row is
+// cut into vectors of 16 bytes, counted from the boundary at or before its
+// first element; those that lie in it whole are loaded whole (q's too, where it
+// lies the same way), kPieces of them per lane in flight.
+constexpr int kPieces = 4;
 template <typename T>
 struct Source {
+  static constexpr int VEC = 16 / sizeof(T);
   const T *p, *q;
   int V, skip;
-  static constexpr int VEC = 16 / sizeof(T);
-  __device__ __forceinline__ void load(int e, float (&x)[VEC]) const {
-    load_vec<T, VEC>(p, e, V, x);
-    if (q) {
-      float y[VEC];
-      load_vec<T, VEC>(q, e, V, y);
+  int mis, n_vec, whole0, whole1;  // vectors [whole0, whole1) lie in the row
+  bool q_alike;
+
+  __device__ __forceinline__ Source(const T *p_, const T *q_, int V_, int skip_)
+      : p(p_), q(q_), V(V_), skip(skip_) {
+    mis = (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+    n_vec = (V + mis + VEC - 1) / VEC;
+    whole0 = mis ? 1 : 0;
+    whole1 = (V + mis) / VEC;
+    q_alike = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15u) == 0;
+  }
+  // One vector, element by element; elements outside the row are 0.
+  __device__ __forceinline__ void load(int v, float (&x)[VEC]) const {
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) x[k] = sub_sat(x[k], y[k]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) x[k] = e + k == skip ? 0.f : __saturatef(x[k]);
+    for (int k = 0; k < VEC; ++k) {
+      const int e = v * VEC - mis + k;
+      x[k] = 0.f;
+      if (e >= 0 && e < V && e != skip)
+        x[k] = sub_sat(as_float(p[e]), q ? as_float(q[e]) : 0.f);
     }
   }
-  __device__ __forceinline__ long long sum(int e) const {
-    float x[VEC];
-    load(e, x);
+  static __device__ __forceinline__ long long sum(const float (&x)[VEC]) {
     Weight s{0, 0};
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
@@ -101,189 +99,298 @@ struct Source {
     }
     return s.value();
   }
+  // Sums of the lane's vectors vb + 32 x + lane below v1, x < kPieces.
+  __device__ __forceinline__ void pieces(int vb, int v1, long long (&s)[kPieces]) const {
+    const int lane = threadIdx.x & 31;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    uint4 a[kPieces], b[kPieces];
+    const bool two = q && q_alike;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int v = vb + 32 * x + lane;
+      const bool in = v >= whole0 && v < whole1 && v < v1 && !(q && !q_alike);
+      a[x] = b[x] = zero;
+      if (in) a[x] = __ldg(reinterpret_cast<const uint4 *>(p - mis) + v);
+      if (in && two) b[x] = __ldg(reinterpret_cast<const uint4 *>(q - mis) + v);
+    }
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int v = vb + 32 * x + lane;
+      const T *t = reinterpret_cast<const T *>(&a[x]), *u = reinterpret_cast<const T *>(&b[x]);
+      float f[VEC];
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        f[k] = sub_sat(as_float(t[k]), as_float(u[k]));
+        if (!q && v * VEC - mis + k == skip) f[k] = 0.f;
+      }
+      s[x] = sum(f);
+      if (v < v1 && (v < whole0 || v >= whole1 || (q && !q_alike))) {
+        load(v, f);
+        s[x] = sum(f);
+      }
+    }
+  }
 };
 
-// One cluster of C CTAs per request. Every CTA decides the request's drafts
-// for itself (a handful of gathers), then sums the weights of its share of
-// the vocabulary; each warp has a contiguous segment. The shares' sums meet
-// through distributed shared memory, and the one warp whose segment holds the
-// threshold goes over that segment again. Bound by HBM: one row of p, and of q
-// where a draft was refused, per request; C CTAs bring a single request's row
-// in when there are few.
+// By a warp: the token in whose weight `at` falls, the vectors [v0, v1) of the
+// row coming after weights of sum `before`; -1 in the lanes that do not have it.
+template <typename T>
+__device__ __forceinline__ int find(const Source<T> &src, int v0, int v1, long long before,
+                                    long long at) {
+  constexpr int VEC = Source<T>::VEC;
+  const int lane = threadIdx.x & 31;
+  for (int vb = v0; vb < v1; vb += 32 * kPieces) {
+    long long mine[kPieces], all[kPieces];
+    src.pieces(vb, v1, mine);
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) all[x] = mine[x];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x) all[x] += __shfl_xor_sync(0xffffffffu, all[x], o);
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      if (at >= before + all[x]) {
+        before += all[x];
+        continue;
+      }
+      long long incl = mine[x];
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      long long c = before + incl - mine[x];
+      if (at < c || at >= c + mine[x]) return -1;
+      const int v = vb + x * 32 + lane;
+      float f[VEC];
+      src.load(v, f);
+      int tok = v * VEC - src.mis;
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {  // the first element whose sum passes `at`
+        c += fixed_weight(f[k]).value();
+        tok += c <= at;
+      }
+      return tok;
+    }
+  }
+  return -1;
+}
+
+// What a request's drafts came to.
+struct Decision {
+  int lo, hi;  // rows of the chunk (hi <= lo: none)
+  int row;     // of the first draft refused, or the last one
+  int bad;     // that draft is no token
+  int skip;    // the token left out of the draw where the drafter has no probabilities
+};
+
+// By one warp, every lane gets it.
+template <typename T>
+__device__ Decision decide(const VerifyArgs<T> &a, int i) {
+  const int lane = threadIdx.x & 31;
+  const int lo = a.cu[i], hi = a.cu[i + 1];
+  if (lo < 0 || hi < lo || hi > a.T_rows) return {0, -1, 0, 0, -1};
+  Decision d{lo, hi, hi - 1, 0, -1};
+  for (int t0 = lo; t0 < hi - 1; t0 += 32) {
+    const int t = t0 + lane;
+    bool refuse = false;
+    int y = 0;
+    if (t < hi - 1) {
+      y = a.ids[t + 1];
+      refuse = true;
+      if (y >= 0 && y < a.V) {
+        const float py = as_float(a.p[t * a.p_row + y]);
+        const float qy = a.q ? as_float(a.q[t * a.q_row + y]) : 1.f;
+        refuse = !(a.u[t] * qy < py);
+      }
+    }
+    const unsigned any = __ballot_sync(0xffffffffu, refuse);
+    if (any) {
+      d.row = t0 + __ffs(any) - 1;
+      y = __shfl_sync(0xffffffffu, y, __ffs(any) - 1);
+      d.bad = y < 0 || y >= a.V;
+      d.skip = a.q || d.bad ? -1 : y;
+      break;
+    }
+  }
+  return d;
+}
+
+// Clusters of C CTAs, each cluster one request after another. The reading
+// warps of its CTAs sum the weights of a share of the vocabulary each, a
+// contiguous segment per warp; the CTAs' sums meet through distributed shared
+// memory. A ninth warp of each CTA decides the next request's drafts (three
+// dependent loads) while the others read, writes the accepted tokens, and,
+// where the draw falls into its CTA, goes over that warp's segment again while
+// the others are at the next request: with the reading warps doing this, a row
+// took 8 of 22 us in which nothing was read. Bound by HBM: one row of p, and of
+// q where a draft was refused, per request.
 template <typename T>
 __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a) {
-  constexpr int VEC = Source<T>::VEC;
-  __shared__ int s_first, s_bad;
-  __shared__ long long s_warp[kVerifyWarps];
+  __shared__ Decision s_dec[2];
+  __shared__ long long s_warp[2][kVerifyWarps];
   __shared__ long long s_cta[2][kVerifyMaxCluster];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int C = a.C, rank = blockIdx.x % C, i = blockIdx.x / C;
-  const int lo = a.cu[i], hi = a.cu[i + 1];
-  const bool sane = lo >= 0 && hi >= lo && hi <= a.T_rows;
-  if (rank == 0 && i == a.R - 1 && sane) {
-    for (int64_t t = hi + tid; t < a.T_rows; t += kVerifyThreads) {
+  const int C = a.C, rank = blockIdx.x % C, cluster = blockIdx.x / C;
+  const bool control = warp == kVerifyWarps;
+  if (blockIdx.x == gridDim.x - 1) {  // rows that no request owns
+    const int t0 = max(0, a.cu[a.R]);
+    for (int64_t t = t0 + tid; t < a.T_rows; t += kVerifyThreads) {
       a.out_ids[t] = -1;
       if (a.logp) a.logp[t] = 0.f;
     }
   }
-  if (!sane || hi == lo) {
-    if (rank == 0 && tid == 0) {
-      a.n_emit[i] = 0;
-      if (!sane) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
-    }
-    return;  // the whole cluster
-  }
-  // Drafts: the first one refused, or the last row.
-  if (warp == 0) {
-    const int K = hi - lo - 1;
-    int first = K, bad = 0;
-    for (int j0 = 0; j0 < K && first == K; j0 += 32) {
-      const int j = j0 + lane;
-      bool refuse = false, out = false;
-      if (j < K) {
-        const int y = a.ids[lo + j + 1];
-        out = y < 0 || y >= a.V;
-        if (out) {
-          refuse = true;
-        } else {
-          const float py = as_float(a.p[(lo + j) * a.p_row + y]);
-          const float qy = a.q ? as_float(a.q[(lo + j) * a.q_row + y]) : 1.f;
-          refuse = !(a.u[lo + j] * qy < py);
-        }
-      }
-      const unsigned any = __ballot_sync(0xffffffffu, refuse);
-      if (any) {
-        first = j0 + __ffs(any) - 1;
-        bad = __shfl_sync(0xffffffffu, (int)out, __ffs(any) - 1);
-      }
-    }
-    if (lane == 0) {
-      s_first = first;
-      s_bad = bad;
-    }
+  if (control) {
+    const Decision d = decide(a, cluster);
+    if (lane == 0) s_dec[0] = d;
   }
   __syncthreads();
-  const int first = s_first, row = lo + first;
-  const bool drafted = row + 1 < hi;
-  const T *prow = a.p + row * a.p_row;
-  Source<T> src{prow, drafted && a.q ? a.q + row * a.q_row : nullptr, a.V,
-                drafted && !a.q && !s_bad ? a.ids[row + 1] : -1};
-  if (rank == 0) {
-    if (s_bad && tid == 0) flag_error(a.dev_err, PAIR_DEV_ERR_TARGET_RANGE);
-    for (int t = lo + tid; t < hi; t += kVerifyThreads) {
-      if (t == row) continue;
-      const int y = t < row ? a.ids[t + 1] : -1;
-      a.out_ids[t] = y;
-      if (a.logp) a.logp[t] = t < row ? logf(as_float(a.p[t * a.p_row + y])) : 0.f;
-    }
-  }
-  // Segments in whole vectors, counted from the 16-byte boundary at or before
-  // the row of p.
-  const int mis = (int)((reinterpret_cast<uintptr_t>(prow) & 15u) / sizeof(T));
-  const int n_vec = (int)ceil_div((int64_t)a.V + mis, VEC);
-  const int n_seg = C * kVerifyWarps;
-  const int per = (n_vec + n_seg - 1) / n_seg;
-  const int v0 = min((rank * kVerifyWarps + warp) * per, n_vec), v1 = min(v0 + per, n_vec);
-  for (int pass = 0; pass < 2; ++pass) {
-    long long sum = 0;
-#pragma unroll 4
-    for (int v = v0 + lane; v < v1; v += 32) sum += src.sum(v * VEC - mis);
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s_warp[warp] = sum;
-    __syncthreads();
-    if (warp == 0) {
-      long long x = lane < kVerifyWarps ? s_warp[lane] : 0;
-      for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-      if (lane < C) {
-        const uint32_t to = mapa(smem_u32(&s_cta[pass][rank]), lane);
-        asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(x) : "memory");
+  int round = 0;  // of the exchange, alternating between two buffers
+  for (int i = cluster, it = 0; i < a.R; i += a.clusters, ++it) {
+    const Decision d = s_dec[it & 1];
+    const bool empty = d.hi <= d.lo;
+    if (control) {
+      if (i + a.clusters < a.R) {
+        const Decision next = decide(a, i + a.clusters);
+        if (lane == 0) s_dec[(it + 1) & 1] = next;
+      }
+      if (rank == 0) {
+        if (empty && lane == 0) {
+          a.n_emit[i] = 0;
+          if (d.hi < d.lo) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+        }
+        if (d.bad && lane == 0) flag_error(a.dev_err, PAIR_DEV_ERR_TARGET_RANGE);
+        for (int t = d.lo + lane; t < d.hi; t += 32) {
+          if (t == d.row) continue;
+          const int y = t < d.row ? a.ids[t + 1] : -1;
+          a.out_ids[t] = y;
+          if (a.logp) a.logp[t] = t < d.row ? logf(as_float(a.p[t * a.p_row + y])) : 0.f;
+        }
       }
     }
-    cluster_sync();
-    long long total = 0, before = 0;
-    for (int c = 0; c < C; ++c) {
-      if (c == rank) before = total;
-      total += s_cta[pass][c];
+    if (empty) {
+      __syncthreads();
+      continue;
     }
-    if (total == 0) {
-      if (pass == 0) {  // nothing left of the difference: p alone
+    const T *prow = a.p + d.row * a.p_row;
+    Source<T> src(prow, d.row + 1 < d.hi && a.q ? a.q + d.row * a.q_row : nullptr, a.V, d.skip);
+    const int n_vec = src.n_vec;
+    const int n_seg = C * kVerifyWarps;
+    const int per = (n_vec + n_seg - 1) / n_seg;
+    for (int pass = 0; pass < 2; ++pass) {
+      const int buf = round++ & 1;
+      if (!control) {
+        const int v0 = min((rank * kVerifyWarps + warp) * per, n_vec), v1 = min(v0 + per, n_vec);
+        long long sum = 0;
+        for (int vb = v0; vb < v1; vb += 32 * kPieces) {
+          long long x[kPieces];
+          src.pieces(vb, v1, x);
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) sum += x[k];
+        }
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) s_warp[buf][warp] = sum;
+      }
+      __syncthreads();
+      if (control) {
+        long long x = lane < kVerifyWarps ? s_warp[buf][lane] : 0;
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (lane < C) {
+          const uint32_t to = mapa(smem_u32(&s_cta[buf][rank]), lane);
+          asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(x) : "memory");
+        }
+      }
+      cluster_sync();
+      long long total = 0, before = 0;
+      for (int c = 0; c < C; ++c) {
+        if (c == rank) before = total;
+        total += s_cta[buf][c];
+      }
+      if (total == 0 && pass == 0) {  // nothing left of the difference: p alone
         src.q = nullptr;
         src.skip = -1;
-        __syncthreads();
         continue;
       }
-      if (rank == 0 && tid == 0) {
-        a.out_ids[row] = -1;
-        if (a.logp) a.logp[row] = 0.f;
-        a.n_emit[i] = first;
-        flag_error(a.dev_err, PAIR_DEV_ERR_PROBABILITY);
+      if (!control) break;
+      if (total == 0) {
+        if (rank == 0 && lane == 0) {
+          a.out_ids[d.row] = -1;
+          if (a.logp) a.logp[d.row] = 0.f;
+          a.n_emit[i] = d.row - d.lo;
+          flag_error(a.dev_err, PAIR_DEV_ERR_PROBABILITY);
+        }
+        break;
       }
-      return;
+      long long at = (long long)((double)a.u_draw[i] * (double)total);
+      at = max(min(at, total - 1), 0ll);
+      if (at < before || at >= before + s_cta[buf][rank]) break;
+      int w = 0;
+      while (at >= before + s_warp[buf][w]) before += s_warp[buf][w++];
+      const int v0 = min((rank * kVerifyWarps + w) * per, n_vec), v1 = min(v0 + per, n_vec);
+      const int tok = find(src, v0, v1, before, at);
+      if (tok >= 0) {
+        a.out_ids[d.row] = tok;
+        if (a.logp) a.logp[d.row] = logf(as_float(prow[tok]));
+        a.n_emit[i] = d.row - d.lo + 1;
+      }
+      break;
     }
-    long long at = (long long)((double)a.u_draw[i] * (double)total);
-    at = max(min(at, total - 1), 0ll);
-    for (int k = 0; k < warp; ++k) before += s_warp[k];
-    if (at < before || at >= before + s_warp[warp]) return;
-    // This warp's segment again, kAhead pieces of 32 vectors in flight.
-    constexpr int kAhead = 8;
-    for (int vb = v0; vb < v1; vb += 32 * kAhead) {
-      long long mine[kAhead], all[kAhead];
-#pragma unroll
-      for (int x = 0; x < kAhead; ++x) {
-        const int v = vb + x * 32 + lane;
-        mine[x] = v < v1 ? src.sum(v * VEC - mis) : 0;
-        all[x] = mine[x];
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int x = 0; x < kAhead; ++x) all[x] += __shfl_xor_sync(0xffffffffu, all[x], o);
-#pragma unroll
-      for (int x = 0; x < kAhead; ++x) {
-        if (at >= before + all[x]) {
-          before += all[x];
-          continue;
-        }
-        long long incl = mine[x];
-        for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-          if (lane >= o) incl += y;
-        }
-        long long c = before + incl - mine[x];
-        if (at >= c && at < c + mine[x]) {
-          const int e = (vb + x * 32 + lane) * VEC - mis;
-          float f[VEC];
-          src.load(e, f);
-          int tok = e;
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) {  // the first k whose sum passes `at`
-            c += fixed_weight(f[k]).value();
-            if (c <= at) tok = e + k + 1;
-          }
-          a.out_ids[row] = tok;
-          if (a.logp) a.logp[row] = logf(as_float(prow[tok]));
-          a.n_emit[i] = first + 1;
-        }
-        return;
-      }
-    }
-    return;
   }
+}
+
+// Clusters of C CTAs that fit on the device at once (cached per type and C).
+template <typename T>
+int resident_clusters(int C) {
+  static std::atomic<int> known[kVerifyMaxCluster + 1];
+  int n = known[C].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(C * 64, 1, 1);
+  cfg.blockDim = dim3(kVerifyThreads, 1, 1);
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = C;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaFuncSetAttribute(verify_kernel<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+          cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, verify_kernel<T>, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 0;
+  }
+  known[C].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 template <typename T>
 pair_status launch_verify(VerifyArgs<T> a, cudaStream_t s) {
-  // CTAs per request: a full cluster while the requests leave SMs idle.
-  int C = kVerifyMaxCluster;
-  while (C > 1 && (int64_t)a.R * C > 8 * 152) C /= 2;
+  // CTAs of a cluster: the time goes with rounds x (1 / C + the exchange's share
+  // of a row's reading), rounds = requests / clusters that fit. A large C leaves
+  // the fewest SMs without work in the last round, and brings a single
+  // request's row in from many SMs; short rows are not worth many CTAs.
+  int best = 0, clusters = 0;
+  double least = 0;
+  for (int C = 1; C <= kVerifyMaxCluster && (C == 1 || C * kVerifyLeast <= a.V); C *= 2) {
+    const int n = resident_clusters<T>(C);
+    if (n < 1) continue;
+    const double t = (double)ceil_div(a.R, n) * (1.0 / C + 3000.0 / a.V);
+    if (best == 0 || t < least) {
+      best = C;
+      least = t;
+      clusters = a.R < n ? a.R : n;
+    }
+  }
+  if (best == 0) return PAIR_ERR_CUDA;
+  a.C = best;
+  a.clusters = clusters;
   cudaLaunchConfig_t cfg = {};
-  a.C = C;
-  cfg.gridDim = dim3((unsigned)C * (unsigned)a.R, 1, 1);
+  cfg.gridDim = dim3((unsigned)best * (unsigned)clusters, 1, 1);
   cfg.blockDim = dim3(kVerifyThreads, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = C;
+  attr.val.clusterDim.x = best;
   attr.val.clusterDim.y = 1;
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
@@ -319,9 +426,9 @@ extern "C" pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (dt == PAIR_BF16)
     return launch_verify<__nv_bfloat16>(
-        {T, R, V, 1, static_cast<const __nv_bfloat16 *>(p), static_cast<const __nv_bfloat16 *>(q),
+        {T, R, V, 1, 1, static_cast<const __nv_bfloat16 *>(p), static_cast<const __nv_bfloat16 *>(q),
          p_row, q_row, ids, cu_new, u, u_draw, out_ids, logp, n_emit, dev_err}, s);
-  return launch_verify<float>({T, R, V, 1, static_cast<const float *>(p),
+  return launch_verify<float>({T, R, V, 1, 1, static_cast<const float *>(p),
                                static_cast<const float *>(q), p_row, q_row, ids, cu_new, u,
                                u_draw, out_ids, logp, n_emit, dev_err}, s);
 }
