@@ -283,9 +283,13 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
         const float *p = a.part + slots[k] * part_floats(M, D);
         const float f = exp2f(p[r] - ref);
         l = fmaf(p[M + r], f, l);
-        const float *src = p + 2 * M + r * D + lane * (D / 32);
+        const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * (D / 32));
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) o[c] = fmaf(src[c], f, o[c]);
+        for (int c = 0; c < D / 64; ++c) {
+          const float2 x = src[c];
+          o[2 * c] = fmaf(x.x, f, o[2 * c]);
+          o[2 * c + 1] = fmaf(x.y, f, o[2 * c + 1]);
+        }
       }
       const RowAt at = row_at(a, req.row0, d.rt * M, d.h, r);
       const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -305,7 +309,7 @@ pair_status run_simt(const Args &a, cudaStream_t s) {
   static_assert(smem <= 232448, "shared memory of a CTA");
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count());
+  const int ctas = useful_ctas(a, kSimtRows, (D <= 128 ? 2 : 1) * sm_count());
   PAIR_BEGIN("attend_simt", s);
   attend_simt_kernel<D><<<ctas, kSimtThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
@@ -315,7 +319,8 @@ pair_status run_simt(const Args &a, cudaStream_t s) {
 template <typename T, int D>
 pair_status run_join(const Args &a, int M, int ctas, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas, M / 16, 1);
+  const int64_t rows = a.T * a.g < M ? a.T * a.g : M;  // of a unit, at most
+  cfg.gridDim = dim3(ctas, (unsigned)ceil_div(rows, 16), 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr;
@@ -344,6 +349,15 @@ size_t desc_bytes() { return kMaxCtas * 2 * sizeof(Desc); }
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
 }  // namespace
+
+// CTAs (or pairs) of a launch: as many as fit at once, or as the work can be
+// worth at most: the host knows the table's width, not the lengths.
+int useful_ctas(const Args &a, int M, int fit) {
+  const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
+  const double keys = units * a.Hkv * (kUnitCost + (double)a.width * a.page + (double)M / a.g);
+  fit = fit < kMaxCtas ? fit : kMaxCtas;
+  return keys < (double)fit * kMinKeys ? 1 + (int)(keys / kMinKeys) : fit;
+}
 
 int sm_count() {
   int dev = 0, n = 0;

@@ -29,7 +29,11 @@ namespace attend {
 constexpr int kMaxCtas = 480;    // of one call, at most
 constexpr int kMaxRows = 256;    // rows of a unit, at most
 constexpr int kManyRows = 256;   // rows of a unit of the kernel for many rows
-constexpr int kFewRows = 64;     // rows of a unit of the kernel for few rows
+constexpr int kFewTile = 64;     // rows of a unit of the kernel for few rows
+// Chunks of up to so many rows go to the kernel for few rows, longer ones to the
+// tensor cores: 64 chunks behind 2000 keys of 8 heads take 120 us at 32 rows in
+// the former; at 48 161 there and 134 here.
+constexpr int kFewRows = 32;
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kUnitCost = 48;    // a unit's fixed cost, in keys
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
@@ -360,6 +364,7 @@ bool many_applies(const Args &a, int D);
 pair_status launch_many(const Args &a, int D, cudaStream_t s);
 pair_status launch_join(const Args &a, int D, int M, int ctas, pair_dtype dt, cudaStream_t s);
 int sm_count();
+int useful_ctas(const Args &a, int M, int fit);
 
 }  // namespace attend
 }  // namespace pairk

@@ -10,8 +10,7 @@ using namespace tc;
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int M = kFewRows;
-constexpr int BN = 64;  // keys of a tile
+constexpr int M = kFewTile;
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -40,7 +39,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 
 template <int D>
 struct Few {
-  static constexpr int kStages = D == 64 ? 4 : 2;
+  static constexpr int BN = D == 64 ? 128 : 64;     // keys of a tile
+  static constexpr int kStages = 2;
   static constexpr int kTile = BN * D * 2;          // bytes of a tile of keys or values
   static constexpr int kChunks = D / 8;             // 16-byte pieces of a row
   static constexpr int kRowsPerPass = kThreads / kChunks;
@@ -63,7 +63,7 @@ template <int D, int WR>
 __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uint8_t *smem,
                                             int cta, int seg) {
   using F = Few<D>;
-  constexpr int WK = kWarps / WR, KW = BN / WK, NT = KW / 8, NST = F::kStages;
+  constexpr int BN = F::BN, WK = kWarps / WR, KW = BN / WK, NT = KW / 8, NST = F::kStages;
   constexpr bool kQRegs = D <= 128;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int wr = warp % WR, wk = warp / WR;
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(
   clear_spare_rows<__nv_bfloat16, D, kThreads>(a, cta, ctas);
   if (cta == ctas - 1)
     report_requests(a);
-  Walk<M, BN> walk{find_share<kThreads>(a, M, cta, ctas, reinterpret_cast<int64_t *>(smem))};
+  Walk<M, Few<D>::BN> walk{find_share<kThreads>(a, M, cta, ctas, reinterpret_cast<int64_t *>(smem))};
   Segment s;
   for (int seg = 0; walk.next(a, &s); ++seg) {
     if (s.rows <= 16)
@@ -331,7 +331,7 @@ pair_status run_few(const Args &a, cudaStream_t s) {
   constexpr int smem = Few<D>::kBytes;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_few_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = min(kMaxCtas, (D <= 128 ? 3 : 1) * sm_count());
+  const int ctas = useful_ctas(a, M, (D <= 128 ? 3 : 1) * sm_count());
   PAIR_BEGIN("attend_few", s);
   attend_few_kernel<D><<<ctas, kThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);

@@ -10,7 +10,8 @@ namespace {
 using namespace tc;
 
 // CTA: warps 0-3 and 4-7 the softmax of one tile of 128 rows each (a row per
-// thread), warp 8 the TMA producer, warp 9 the MMA issuer. A row's 128 scores
+// thread), warps 8 and 10 the producers of keys and of values (TMA), warp 9 the
+// MMA issuer. A row's 128 scores
 // stay in registers: the third warpgroup gives up registers to the other two
 // (208 x 256 + 80 x 128 of the 168 x 384 that the block is launched with).
 constexpr int kThreads = 384;
@@ -44,6 +45,12 @@ struct Maps {
   int8_t k_at[3], v_at[3];  // dimension (1 to 3) of page, token, head
   int box;                  // tokens of a box
 };
+
+// A warp's arrival, for what its lanes have done (and fenced) before.
+__device__ __forceinline__ void warp_arrive(uint64_t *bar) {
+  __syncwarp();
+  if (elect_one()) mbar_arrive(bar);
+}
 
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc,
                                             uint32_t idesc, uint32_t accumulate) {
@@ -140,46 +147,62 @@ __device__ __forceinline__ bool edge_tile(const Segment &s, int t) {
   return (t + 1) * BN > s.least;
 }
 
-template <int D>
+// Keys (kv = 0) or values (1) of every tile, a box per lane. A warp each: the
+// 16 boxes of a tile of pages of 16 take some 1300 cycles to issue, and one warp
+// for both kept the products waiting. The page of the tile after the next one is
+// on its way meanwhile.
+template <int D, int kv>
 __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN> walk) {
   using C = Tc<D>;
   const int lane = threadIdx.x & 31;
   volatile int *abort = &sm.abort;
   Ring<C::kStages> ring;
+  ring.step(kv);
   int issued = 0;
-  const int box = maps.box, boxes = BN / box;
+  const int box = maps.box;
+  const bool mine = lane * box < BN;
+  const int8_t *where = kv ? maps.v_at : maps.k_at;
+  const CUtensorMap *map = kv ? &maps.v : &maps.k;
+  const int by = BN / a.page, by_off = BN % a.page;  // a tile's way in the table
   bool ok = true;
   Segment s;
   while (ok && walk.next(a, &s)) {
-    int off = 0, id = -1;
-    auto find = [&](int t) {
-      const int key = t * BN + lane * box;
-      id = t < s.t1 && lane < boxes && key < s.keys ? page_of(a, s.i, key, &off) : -1;
-    };
-    find(s.t0);
-    for (int t = s.t0; t < s.t1 && ok; ++t) {
-      const int cur = id, cur_off = off;
-      find(t + 1);
-      const unsigned some = __ballot_sync(0xffffffffu, cur >= 0);
-      const uint32_t bytes = __popc(some) * box * D * 2;
-      for (int kv = 0; kv < 2; ++kv) {
-        if (!(ok = wait(&sm.empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
-        uint64_t *bar = &sm.full[ring.stage];
-        if (lane == 0) mbar_expect_tx(bar, bytes);
-        __syncwarp();
-        if (cur >= 0) {
-          const int8_t *at = kv ? maps.v_at : maps.k_at;
-          const int c1 = at[0] == 1 ? cur : at[1] == 1 ? cur_off : s.h;
-          const int c2 = at[0] == 2 ? cur : at[1] == 2 ? cur_off : s.h;
-          const int c3 = at[0] == 3 ? cur : at[1] == 3 ? cur_off : s.h;
-#pragma unroll
-          for (int x = 0; x < C::kAtoms; ++x)
-            tma_load_4d(sm.kv[ring.stage] + x * C::kAtom + lane * box * 128,
-                        kv ? &maps.v : &maps.k, bar, x * 64, c1, c2, c3);
-        }
-        ++issued;
-        ring.step();
+    int key = s.t0 * BN + lane * box, at = key / a.page, off = key - at * a.page;
+    const int32_t *row = a.table + (int64_t)s.i * a.width;
+    const int end = min(s.keys, s.t1 * BN);
+    int id = mine && key < end ? row[at] : 0;
+    for (int t = s.t0; t < s.t1; ++t) {
+      const bool load = mine && key < end;
+      const int cur_off = off;
+      int cur = id;
+      key += BN;
+      at += by;
+      off += by_off;
+      if (off >= a.page) {
+        off -= a.page;
+        ++at;
       }
+      if (mine && key < end) id = row[at];
+      if (!(ok = wait(&sm.empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
+      uint64_t *bar = &sm.full[ring.stage];
+      const int n = __popc(__ballot_sync(0xffffffffu, load));
+      if (lane == 0) mbar_expect_tx(bar, n * box * D * 2);
+      __syncwarp();
+      if (load) {
+        if ((unsigned)cur >= (unsigned)a.num_pages) {
+          flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+          cur = 0;
+        }
+        const int c1 = where[0] == 1 ? cur : where[1] == 1 ? cur_off : s.h;
+        const int c2 = where[0] == 2 ? cur : where[1] == 2 ? cur_off : s.h;
+        const int c3 = where[0] == 3 ? cur : where[1] == 3 ? cur_off : s.h;
+        uint8_t *dst = sm.kv[ring.stage] + lane * box * 128;
+#pragma unroll
+        for (int x = 0; x < C::kAtoms; ++x)
+          tma_load_4d(dst + x * C::kAtom, map, bar, x * 64, c1, c2, c3);
+      }
+      ++issued;
+      ring.step(2);
     }
   }
   // Nothing may still be on its way into shared memory when the CTA ends: on
@@ -188,9 +211,19 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
   if (!ok) {
     volatile int never = 0;
     Ring<C::kStages> r;
-    for (int x = 0; x < issued; ++x, r.step())
-      if (x >= issued - C::kStages) wait_limit(&sm.full[r.stage], r.phase, &never, a.dev_err, 10000000);
+    r.step(kv);
+    for (int x = 0; x < issued; ++x, r.step(2))
+      if (2 * x >= 2 * issued - C::kStages) wait_limit(&sm.full[r.stage], r.phase, &never, a.dev_err, 10000000);
   }
+}
+
+// Waits, each lane of the first `n` for a barrier and phase of its own: one poll
+// of several costs a warp as much as one.
+__device__ __forceinline__ bool wait_lanes(int n, uint64_t *bar, uint32_t phase,
+                                           volatile int *abort, int32_t *dev_err) {
+  bool ok = true;
+  if ((int)(threadIdx.x & 31) < n) ok = wait(bar, phase, abort, dev_err);
+  return __all_sync(0xffffffffu, ok);
 }
 
 template <int D>
@@ -208,9 +241,9 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
     if (elect_one()) {
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        const uint32_t at = (kk >> 2) * (C::kAtom >> 4) + (kk & 3) * 2;
-        mma_bf16(tmem + w * 128, dq + w * (C::kTile >> 4) + at, dk + stage * (C::kTile >> 4) + at,
-                 C::kIdescS, kk != 0);
+        const uint32_t in = (kk & 3) * 2;
+        mma_bf16(tmem + w * 128, dq + (w * C::kTile + (kk >> 2) * C::kAtom) / 16 + in,
+                 dk + (stage * C::kTile + (kk >> 2) * C::kAtom) / 16 + in, C::kIdescS, kk != 0);
       }
       mma_commit(&sm.s_full[w]);
       if (last) mma_commit(&sm.empty[stage]);
@@ -224,7 +257,7 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
       for (int kk = 0; kk < BN / 32; ++kk) {
         const int at = half * (BN / 32) + kk;
         mma_bf16_ts(tmem + 256 + w * D, tmem + w * 128 + at * 8,
-                    dv + stage * (C::kTile >> 4) + at * 128, C::kIdescO, !first || at != 0);
+                    dv + stage * C::kTile / 16 + at * 128, C::kIdescO, !first || at != 0);
       }
       if (half) {
         mma_commit(&sm.pv_done[w]);
@@ -247,18 +280,29 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
     ring.step();
     for (int t = s.t0; t < s.t1 && ok; ++t) {
       const int v_stage = ring.stage;
-      const bool more = t + 1 < s.t1;
-      if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
-      if (edge_tile(s, t)) {
-        if (!(ok = wait(&sm.looked[v_stage], (looked_ph >> v_stage) & 1, abort, a.dev_err))) break;
-        looked_ph ^= 1u << v_stage;
-      }
+      const uint32_t v_phase = ring.phase;
+      const bool more = t + 1 < s.t1, edge = edge_tile(s, t);
       ring.step();
-      if (more && !(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+      // Before the first products of a tile: weights, values, the next keys, and
+      // the values looked over.
+      {
+        const int lane = threadIdx.x & 31;
+        const bool next = lane == 2 && more, look = lane == 3 && edge;
+        uint64_t *bar = lane == 0   ? &sm.p_ready[0][0]
+                        : next      ? &sm.full[ring.stage]
+                        : look      ? &sm.looked[v_stage]
+                                    : &sm.full[v_stage];
+        const uint32_t phase = lane == 0 ? p_ph[0]
+                               : next    ? ring.phase
+                               : look    ? (looked_ph >> v_stage) & 1
+                                         : v_phase;
+        if (!(ok = wait_lanes(4, bar, phase, abort, a.dev_err))) break;
+        if (edge) looked_ph ^= 1u << v_stage;
+      }
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (w > top) break;
-        if (!(ok = wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err))) break;
+        if (w && !(ok = wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err))) break;
         tc_fence_after();
         sums(w, v_stage, 0, t == s.t0, false);
         if (!(ok = wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err))) break;
@@ -281,13 +325,12 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
 // Values of an edge tile, by the threads of the active tiles: keys from `nk` on
 // become 0, what is not finite among those that some row does not see (from
 // `from` on) too (add_not_finite brings it back for the rows that see it).
-template <int D>
+template <int kAtoms>
 __device__ __forceinline__ void look_over(uint8_t *tile, int from, int nk, int threads,
                                           int *any_bad) {
-  using C = Tc<D>;
 #pragma unroll
-  for (int atom = 0; atom < C::kAtoms; ++atom) {
-    uint4 *base = reinterpret_cast<uint4 *>(tile + atom * C::kAtom);
+  for (int atom = 0; atom < kAtoms; ++atom) {
+    uint4 *base = reinterpret_cast<uint4 *>(tile + atom * 128 * 128);
 #pragma unroll 4
     for (int x = from * 8 + threadIdx.x; x < 1024; x += threads) {
       if ((x >> 3) >= nk) {
@@ -346,7 +389,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
                                  (((c & 7) ^ (row & 7)) << 4)) = u[c];
     }
     fence_async_smem();
-    mbar_arrive(&sm.q_full[w]);
+    warp_arrive(&sm.q_full[w]);
   };
   Segment s, ahead;
   bool more = walk.next(a, &ahead);
@@ -360,21 +403,26 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
     } else if (s.t0 < s.t1) {
       const int seen = min(s.seen(mine ? r : 0, a.g), s.kv);
       for (int t = s.t0; t < s.t1; ++t) {
-        ring.step();  // the values' place
+        ring.step();
+        const int v_stage = ring.stage;
+        const uint32_t v_phase = ring.phase;
+        ring.step();
         const bool edge = edge_tile(s, t);
         const int key0 = t * BN;
-        if (edge) {
-          if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
-          look_over<D>(sm.kv[ring.stage], max(0, s.least - key0), min(BN, s.keys - key0),
-                       s.rows > 128 ? 256 : 128, &sm.any_bad);
-          fence_async_smem();
-          mbar_arrive(&sm.looked[ring.stage]);
-          if (s.rows <= 128) mbar_arrive(&sm.looked[ring.stage]);  // for the other tile's threads
-        }
-        ring.step();
         if (!(ok = wait(&sm.s_full[w], s_ph, abort, a.dev_err))) break;
         s_ph ^= 1;
         tc_fence_after();
+        if (edge) {
+          // Behind the wait for the scores, which go in step with this tile: a
+          // tile that sat out some segments could be whole rounds of the ring
+          // ahead, where a barrier's phase means another round.
+          if (!(ok = wait(&sm.full[v_stage], v_phase, abort, a.dev_err))) break;
+          look_over<C::kAtoms>(sm.kv[v_stage], max(0, s.least - key0), min(BN, s.keys - key0),
+                               s.rows > 128 ? 256 : 128, &sm.any_bad);
+          fence_async_smem();
+          warp_arrive(&sm.looked[v_stage]);
+          if (s.rows <= 128) warp_arrive(&sm.looked[v_stage]);  // for the other tile's warps
+        }
         uint32_t x[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + c * 32, x[c]);
@@ -442,7 +490,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
           tmem_st32(tS + c * 16, p);
           tmem_st_wait();
           tc_fence_before();
-          mbar_arrive(&sm.p_ready[w][c >> 1]);
+          warp_arrive(&sm.p_ready[w][c >> 1]);
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
@@ -531,14 +579,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int x = 0; x < Tc<D>::kStages; ++x) {
       mbar_init(&sm.full[x], 1);
       mbar_init(&sm.empty[x], 1);
-      mbar_init(&sm.looked[x], 256);
+      mbar_init(&sm.looked[x], 8);
     }
     mbar_init(&sm.done, 1);
     for (int w = 0; w < 2; ++w) {
-      mbar_init(&sm.q_full[w], 128);
+      mbar_init(&sm.q_full[w], 4);
       mbar_init(&sm.s_full[w], 1);
-      mbar_init(&sm.p_ready[w][0], 128);
-      mbar_init(&sm.p_ready[w][1], 128);
+      mbar_init(&sm.p_ready[w][0], 4);
+      mbar_init(&sm.p_ready[w][1], 4);
       mbar_init(&sm.pv_done[w], 1);
     }
     sm.abort = 0;
@@ -555,7 +603,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 8)
-      produce<D>(a, maps, sm, walk);
+      produce<D, 0>(a, maps, sm, walk);
+    else if (warp == 10)
+      produce<D, 1>(a, maps, sm, walk);
     else if (warp == 9)
       issue<D>(a, sm, walk);
   } else {
@@ -610,7 +660,7 @@ pair_status run_many(const Args &a, const Maps &maps, cudaStream_t s) {
   static_assert(smem <= 232448, "shared memory of a CTA");
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_many_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = min(kMaxCtas, sm_count());
+  const int ctas = useful_ctas(a, M, sm_count());
   PAIR_BEGIN("attend_many", s);
   attend_many_kernel<D><<<ctas, kThreads, smem, s>>>(a, maps);
   PAIR_LAUNCH_CHECK(s);
@@ -620,7 +670,7 @@ pair_status run_many(const Args &a, const Maps &maps, cudaStream_t s) {
 bool many_maps(const Args &a, int D, Maps *maps) {
   // A box is the largest power of two of tokens, up to a tile, that divides
   // the page; the swizzle's period is 8 rows.
-  int box = 128;
+  int box = BN;
   while (a.page % box != 0) box /= 2;
   if (D > 128 || box < 8) return false;
   maps->box = box;

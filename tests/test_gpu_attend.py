@@ -130,6 +130,17 @@ def test_attend_many_requests():
     check(build(reqs, 2, 1, 64, 16, torch.bfloat16, seed=3))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_many_short_chunks(D):
+    """Hundreds of short chunks, some of one tile of rows, some of more, so that
+    a CTA works off many units of few key tiles one after the other."""
+    rng = np.random.default_rng(D)
+    reqs = [(int(n), int(n + rng.integers(0, 200))) for n in rng.integers(0, 130, 400)]
+    check(build(reqs, 4, 2, D, 32, torch.bfloat16, seed=D))
+    reqs = [(int(n), int(n + rng.integers(0, 140))) for n in rng.integers(130, 270, 60)]
+    check(build(reqs, 10, 2, D, 8, torch.bfloat16, layout="head", seed=D + 1))
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("n", [6, 150])
