@@ -452,33 +452,68 @@ def pair_grad_noalloc(H, W, y, mask, cu_seqlens, a, dH=None, dW=None,
     return Jobj, dH, dW, logp_seq
 
 
-def _strided(t, name, dtype, shape, like):
-    """A CUDA tensor on like's device whose last dimension is contiguous (rows
-    of a wider array are fine); the library checks alignment."""
+# The rollout step's calls are made once per generated chunk and a small one is
+# over in a few microseconds on the GPU, so each tensor is checked by one
+# expression; what fails it goes through the checks that say why.
+def _index(t, name):
+    """Index of the device that a call's leading tensor is on."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % name)
-    if t.dtype is not dtype:
-        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.shape != shape:
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t.get_device()
+
+
+def _same_device(like, name, t):
     if t.device != like.device:
         raise ValueError("%s must be on %s, got %s" % (name, like.device, t.device))
-    if t.stride(-1) != 1 and t.shape[-1] != 1:
-        raise ValueError("%s must be contiguous in its last dimension" % name)
 
 
-def _same_device(like, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != like.device:
-            raise ValueError("%s must be on %s, got %s" % (name, like.device, t.device))
+def _ptr(t, name, dtype, shape, like, at):
+    """Pointer of a contiguous tensor on like's device, whose index is `at`."""
+    if not (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
+            and t.is_contiguous() and t.get_device() == at):
+        _need(t, name, dtype, shape)
+        _same_device(like, name, t)
+    return t.data_ptr()
 
 
-def _cache(k_cache, v_cache, dtype, like):
+def _out_ptr(t, name, dtype, shape, like, at):
+    """Output tensor (allocated where it is None) and its pointer."""
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+        return t, t.data_ptr()
+    return t, _ptr(t, name, dtype, shape, like, at)
+
+
+def _err_ptr(dev_err, like, at):
+    return None if dev_err is None else _ptr(dev_err, "dev_err", torch.int32, (1,), like, at)
+
+
+def _strided(t, name, dtype, shape, like, at):
+    """Pointer of a tensor on like's device whose last dimension is contiguous
+    (rows of a wider array are fine); the library checks alignment."""
+    if not (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
+            and t.get_device() == at and t.stride(-1) == 1):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError("%s must be a CUDA tensor" % name)
+        if t.dtype is not dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape),
+                                                                tuple(t.shape)))
+        _same_device(like, name, t)
+        if t.stride(-1) != 1 and t.shape[-1] != 1:
+            raise ValueError("%s must be contiguous in its last dimension" % name)
+    return t.data_ptr()
+
+
+def _cache(k_cache, v_cache, like, at):
+    """Pointers and strides of both caches, their shape."""
     if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
         raise ValueError("k_cache must be [num_pages, page_size, Hkv, D]")
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        _strided(t, name, dtype, k_cache.shape, like)
-    return (CacheStrides(*k_cache.stride()[:3]), CacheStrides(*v_cache.stride()[:3]))
+    shape, dtype = k_cache.shape, like.dtype
+    k, v = (_strided(k_cache, "k_cache", dtype, shape, like, at),
+            _strided(v_cache, "v_cache", dtype, shape, like, at))
+    return (k, CacheStrides(*k_cache.stride()[:3]), v, CacheStrides(*v_cache.stride()[:3]), shape)
 
 
 def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, page_size, T,
@@ -489,23 +524,20 @@ def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, pa
     block_table gets the new pages in place. Returns (kv_len [R], held_out
     [R], cu_new [R+1], slots [T] int64, taken [1])."""
     R, width = block_table.shape
-    dev, i32 = lens.device, torch.int32
-    _need(lens, "lens", i32, (R,))
-    _need(held, "held", i32, (R,))
-    _need(n_new, "n_new", i32, (R,))
-    _need(free_pages, "free_pages", i32)
-    _need(free_count, "free_count", i32, (1,))
-    _need(block_table, "block_table", i32)
-    _same_device(lens, held=held, n_new=n_new, free_pages=free_pages, free_count=free_count,
-                 block_table=block_table, dev_err=dev_err)
-    kv_len = _out(kv_len, "kv_len", (R,), i32, dev)
-    held_out = _out(held_out, "held_out", (R,), i32, dev)
-    cu_new = _out(cu_new, "cu_new", (R + 1,), i32, dev)
-    slots = _out(slots, "slots", (int(T),), torch.int64, dev)
-    taken = _out(taken, "taken", (1,), i32, dev)
-    _call("pair_pages_extend", lens, stream, R, int(page_size), width, _p(lens), _p(held),
-          _p(n_new), _p(free_pages), free_pages.numel(), _p(free_count), int(T), _p(block_table),
-          _p(kv_len), _p(held_out), _p(cu_new), _p(slots), _p(taken), _p(dev_err))
+    i32, T, at, per = torch.int32, int(T), _index(lens, "lens"), (R,)
+    F = free_pages.numel()
+    ins = (_ptr(lens, "lens", i32, per, lens, at), _ptr(held, "held", i32, per, lens, at),
+           _ptr(n_new, "n_new", i32, per, lens, at),
+           _ptr(free_pages, "free_pages", i32, (F,), lens, at))
+    count = _ptr(free_count, "free_count", i32, (1,), lens, at)
+    table = _ptr(block_table, "block_table", i32, (R, width), lens, at)
+    kv_len, kv_p = _out_ptr(kv_len, "kv_len", i32, per, lens, at)
+    held_out, held_p = _out_ptr(held_out, "held_out", i32, per, lens, at)
+    cu_new, cu_p = _out_ptr(cu_new, "cu_new", i32, (R + 1,), lens, at)
+    slots, slots_p = _out_ptr(slots, "slots", torch.int64, (T,), lens, at)
+    taken, taken_p = _out_ptr(taken, "taken", i32, (1,), lens, at)
+    _call("pair_pages_extend", lens, stream, R, int(page_size), width, *ins, F, count, T, table,
+          kv_p, held_p, cu_p, slots_p, taken_p, _err_ptr(dev_err, lens, at))
     return kv_len, held_out, cu_new, slots, taken
 
 
@@ -514,18 +546,16 @@ def pair_cache_append(k, v, slots, k_cache, v_cache, dev_err=None, stream=None):
     out) of the caches [num_pages, page_size, Hkv, D] (see pair.h). k, v and
     the caches may be views with other strides. Returns (k_cache, v_cache)."""
     T, H, D = k.shape
-    dt = _pair_dtype(k, "k")
-    for t, name in ((k, "k"), (v, "v")):
-        _strided(t, name, k.dtype, (T, H, D), k)
-    _need(slots, "slots", torch.int64, (T,))
-    _same_device(k, slots=slots, dev_err=dev_err)
-    ks, vs = _cache(k_cache, v_cache, k.dtype, k)
-    if k_cache.shape[2:] != (H, D):
-        raise ValueError("k_cache must have %d heads of %d, got %s" % (H, D,
-                                                                       tuple(k_cache.shape)))
-    _call("pair_cache_append", k, stream, T, H, D, dt, _p(k), k.stride(0), k.stride(1), _p(v),
-          v.stride(0), v.stride(1), _p(slots), k_cache.shape[0], k_cache.shape[1], _p(k_cache),
-          ks, _p(v_cache), vs, _p(dev_err))
+    dt, at = _pair_dtype(k, "k"), _index(k, "k")
+    kp, vp = (_strided(k, "k", k.dtype, (T, H, D), k, at),
+              _strided(v, "v", k.dtype, (T, H, D), k, at))
+    slots_p = _ptr(slots, "slots", torch.int64, (T,), k, at)
+    kc, ks, vc, vs, shape = _cache(k_cache, v_cache, k, at)
+    if shape[2] != H or shape[3] != D:
+        raise ValueError("k_cache must have %d heads of %d, got %s" % (H, D, tuple(shape)))
+    _call("pair_cache_append", k, stream, T, H, D, dt, kp, k.stride(0), k.stride(1), vp,
+          v.stride(0), v.stride(1), slots_p, shape[0], shape[1], kc, ks, vc, vs,
+          _err_ptr(dev_err, k, at))
     return k_cache, v_cache
 
 
@@ -539,32 +569,27 @@ def pair_attend_paged(q, k_cache, v_cache, block_table, kv_len, cu_new, scale=No
     (see pair.h). q [T, Hq, D], caches [num_pages, page_size, Hkv, D] (views
     with other strides too), block_table [R, width], kv_len [R], cu_new [R+1]
     int32; scale is D ** -0.5 by default; max_new is the longest chunk if the
-    host knows it. Returns (out [T, Hq, D], lse [T, Hq]
-    float32)."""
+    host knows it. Returns (out [T, Hq, D], lse [T, Hq] float32)."""
     T, Hq, D = q.shape
-    dt = _pair_dtype(q, "q")
-    _strided(q, "q", q.dtype, (T, Hq, D), q)
-    ks, vs = _cache(k_cache, v_cache, q.dtype, q)
-    Hkv = k_cache.shape[2]
-    if k_cache.shape[3] != D:
-        raise ValueError("k_cache must have heads of %d, got %s" % (D, tuple(k_cache.shape)))
+    dt, at, i32 = _pair_dtype(q, "q"), _index(q, "q"), torch.int32
+    qp = _strided(q, "q", q.dtype, (T, Hq, D), q, at)
+    kc, ks, vc, vs, shape = _cache(k_cache, v_cache, q, at)
+    if shape[3] != D:
+        raise ValueError("k_cache must have heads of %d, got %s" % (D, tuple(shape)))
     R, width = block_table.shape
-    _need(block_table, "block_table", torch.int32)
-    _need(kv_len, "kv_len", torch.int32, (R,))
-    _need(cu_new, "cu_new", torch.int32, (R + 1,))
-    _same_device(q, block_table=block_table, kv_len=kv_len, cu_new=cu_new, ws=ws,
-                 dev_err=dev_err)
-    dev = q.device
-    out = _out(out, "out", (T, Hq, D), q.dtype, dev)
-    lse = _out(lse, "lse", (T, Hq), torch.float32, dev)
+    table = _ptr(block_table, "block_table", i32, (R, width), q, at)
+    lens = _ptr(kv_len, "kv_len", i32, (R,), q, at)
+    cu = _ptr(cu_new, "cu_new", i32, (R + 1,), q, at)
+    out, out_p = _out_ptr(out, "out", q.dtype, (T, Hq, D), q, at)
+    lse, lse_p = _out_ptr(lse, "lse", torch.float32, (T, Hq), q, at)
     if ws is None:
-        need = pair_attend_workspace_size(R, Hq, Hkv, D, dt)
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-    _need(ws, "ws", torch.uint8)
-    _call("pair_attend_paged", q, stream, T, R, Hq, Hkv, D, dt, _p(q), q.stride(0), q.stride(1),
-          _p(k_cache), ks, _p(v_cache), vs, k_cache.shape[0], k_cache.shape[1], _p(block_table),
-          width, _p(kv_len), _p(cu_new), float(D ** -0.5 if scale is None else scale),
-          int(max_new), _p(out), _p(lse), _p(ws), ws.numel(), _p(dev_err))
+        need = pair_attend_workspace_size(R, Hq, shape[2], D, dt)
+        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    n = ws.numel()
+    _call("pair_attend_paged", q, stream, T, R, Hq, shape[2], D, dt, qp, q.stride(0), q.stride(1),
+          kc, ks, vc, vs, shape[0], shape[1], table, width, lens, cu,
+          D ** -0.5 if scale is None else float(scale), int(max_new), out_p, lse_p,
+          _ptr(ws, "ws", torch.uint8, (n,), q, at), n, _err_ptr(dev_err, q, at))
     return out, lse
 
 
@@ -576,23 +601,18 @@ def pair_verify_drafts(p, ids, cu_new, u, u_draw, q=None, out_ids=None, logp=Non
     were looked up. Returns (out_ids [T] int32, logp [T] float32, n_emit [R]
     int32)."""
     T, V = p.shape
-    dt = _pair_dtype(p, "p")
-    _strided(p, "p", p.dtype, (T, V), p)
-    if q is not None:
-        _strided(q, "q", p.dtype, (T, V), p)
+    dt, at, i32, f32 = _pair_dtype(p, "p"), _index(p, "p"), torch.int32, torch.float32
+    pp = _strided(p, "p", p.dtype, (T, V), p, at)
+    qp, q_row = (None, 0) if q is None else (_strided(q, "q", p.dtype, (T, V), p, at), q.stride(0))
     R = cu_new.numel() - 1
-    _need(ids, "ids", torch.int32, (T,))
-    _need(cu_new, "cu_new", torch.int32, (R + 1,))
-    _need(u, "u", torch.float32, (T,))
-    _need(u_draw, "u_draw", torch.float32, (R,))
-    _same_device(p, ids=ids, cu_new=cu_new, u=u, u_draw=u_draw, dev_err=dev_err)
-    dev = p.device
-    out_ids = _out(out_ids, "out_ids", (T,), torch.int32, dev)
-    logp = _out(logp, "logp", (T,), torch.float32, dev)
-    n_emit = _out(n_emit, "n_emit", (R,), torch.int32, dev)
-    _call("pair_verify_drafts", p, stream, T, R, V, dt, _p(p), p.stride(0), _p(q),
-          0 if q is None else q.stride(0), _p(ids), _p(cu_new), _p(u), _p(u_draw), _p(out_ids),
-          _p(logp), _p(n_emit), _p(dev_err))
+    ids_p = _ptr(ids, "ids", i32, (T,), p, at)
+    cu = _ptr(cu_new, "cu_new", i32, (R + 1,), p, at)
+    up, dp = _ptr(u, "u", f32, (T,), p, at), _ptr(u_draw, "u_draw", f32, (R,), p, at)
+    out_ids, out_p = _out_ptr(out_ids, "out_ids", i32, (T,), p, at)
+    logp, logp_p = _out_ptr(logp, "logp", f32, (T,), p, at)
+    n_emit, n_p = _out_ptr(n_emit, "n_emit", i32, (R,), p, at)
+    _call("pair_verify_drafts", p, stream, T, R, V, dt, pp, p.stride(0), qp, q_row, ids_p, cu, up,
+          dp, out_p, logp_p, n_p, _err_ptr(dev_err, p, at))
     return out_ids, logp, n_emit
 
 

@@ -74,26 +74,25 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
   const __nv_bfloat16 *kc = static_cast<const __nv_bfloat16 *>(a.kc);
   const __nv_bfloat16 *vc = static_cast<const __nv_bfloat16 *>(a.vc);
 
-  __syncthreads();
-  if (tid == 0) *any_bad = 0;
-  for (int x = tid; x < 16 * WR * F::kChunks; x += kThreads) {
-    const int r = x / F::kChunks, c = x % F::kChunks;
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (r < s.rows) {
-      const RowAt at = row_at(a, s.row0, s.r0, s.h, r);
-      u = *reinterpret_cast<const uint4 *>(q + at.token * a.q_row + at.head * a.q_head + c * 8);
-    }
-    *reinterpret_cast<uint4 *>(smem + F::kQ + r * D * 2 + ((c ^ (r & 7)) << 4)) = u;
-  }
-  // Offsets of a tile's rows: thread k < BN has key k's.
+  // The page of a tile's key tid (off < 0: no such key). What the cache's owner
+  // wrote is looked at when it is used, so the reads overlap.
   auto find_page = [&](int t, int *off) {
     const int key = t * BN + tid;
-    return t < s.t1 && tid < BN && key < s.keys ? page_of(a, s.i, key, off) : -1;
+    *off = -1;
+    if (t >= s.t1 || tid >= BN || key >= s.keys) return 0;
+    const int at = key / a.page;
+    *off = key - at * a.page;
+    return a.table[(int64_t)s.i * a.width + at];
   };
+  // Offsets of a tile's rows: thread k < BN has key k's.
   auto put_offsets = [&](int buf, int id, int off) {
     if (tid < BN) {
-      offs[(buf * 2) * BN + tid] = id < 0 ? -1 : cache_row(a, a.ks, id, off, s.h);
-      offs[(buf * 2 + 1) * BN + tid] = id < 0 ? -1 : cache_row(a, a.vs, id, off, s.h);
+      if (off >= 0 && (unsigned)id >= (unsigned)a.num_pages) {
+        flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+        id = 0;
+      }
+      offs[(buf * 2) * BN + tid] = off < 0 ? -1 : cache_row(a, a.ks, id, off, s.h);
+      offs[(buf * 2 + 1) * BN + tid] = off < 0 ? -1 : cache_row(a, a.vs, id, off, s.h);
     }
   };
   auto load_tile = [&](int t, int stage, int buf) {
@@ -111,13 +110,30 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
     }
     cp_async_commit();
   };
+  int id[NST], off[NST];
 #pragma unroll
-  for (int x = 0; x < NST - 1; ++x) {
-    int off = 0;
-    const int id = find_page(s.t0 + x, &off);
-    put_offsets(x, id, off);
+  for (int x = 0; x < NST; ++x) id[x] = find_page(s.t0 + x, &off[x]);
+  constexpr int kQPieces = 16 * WR * F::kChunks / kThreads;
+  uint4 qv[kQPieces];
+#pragma unroll
+  for (int y = 0; y < kQPieces; ++y) {
+    const int x = tid + y * kThreads, r = x / F::kChunks, c = x % F::kChunks;
+    qv[y] = make_uint4(0, 0, 0, 0);
+    if (r < s.rows) {
+      const RowAt at = row_at(a, s.row0, s.r0, s.h, r);
+      qv[y] = *reinterpret_cast<const uint4 *>(q + at.token * a.q_row + at.head * a.q_head + c * 8);
+    }
   }
-  int next_off = 0, next_id = find_page(s.t0 + NST - 1, &next_off);
+  __syncthreads();  // the segment before is through
+  if (tid == 0) *any_bad = 0;
+#pragma unroll
+  for (int x = 0; x < NST - 1; ++x) put_offsets(x, id[x], off[x]);
+  int next_id = id[NST - 1], next_off = off[NST - 1];
+#pragma unroll
+  for (int y = 0; y < kQPieces; ++y) {
+    const int x = tid + y * kThreads, r = x / F::kChunks, c = x % F::kChunks;
+    *reinterpret_cast<uint4 *>(smem + F::kQ + r * D * 2 + ((c ^ (r & 7)) << 4)) = qv[y];
+  }
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < NST - 1; ++x) load_tile(s.t0 + x, x, x);
