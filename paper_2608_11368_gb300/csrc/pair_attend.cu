@@ -32,7 +32,7 @@ struct SimtSmem {
 // that arrive two tiles ahead (asynchronous copies into shared memory). A
 // thread forms the scores of one key with its group's rows (the queries are
 // broadcast reads), then the output sums of its columns for 16 rows (8 at D =
-// 64), four keys at a time. Bound by latency at small sizes (four barriers and
+// 64), four keys at a time; rows that are not in use are left out. Bound by latency at small sizes (four barriers and
 // two exchanges per tile), else by shared-memory reads.
 template <int D>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   S &sm = *reinterpret_cast<S *>(raw);
   constexpr int M = kSimtRows, BN = S::kKeys, NST = S::kStages, V4 = D / 4;
   constexpr int QR = M * BN / kSimtThreads;                      // rows of a thread's scores
+  constexpr int QG = M / QR;                                     // groups of them
   constexpr int CPT = D >= kSimtThreads ? D / kSimtThreads : 1;  // columns per thread
   constexpr int RG = D >= kSimtThreads ? 1 : kSimtThreads / D;   // row groups
   constexpr int RPT = M / RG;
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
     int seen[RPT];
 #pragma unroll
     for (int r = 0; r < RPT; ++r) {
-      seen[r] = sm.seen[rg * RPT + r];
+      seen[r] = sm.seen[r * RG + rg];
 #pragma unroll
       for (int c = 0; c < CPT; ++c) o[r][c] = 0.f;
     }
@@ -114,20 +115,21 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       __syncthreads();  // tile t is there, tile t - 1's stage free
       put_offsets(t + 2);
       {
-        const int k = tid % BN, r0 = tid / BN * QR;
+        const int k = tid % BN, g0 = tid / BN;  // rows g0, g0 + QG, ..
         float acc[QR] = {};
 #pragma unroll 4
         for (int d = 0; d < D; d += 4) {
           const float4 x = *reinterpret_cast<const float4 *>(&sm.k[st][k][d]);
 #pragma unroll
           for (int r = 0; r < QR; ++r) {
-            const float4 y = *reinterpret_cast<const float4 *>(&sm.q[r0 + r][d]);
+            if (r * QG >= s.rows) break;
+            const float4 y = *reinterpret_cast<const float4 *>(&sm.q[r * QG + g0][d]);
             acc[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc[r]))));
           }
         }
 #pragma unroll
         for (int r = 0; r < QR; ++r)
-          sm.p[r0 + r][k] = key0 + k < sm.seen[r0 + r] ? acc[r] * scale : -INFINITY;
+          sm.p[r * QG + g0][k] = key0 + k < sm.seen[r * QG + g0] ? acc[r] * scale : -INFINITY;
       }
       __syncthreads();
       fetch(t + 2);
@@ -177,7 +179,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
 #pragma unroll
       for (int r = 0; r < RPT; ++r)
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) o[r][c] *= sm.fix[rg * RPT + r];
+        for (int c = 0; c < CPT; ++c) o[r][c] *= sm.fix[r * RG + rg];
       // A value that a row does not see must not reach its sums, not even
       // times zero: it may be NaN. Behind the last key the values are zeros.
       const bool edge = key0 + BN > s.least;
@@ -190,7 +192,8 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
           for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[st][k + y][col + c * kSimtThreads];
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
-          const float4 p4 = *reinterpret_cast<const float4 *>(&sm.p[rg * RPT + r][k]);
+          if (r * RG >= s.rows) break;
+          const float4 p4 = *reinterpret_cast<const float4 *>(&sm.p[r * RG + rg][k]);
           const float p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
           for (int y = 0; y < 4; ++y)
@@ -207,7 +210,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
     if (s.whole()) {
 #pragma unroll
       for (int r = 0; r < RPT; ++r) {
-        const int rr = rg * RPT + r;
+        const int rr = r * RG + rg;
         if (rr >= s.rows) continue;
         const RowAt at = row_at(a, s.row0, s.r0, s.h, rr);
         const float l = sm.l[rr], inv = l == 0.f ? 0.f : 1.f / l;
@@ -228,7 +231,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       for (int r = 0; r < RPT; ++r)
 #pragma unroll
         for (int c = 0; c < CPT; ++c)
-          part[2 * M + (rg * RPT + r) * D + col + c * kSimtThreads] = o[r][c];
+          part[2 * M + (r * RG + rg) * D + col + c * kSimtThreads] = o[r][c];
     }
   }
   let_next_start();
@@ -243,63 +246,58 @@ template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M, int ctas) {
   __shared__ int slots[kMaxCtas];
   __shared__ int n_slots;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_previous();
-  for (int which = 0; which < 2; ++which) {
-    const int mine = blockIdx.x * 2 + which;
-    const Desc d = a.desc[mine];
-    if (d.tiles == 0 || d.t0 != 0) continue;
-    __syncthreads();
-    if (warp == 0) {
-      int n = 1;
-      if (lane == 0) slots[0] = mine;
-      bool more = true;
-      for (int c0 = blockIdx.x + 1; more && c0 < ctas; c0 += 32) {
-        const int c = c0 + lane;
-        Desc e{};
-        if (c < ctas) e = a.desc[c * 2];
-        const bool in = e.tiles > 0 && e.i == d.i && e.h == d.h && e.rt == d.rt;
-        const unsigned ins = __ballot_sync(0xffffffffu, in);
-        if (in) slots[n + __popc(ins & ((1u << lane) - 1))] = c * 2;
-        n += __popc(ins);
-        more = !__any_sync(0xffffffffu, in && e.t1 == e.tiles);
-      }
-      if (lane == 0) n_slots = n;
+  const int mine = blockIdx.x * 2 + blockIdx.z;
+  const Desc d = a.desc[mine];
+  if (d.tiles == 0 || d.t0 != 0) return;
+  const Request req = request(a, d.i);
+  if (warp == 0) {
+    int n = 1;
+    if (lane == 0) slots[0] = mine;
+    bool more = true;
+    for (int c0 = blockIdx.x + 1; more && c0 < ctas; c0 += 32) {
+      const int c = c0 + lane;
+      Desc e{};
+      if (c < ctas) e = a.desc[c * 2];
+      const bool in = e.tiles > 0 && e.i == d.i && e.h == d.h && e.rt == d.rt;
+      const unsigned ins = __ballot_sync(0xffffffffu, in);
+      if (in) slots[n + __popc(ins & ((1u << lane) - 1))] = c * 2;
+      n += __popc(ins);
+      more = !__any_sync(0xffffffffu, in && e.t1 == e.tiles);
     }
-    __syncthreads();
-    const int n = n_slots;
-    const Request req = request(a, d.i);
-    const int rows = min(M, req.n * a.g - d.rt * M);
-    for (int r = blockIdx.y * (kJoinThreads / 32) + warp; r < rows;
-         r += gridDim.y * (kJoinThreads / 32)) {
-      float mx = -INFINITY;
-      for (int k = lane; k < n; k += 32)
-        mx = fmaxf(mx, a.part[slots[k] * part_floats(M, D) + r]);
-      for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      float l = 0.f, o[D / 32] = {};
+    if (lane == 0) n_slots = n;
+  }
+  __syncthreads();
+  const int n = n_slots;
+  const int rows = min(M, req.n * a.g - d.rt * M);
+  for (int r = blockIdx.y * (kJoinThreads / 32) + warp; r < rows;
+       r += gridDim.y * (kJoinThreads / 32)) {
+    float mx = -INFINITY;
+    for (int k = lane; k < n; k += 32) mx = fmaxf(mx, a.part[slots[k] * part_floats(M, D) + r]);
+    for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float l = 0.f, o[D / 32] = {};
 #pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const float *p = a.part + slots[k] * part_floats(M, D);
-        const float f = exp2f(p[r] - ref);
-        l = fmaf(p[M + r], f, l);
-        const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * (D / 32));
+    for (int k = 0; k < n; ++k) {
+      const float *p = a.part + slots[k] * part_floats(M, D);
+      const float f = exp2f(p[r] - ref);
+      l = fmaf(p[M + r], f, l);
+      const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * (D / 32));
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          const float2 x = src[c];
-          o[2 * c] = fmaf(x.x, f, o[2 * c]);
-          o[2 * c + 1] = fmaf(x.y, f, o[2 * c + 1]);
-        }
+      for (int c = 0; c < D / 64; ++c) {
+        const float2 x = src[c];
+        o[2 * c] = fmaf(x.x, f, o[2 * c]);
+        o[2 * c + 1] = fmaf(x.y, f, o[2 * c + 1]);
       }
-      const RowAt at = row_at(a, req.row0, d.rt * M, d.h, r);
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D + lane * (D / 32);
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) from_float(out + c, o[c] * inv);
-      if (lane == 0 && a.lse)
-        a.lse[at.token * a.Hq + at.head] =
-            l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
     }
+    const RowAt at = row_at(a, req.row0, d.rt * M, d.h, r);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D + lane * (D / 32);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) from_float(out + c, o[c] * inv);
+    if (lane == 0 && a.lse)
+      a.lse[at.token * a.Hq + at.head] = l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
   }
 }
 
@@ -320,7 +318,7 @@ template <typename T, int D>
 pair_status run_join(const Args &a, int M, int ctas, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   const int64_t rows = a.T * a.g < M ? a.T * a.g : M;  // of a unit, at most
-  cfg.gridDim = dim3(ctas, (unsigned)ceil_div(rows, 16), 1);
+  cfg.gridDim = dim3(ctas, (unsigned)ceil_div(rows, 16), 2);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr;
