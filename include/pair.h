@@ -609,6 +609,8 @@ PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_d
  *      [0, num_pages) or a kv_len that is negative or beyond the table row
  *      (that request's rows are unspecified), or offsets cu_new that decrease
  *      or pass T (all rows are). Nothing outside the arrays is read or written.
+ *      PAIR_DEV_ERR_TIMEOUT as for pair_grad.
+ * No output, nor ws, may overlap an input.
  * Deterministic for the same arguments on the same device.
  */
 PAIR_API size_t pair_attend_workspace_size(int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
@@ -653,7 +655,7 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  *      PAIR_DEV_ERR_PROBABILITY: all weights of p are 0 (the token is -1 and
  *      not counted); PAIR_DEV_ERR_PAGES: offsets that decrease or pass T (the
  *      request is left out).
- * Deterministic. One launch, no workspace.
+ * No output may overlap an input. Deterministic. One launch, no workspace.
  */
 PAIR_API pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_dtype dt,
                                         const void *p, int64_t p_row, const void *q,

@@ -8,7 +8,10 @@ library ``libpair.so`` (header ``include/pair.h``):
 
 * ``pair_coeffs``: per-rollout coefficients of Eq. (pair-advantage);
 * ``pair_grad``: the LM-head realisation of the objective sum_i A_i log pi;
-* ``pair_estimate_dense``: Eq. (pair-ht) for explicit score vectors.
+* ``pair_estimate_dense``: Eq. (pair-ht) for explicit score vectors;
+* ``pair_pages_extend``, ``pair_cache_append``, ``pair_attend_paged``,
+  ``pair_verify_drafts``: a step of generating the continued rollouts, from a
+  paged cache and with drafted tokens.
 
 ``binding`` wraps those entry points for torch tensors (argument marshalling
 only). ``synth`` draws seeded synthetic workloads. Importing this package

@@ -562,7 +562,11 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
 // TMEM, the weights back into TMEM in the place of the scores (bf16, the A
 // operand of the second product), O_w += P_w V in TMEM throughout. Keys and
 // values come by TMA, one box per page piece, into the layout the products
-// read. Bound by the tensor cores and, close behind, by the exponentials.
+// read. Four chunks of 1025 to 2048 tokens behind 1000 to 6144 (32/8 heads of
+// 128): 422 us, 1.24 PFLOP/s, the tensor pipe 59 % active. Bound by shared
+// memory's reads (a product Q K^T of 64 cycles reads 8 KB at 128 bytes a cycle,
+// beside TMA's writes) and by the step's chain: products, scores out of TMEM,
+// maximum, exponentials, weights into TMEM.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     attend_many_kernel(Args a, const __grid_constant__ Maps maps) {
