@@ -11,7 +11,7 @@ using namespace tc;
 
 // CTA: warps 0-3 and 4-7 the softmax of one tile of 128 rows each (a row per
 // thread), warps 8 and 10 the producers of keys and of values (TMA), warp 9 the
-// MMA issuer. A row's 128 scores
+// MMA issuer, warp 11 looks values over. A row's 128 scores
 // stay in registers: the third warpgroup gives up registers to the other two
 // (208 x 256 + 80 x 128 of the 168 x 384 that the block is launched with).
 constexpr int kThreads = 384;
@@ -20,7 +20,8 @@ constexpr int BN = 128;       // keys of a tile
 
 template <int D>
 struct Tc {
-  static constexpr int kStages = D == 64 ? 8 : 5;  // ring of key and value tiles
+  static constexpr int kKeyStages = D == 64 ? 4 : 2;    // ring of key tiles
+  static constexpr int kValueStages = D == 64 ? 4 : 3;  // ring of value tiles
   static constexpr int kAtoms = D / 64;            // 128 rows x 64 columns, 128-byte swizzle
   static constexpr uint32_t kAtom = 128 * 128;
   static constexpr uint32_t kTile = kAtoms * kAtom;
@@ -31,9 +32,11 @@ struct Tc {
 template <int D>
 struct Smem {
   uint8_t q[2][Tc<D>::kTile];
-  uint8_t kv[Tc<D>::kStages][Tc<D>::kTile];
-  uint64_t full[Tc<D>::kStages], empty[Tc<D>::kStages];
-  uint64_t looked[Tc<D>::kStages];  // an edge tile's values have been looked over
+  uint8_t k[Tc<D>::kKeyStages][Tc<D>::kTile];
+  uint8_t v[Tc<D>::kValueStages][Tc<D>::kTile];
+  uint64_t k_full[Tc<D>::kKeyStages], k_empty[Tc<D>::kKeyStages];
+  uint64_t v_full[Tc<D>::kValueStages], v_empty[Tc<D>::kValueStages];
+  uint64_t looked[Tc<D>::kValueStages];  // values are there and, in an edge tile, looked over
   uint64_t done, q_full[2], s_full[2], p_ready[2][2], pv_done[2];
   int64_t scratch[kThreads / 32 + 2];
   uint32_t tmem;
@@ -127,22 +130,23 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, u
       : "memory");
 }
 
-// Place in the ring of key and value tiles.
+// Place in a ring of tiles. A barrier's phase tells a waiter one round from the
+// next only while it is in step: every waiter of a ring is its producer, its
+// consumer or one that the consumer waits for in each tile.
 template <int ST>
 struct Ring {
   int stage = 0;
   uint32_t phase = 0;
-  __device__ __forceinline__ void step(int n = 1) {
-    stage += n;
-    if (stage >= ST) {
-      stage -= ST;
+  __device__ __forceinline__ void step() {
+    if (++stage == ST) {
+      stage = 0;
       phase ^= 1;
     }
   }
 };
 
-// Tiles with keys that some row does not see: their scores are masked and
-// their values looked over.
+// Tiles with keys that some row does not see: their scores are masked and their
+// values looked over.
 __device__ __forceinline__ bool edge_tile(const Segment &s, int t) {
   return (t + 1) * BN > s.least;
 }
@@ -156,8 +160,9 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
   using C = Tc<D>;
   const int lane = threadIdx.x & 31;
   volatile int *abort = &sm.abort;
-  Ring<C::kStages> ring;
-  ring.step(kv);
+  constexpr int ST = kv ? C::kValueStages : C::kKeyStages;
+  Ring<ST> ring;
+  uint64_t *full = kv ? sm.v_full : sm.k_full, *empty = kv ? sm.v_empty : sm.k_empty;
   int issued = 0;
   const int box = maps.box;
   const bool mine = lane * box < BN;
@@ -183,8 +188,8 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
         ++at;
       }
       if (mine && key < end) id = row[at];
-      if (!(ok = wait(&sm.empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
-      uint64_t *bar = &sm.full[ring.stage];
+      if (!(ok = wait(&empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
+      uint64_t *bar = &full[ring.stage];
       const int n = __popc(__ballot_sync(0xffffffffu, load));
       if (lane == 0) mbar_expect_tx(bar, n * box * D * 2);
       __syncwarp();
@@ -196,13 +201,13 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
         const int c1 = where[0] == 1 ? cur : where[1] == 1 ? cur_off : s.h;
         const int c2 = where[0] == 2 ? cur : where[1] == 2 ? cur_off : s.h;
         const int c3 = where[0] == 3 ? cur : where[1] == 3 ? cur_off : s.h;
-        uint8_t *dst = sm.kv[ring.stage] + lane * box * 128;
+        uint8_t *dst = (kv ? sm.v[ring.stage] : sm.k[ring.stage]) + lane * box * 128;
 #pragma unroll
         for (int x = 0; x < C::kAtoms; ++x)
           tma_load_4d(dst + x * C::kAtom, map, bar, x * 64, c1, c2, c3);
       }
       ++issued;
-      ring.step(2);
+      ring.step();
     }
   }
   // Nothing may still be on its way into shared memory when the CTA ends: on
@@ -210,10 +215,9 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
   // ones are waited for here (the barrier of a stage completes once per use).
   if (!ok) {
     volatile int never = 0;
-    Ring<C::kStages> r;
-    r.step(kv);
-    for (int x = 0; x < issued; ++x, r.step(2))
-      if (2 * x >= 2 * issued - C::kStages) wait_limit(&sm.full[r.stage], r.phase, &never, a.dev_err, 10000000);
+    Ring<ST> r;
+    for (int x = 0; x < issued; ++x, r.step())
+      if (x >= issued - ST) wait_limit(&full[r.stage], r.phase, &never, a.dev_err, 10000000);
   }
 }
 
@@ -231,11 +235,12 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   using C = Tc<D>;
   volatile int *abort = &sm.abort;
   const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
-  const uint64_t dk = sdesc_sw128(smem_u32(sm.kv[0]), 16, 1024);
-  const uint64_t dv = sdesc_sw128(smem_u32(sm.kv[0]), C::kAtom, 1024);
+  const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
+  const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), C::kAtom, 1024);
   const uint32_t tmem = sm.tmem;
-  Ring<C::kStages> ring;
-  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0}, looked_ph = 0;
+  Ring<C::kKeyStages> kr;
+  Ring<C::kValueStages> vr;
+  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0};
   bool ok = true;
   auto scores = [&](int w, int stage, bool last) {  // S_w = Q_w K^T
     if (elect_one()) {
@@ -246,7 +251,7 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
                  dk + (stage * C::kTile + (kk >> 2) * C::kAtom) / 16 + in, C::kIdescS, kk != 0);
       }
       mma_commit(&sm.s_full[w]);
-      if (last) mma_commit(&sm.empty[stage]);
+      if (last) mma_commit(&sm.k_empty[stage]);
     }
     __syncwarp();
   };
@@ -261,7 +266,7 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
       }
       if (half) {
         mma_commit(&sm.pv_done[w]);
-        if (last) mma_commit(&sm.empty[stage]);
+        if (last) mma_commit(&sm.v_empty[stage]);
       }
     }
     __syncwarp();
@@ -270,50 +275,39 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   while (ok && walk.next(a, &s)) {
     if (s.t0 == s.t1) continue;
     const int top = s.rows > 128;  // the last active tile
-    if (!(ok = wait(&sm.full[ring.stage], ring.phase, abort, a.dev_err))) break;
+    if (!(ok = wait(&sm.k_full[kr.stage], kr.phase, abort, a.dev_err))) break;
     for (int w = 0; w <= top && ok; ++w) {
       if (!(ok = wait(&sm.q_full[w], q_ph[w], abort, a.dev_err))) break;
       q_ph[w] ^= 1;
       tc_fence_after();
-      scores(w, ring.stage, w == top);
+      scores(w, kr.stage, w == top);
     }
-    ring.step();
+    kr.step();
     for (int t = s.t0; t < s.t1 && ok; ++t) {
-      const int v_stage = ring.stage;
-      const uint32_t v_phase = ring.phase;
-      const bool more = t + 1 < s.t1, edge = edge_tile(s, t);
-      ring.step();
-      // Before the first products of a tile: weights, values, the next keys, and
-      // the values looked over.
-      {
-        const int lane = threadIdx.x & 31;
-        const bool next = lane == 2 && more, look = lane == 3 && edge;
-        uint64_t *bar = lane == 0   ? &sm.p_ready[0][0]
-                        : next      ? &sm.full[ring.stage]
-                        : look      ? &sm.looked[v_stage]
-                                    : &sm.full[v_stage];
-        const uint32_t phase = lane == 0 ? p_ph[0]
-                               : next    ? ring.phase
-                               : look    ? (looked_ph >> v_stage) & 1
-                                         : v_phase;
-        if (!(ok = wait_lanes(4, bar, phase, abort, a.dev_err))) break;
-        if (edge) looked_ph ^= 1u << v_stage;
-      }
+      const bool more = t + 1 < s.t1;
+      // Before the first products of a tile: weights, values, the next keys.
+      const int lane = threadIdx.x & 31;
+      uint64_t *bar = lane == 0   ? &sm.p_ready[0][0]
+                      : lane == 1 ? &sm.looked[vr.stage]
+                                  : &sm.k_full[kr.stage];
+      const uint32_t phase = lane == 0 ? p_ph[0] : lane == 1 ? vr.phase : kr.phase;
+      if (!(ok = wait_lanes(more ? 3 : 2, bar, phase, abort, a.dev_err))) break;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (w > top) break;
         if (w && !(ok = wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err))) break;
         tc_fence_after();
-        sums(w, v_stage, 0, t == s.t0, false);
+        sums(w, vr.stage, 0, t == s.t0, false);
         if (!(ok = wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err))) break;
         p_ph[w] ^= 1;
         tc_fence_after();
-        sums(w, v_stage, 1, false, w == top);
+        sums(w, vr.stage, 1, false, w == top);
         // In the tensor pipe's order behind the sums, which read the weights in
         // the place of these scores.
-        if (more) scores(w, ring.stage, w == top);
+        if (more) scores(w, kr.stage, w == top);
       }
-      if (more) ring.step();
+      vr.step();
+      if (more) kr.step();
     }
   }
   if (elect_one()) mma_commit(&sm.done);
@@ -322,37 +316,51 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   wait(&sm.done, 0, &never, a.dev_err);
 }
 
-// Values of an edge tile, by the threads of the active tiles: keys from `nk` on
-// become 0, what is not finite among those that some row does not see (from
-// `from` on) too (add_not_finite brings it back for the rows that see it).
-template <int kAtoms>
-__device__ __forceinline__ void look_over(uint8_t *tile, int from, int nk, int threads,
-                                          int *any_bad) {
-#pragma unroll
-  for (int atom = 0; atom < kAtoms; ++atom) {
-    uint4 *base = reinterpret_cast<uint4 *>(tile + atom * 128 * 128);
+// Of every tile: waits for the values, and in an edge tile makes those of keys
+// from `nk` on 0, and among those that some row does not see (from `from` on) what
+// is not finite too (add_not_finite brings it back for the rows that see it).
+template <int D>
+__device__ void look_over(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
+  using C = Tc<D>;
+  const int lane = threadIdx.x & 31;
+  volatile int *abort = &sm.abort;
+  Ring<C::kValueStages> ring;
+  Segment s;
+  while (walk.next(a, &s)) {
+    for (int t = s.t0; t < s.t1; ++t) {
+      if (!wait(&sm.v_full[ring.stage], ring.phase, abort, a.dev_err)) return;
+      if (edge_tile(s, t)) {
+        const int from = max(0, s.least - t * BN), nk = min(BN, s.keys - t * BN);
+        for (int atom = 0; atom < C::kAtoms; ++atom) {
+          uint4 *base = reinterpret_cast<uint4 *>(sm.v[ring.stage] + atom * C::kAtom);
 #pragma unroll 4
-    for (int x = from * 8 + threadIdx.x; x < 1024; x += threads) {
-      if ((x >> 3) >= nk) {
-        base[x] = make_uint4(0, 0, 0, 0);
-        continue;
-      }
-      uint4 u = base[x];
-      // Zero times what is not finite is NaN.
-      const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
-      const __nv_bfloat162 *v = reinterpret_cast<const __nv_bfloat162 *>(&u);
-      const __nv_bfloat162 t = __hfma2(v[0], zero, __hfma2(v[1], zero, __hfma2(v[2], zero,
-                                                                            __hmul2(v[3], zero))));
-      if (__hisnan(t.x) || __hisnan(t.y)) {
-        uint32_t *w = reinterpret_cast<uint32_t *>(&u);
+          for (int x = from * 8 + lane; x < BN * 8; x += 32) {
+            if ((x >> 3) >= nk) {
+              base[x] = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 u = base[x];
+            // Zero times what is not finite is NaN.
+            const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+            const __nv_bfloat162 *v = reinterpret_cast<const __nv_bfloat162 *>(&u);
+            const __nv_bfloat162 y = __hfma2(
+                v[0], zero, __hfma2(v[1], zero, __hfma2(v[2], zero, __hmul2(v[3], zero))));
+            if (__hisnan(y.x) || __hisnan(y.y)) {
+              uint32_t *w = reinterpret_cast<uint32_t *>(&u);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
-          if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
+              for (int k = 0; k < 4; ++k) {
+                if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+                if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0xffffu;
+              }
+              base[x] = u;
+              *reinterpret_cast<volatile int *>(&sm.any_bad) = 1;
+            }
+          }
         }
-        base[x] = u;
-        *any_bad = 1;
+        fence_async_smem();
       }
+      warp_arrive(&sm.looked[ring.stage]);
+      ring.step();
     }
   }
 }
@@ -368,7 +376,6 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
   // A negative scale goes into the queries' sign, a zero one makes them zero.
   const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
   const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
-  Ring<C::kStages> ring;
   uint32_t s_ph = 0, pv_ph = 0;
   bool ok = true;
   const int r = w * 128 + row;
@@ -398,31 +405,14 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
     s = ahead;
     const bool active = w == 0 || s.rows > 128, mine = r < s.rows;
     float m = -INFINITY, l = 0.f;
-    if (!active) {
-      for (int t = s.t0; t < s.t1; ++t) ring.step(2);
-    } else if (s.t0 < s.t1) {
+    if (active && s.t0 < s.t1) {
       const int seen = min(s.seen(mine ? r : 0, a.g), s.kv);
       for (int t = s.t0; t < s.t1; ++t) {
-        ring.step();
-        const int v_stage = ring.stage;
-        const uint32_t v_phase = ring.phase;
-        ring.step();
         const bool edge = edge_tile(s, t);
         const int key0 = t * BN;
         if (!(ok = wait(&sm.s_full[w], s_ph, abort, a.dev_err))) break;
         s_ph ^= 1;
         tc_fence_after();
-        if (edge) {
-          // Behind the wait for the scores, which go in step with this tile: a
-          // tile that sat out some segments could be whole rounds of the ring
-          // ahead, where a barrier's phase means another round.
-          if (!(ok = wait(&sm.full[v_stage], v_phase, abort, a.dev_err))) break;
-          look_over<C::kAtoms>(sm.kv[v_stage], max(0, s.least - key0), min(BN, s.keys - key0),
-                               s.rows > 128 ? 256 : 128, &sm.any_bad);
-          fence_async_smem();
-          warp_arrive(&sm.looked[v_stage]);
-          if (s.rows <= 128) warp_arrive(&sm.looked[v_stage]);  // for the other tile's warps
-        }
         uint32_t x[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32_async(tS + c * 32, x[c]);
@@ -580,10 +570,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (cta == ctas - 1) report_requests(a);
   }
   if (tid == 0) {
-    for (int x = 0; x < Tc<D>::kStages; ++x) {
-      mbar_init(&sm.full[x], 1);
-      mbar_init(&sm.empty[x], 1);
-      mbar_init(&sm.looked[x], 8);
+    for (int x = 0; x < Tc<D>::kKeyStages; ++x) {
+      mbar_init(&sm.k_full[x], 1);
+      mbar_init(&sm.k_empty[x], 1);
+    }
+    for (int x = 0; x < Tc<D>::kValueStages; ++x) {
+      mbar_init(&sm.v_full[x], 1);
+      mbar_init(&sm.v_empty[x], 1);
+      mbar_init(&sm.looked[x], 1);
     }
     mbar_init(&sm.done, 1);
     for (int w = 0; w < 2; ++w) {
@@ -612,6 +606,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       produce<D, 1>(a, maps, sm, walk);
     else if (warp == 9)
       issue<D>(a, sm, walk);
+    else
+      look_over<D>(a, sm, walk);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     softmax<D>(a, sm, walk, cta);
