@@ -271,31 +271,50 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
   __syncthreads();
   const int n = n_slots;
   const int rows = min(M, req.n * a.g - d.rt * M);
-  for (int r = blockIdx.y * (kJoinThreads / 32) + warp; r < rows;
-       r += gridDim.y * (kJoinThreads / 32)) {
+  constexpr int kWarps = kJoinThreads / 32, C = D / 32;
+  // With few partial sums a warp takes a row; with many (a long unit over many
+  // CTAs) the warps share a row's, in runs, and the first adds up what they have.
+  const bool share = n >= 2 * kWarps;
+  const int k0 = share ? warp * n / kWarps : 0, k1 = share ? (warp + 1) * n / kWarps : n;
+  const int step = share ? gridDim.y : gridDim.y * kWarps;
+  for (int r = share ? blockIdx.y : blockIdx.y * kWarps + warp; r < rows; r += step) {
     float mx = -INFINITY;
     for (int k = lane; k < n; k += 32) mx = fmaxf(mx, a.part[slots[k] * part_floats(M, D) + r]);
     for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
     const float ref = mx == -INFINITY ? 0.f : mx;
-    float l = 0.f, o[D / 32] = {};
+    float l = 0.f, o[C] = {};
 #pragma unroll 4
-    for (int k = 0; k < n; ++k) {
+    for (int k = k0; k < k1; ++k) {
       const float *p = a.part + slots[k] * part_floats(M, D);
       const float f = exp2f(p[r] - ref);
       l = fmaf(p[M + r], f, l);
-      const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * (D / 32));
+      const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * C);
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
+      for (int c = 0; c < C / 2; ++c) {
         const float2 x = src[c];
         o[2 * c] = fmaf(x.x, f, o[2 * c]);
         o[2 * c + 1] = fmaf(x.y, f, o[2 * c + 1]);
       }
     }
+    if (share) {
+      __shared__ float sums[kWarps][D + 1];
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < C; ++c) sums[warp][lane * C + c] = o[c];
+      if (lane == 0) sums[warp][D] = l;
+      __syncthreads();
+      if (warp != 0) continue;
+      for (int w = 1; w < kWarps; ++w) {
+        l += sums[w][D];
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] += sums[w][lane * C + c];
+      }
+    }
     const RowAt at = row_at(a, req.row0, d.rt * M, d.h, r);
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D + lane * (D / 32);
+    T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D + lane * C;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) from_float(out + c, o[c] * inv);
+    for (int c = 0; c < C; ++c) from_float(out + c, o[c] * inv);
     if (lane == 0 && a.lse)
       a.lse[at.token * a.Hq + at.head] = l == 0.f ? -INFINITY : (mx + log2f(l)) * kLn2;
   }
@@ -352,7 +371,7 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 // worth at most: the host knows the table's width, not the lengths.
 int useful_ctas(const Args &a, int M, int fit) {
   const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
-  const double keys = units * a.Hkv * (kUnitCost + (double)a.width * a.page + (double)M / a.g);
+  const double keys = units * a.Hkv * (unit_cost(M) + (double)a.width * a.page + (double)M / a.g);
   fit = fit < kMaxCtas ? fit : kMaxCtas;
   return keys < (double)fit * kMinKeys ? 1 + (int)(keys / kMinKeys) : fit;
 }

@@ -35,7 +35,13 @@ constexpr int kFewTile = 64;     // rows of a unit of the kernel for few rows
 // the former; at 48 161 there and 134 here.
 constexpr int kFewRows = 32;
 constexpr float kLn2 = 0.69314718055994531f;
-constexpr int kUnitCost = 48;    // a unit's fixed cost, in keys
+// A unit's fixed cost, in keys: what a CTA spends between two units and on
+// starting its tiles. 64 chunks of 32 to 256 tokens behind 100 to 3000 keys
+// (many rows): 474 us at 48 keys, 361 at 400, 322 at 800, 337 at 1600; 16 x 16
+// requests with drafts (few rows): 422 at 48, 404 at 128, 398 at 192.
+__host__ __device__ constexpr int unit_cost(int M) {
+  return M == kManyRows ? 800 : M == kFewTile ? 192 : 48;
+}
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
 
 struct Args {
@@ -99,7 +105,7 @@ struct Line {
   int32_t units;  // row tiles per key head
   int32_t M;
   __device__ __forceinline__ Line(const Request &r, int M_, int g) : M(M_) {
-    base = (int64_t)2 * g * (kUnitCost + max(0, r.kv - r.n));
+    base = (int64_t)2 * g * (unit_cost(M_) + max(0, r.kv - r.n));
     units = (int32_t)(((int64_t)r.n * g + M - 1) / M);
   }
   // Length of the first k units, and of unit k.
@@ -142,7 +148,11 @@ __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *sc
     total += scratch[w];
   }
   x += before - sum;  // exclusive
-  const int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * kMinKeys)));
+  int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * kMinKeys)));
+  if (a.R == 1) {  // units of one length, nearly: no CTA across two of them
+    const int64_t units = (int64_t)a.Hkv * Line(request(a, 0), M, a.g).units;
+    if (n > units && units > 0) n -= n % units;
+  }
   Share s{0, 0, 0, 0};
   if (cta < n) {
     s.from = (int64_t)((__int128)total * cta / n);

@@ -130,6 +130,13 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, u
       : "memory");
 }
 
+// 32 bytes, aligned so: a row's owner writes whole sectors.
+__device__ __forceinline__ void store32(void *to, const uint32_t (&u)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(u[0]),
+               "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
+
 // Place in a ring of tiles. A barrier's phase tells a waiter one round from the
 // next only while it is in step: every waiter of a ring is its producer, its
 // consumer or one that the consumer waits for in each tile.
@@ -502,6 +509,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
     const RowAt at = row_at(a, s.row0, s.r0, s.h, mine ? r : 0);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const float m2 = m == -INFINITY ? m : m * scale;
+    const bool aligned32 = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
     const bool bad = s.t0 < s.t1 && *reinterpret_cast<volatile int *>(&sm.any_bad) != 0;
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -513,26 +521,43 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
         for (int k = 0; k < 32; ++k) o[k] = 0.f;
       }
       if (!mine) continue;
+      if (bad) {
 #pragma unroll
-      for (int k = 0; k < 32; k += 8) {
-        float v[8];
+        for (int k = 0; k < 32; k += 8) {
+          float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = o[k + e];
-        if (bad) add_not_finite<D>(a, s, BN, r, c * 32 + k, v);
-        if (whole) {
-          uint4 u;
-          uint32_t *u4 = reinterpret_cast<uint32_t *>(&u);
+          for (int e = 0; e < 8; ++e) v[e] = o[k + e];
+          add_not_finite<D>(a, s, BN, r, c * 32 + k, v);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
-            u4[e] = *reinterpret_cast<const uint32_t *>(&b);
+          for (int e = 0; e < 8; ++e) o[k + e] = v[e];
+        }
+      }
+      if (whole) {
+        __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(a.out) + (at.token * a.Hq + at.head) * D +
+                            c * 32;
+#pragma unroll
+        for (int k = 0; k < 32; k += 16) {
+          uint32_t u[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const __nv_bfloat162 b =
+                __floats2bfloat162_rn(o[k + 2 * e] * inv, o[k + 2 * e + 1] * inv);
+            u[e] = *reinterpret_cast<const uint32_t *>(&b);
           }
-          *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
-                                     (at.token * a.Hq + at.head) * D + c * 32 + k) = u;
-        } else {
-          float4 *dst = reinterpret_cast<float4 *>(part + 2 * M + r * D + c * 32 + k);
-          dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-          dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+          if (aligned32) {
+            store32(to + k, u);
+          } else {
+            *reinterpret_cast<uint4 *>(to + k) = make_uint4(u[0], u[1], u[2], u[3]);
+            *reinterpret_cast<uint4 *>(to + k + 8) = make_uint4(u[4], u[5], u[6], u[7]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8) {
+          uint32_t u[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) u[e] = __float_as_uint(o[k + e]);
+          store32(part + 2 * M + r * D + c * 32 + k, u);
         }
       }
     }

@@ -179,6 +179,16 @@ def test_attend_strided_queries_and_scale(n):
         check(t, scale=scale)
 
 
+@pytest.mark.parametrize("n", [1, 90])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attend_output_on_a_16_byte_boundary(n, dtype):
+    t = build([(n, 300), (2 * n, 2 * n)], 4, 2, 128, 16, dtype, seed=4)
+    shape = t["q"].shape
+    out = torch.empty(t["q"].numel() + 8, dtype=dtype, device="cuda")[8:].view(shape)
+    assert out.data_ptr() % 32 == (16 if dtype is torch.bfloat16 else 0)
+    check(t, out=out)
+
+
 @pytest.mark.parametrize("n", [1, 3, 140])
 def test_attend_large_scores(n):
     """Scores far apart: weights that vanish, maxima that move in every tile."""
