@@ -7,7 +7,10 @@ namespace pairk {
 namespace {
 
 constexpr int kExtendThreads = 1024;
-constexpr int kExtendTokens = 2048;  // slots a block fills
+// Slots per thread: four where that still gives every SM a block, as the scan of
+// all requests is then shared by more of them.
+constexpr int kExtendMany = 4;
+constexpr int64_t kExtendSlots = 152 * kExtendThreads;
 
 struct ExtendArgs {
   int32_t R, page, width;
@@ -42,17 +45,18 @@ __device__ __forceinline__ Need request_need(const ExtendArgs &a, int i) {
 }
 
 // The prefix sums of tokens and of pages over all requests are formed by
-// every block for itself (12 bytes per request, from L2 after the first), a
-// run of consecutive requests per thread, so one launch does. Block b writes
-// the requests of its share and the slots [b kExtendTokens, (b+1)
-// kExtendTokens): a thread finds its token's request by bisection over the
-// runs and a walk along the run. A slot's page is read from the old table
-// entries or from the free list, never from entries this launch writes. Bound
-// by latency: loads of the lengths, one block scan, the bisection, two
-// dependent loads, stores (64 requests of one token: 4 us with the launch), and
-// with many tokens by the search's instructions (4096 requests, 526,000 tokens:
-// 18 us; with a list of requests per block and a warp to each, 38).
-__global__ void __launch_bounds__(kExtendThreads, 2) pages_extend_kernel(ExtendArgs a) {
+// every block for itself (12 bytes per request, from L2 after the first), a run
+// of consecutive requests per thread, so one launch does. A block writes the
+// requests of its share and its 1024 or 4096 slots: a thread finds a token's
+// request by bisection over the runs and a walk along the run. A slot's page is
+// read from the old table entries or from the free list, never from entries this
+// launch writes. Bound by latency: loads of the lengths, one block scan, the
+// bisection, two dependent loads, stores. 64 requests of one token take 4 us with
+// the launch, 4096 of one 9, 4096 of 128 on average 11.4 (a list of requests per
+// block and a warp to each: 38; a bisection per token: 18).
+template <int kPerLane>
+__global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs a) {
+  constexpr int kTokens = kPerLane * kExtendThreads;
   __shared__ int64_t warp_n[32], warp_p[32];
   __shared__ int64_t run_n[kExtendThreads], run_p[kExtendThreads];  // sums before a run
   __shared__ int last_page;
@@ -103,31 +107,43 @@ __global__ void __launch_bounds__(kExtendThreads, 2) pages_extend_kernel(ExtendA
   run_p[tid] = xp;
   __syncthreads();
 
-  const int64_t t0 = (int64_t)blockIdx.x * kExtendTokens;
-  const int64_t t1 = min(t0 + kExtendTokens, a.T);
-  for (int64_t t = t0 + tid; t < t1; t += kExtendThreads) {
+  // A warp has consecutive tokens, a lane every 32nd of them: the next one is
+  // mostly in the same run, a step or none further.
+  const int64_t t0 = (int64_t)blockIdx.x * kTokens + warp * (32 * kPerLane) + lane;
+  int run = -1, i = 0;
+  int64_t run_end = 0, row = 0, before = 0;
+  Need r{};
+#pragma unroll
+  for (int x = 0; x < kPerLane; ++x) {
+    const int64_t t = t0 + 32 * x;
+    if (t >= a.T) break;
     int64_t slot = -1;
     if (t < total_n) {
-      int lo = 0, hi = kExtendThreads;  // run_n[lo] <= t < run_n[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (run_n[mid] <= t) lo = mid; else hi = mid;
+      if (t >= run_end) {
+        int lo = run < 0 ? 0 : run, hi = kExtendThreads;  // run_n[lo] <= t < run_n[hi]
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (run_n[mid] <= t) lo = mid; else hi = mid;
+        }
+        run = lo;
+        run_end = lo + 1 < kExtendThreads ? run_n[lo + 1] : total_n;
+        i = lo * per;
+        row = run_n[lo];
+        before = run_p[lo];
+        r = request_need(a, i);
       }
-      int i = lo * per;
-      int64_t row = run_n[lo], first = run_p[lo];
-      Need r = request_need(a, i);
       while (row + r.n <= t) {
         row += r.n;
-        first += r.pages;
+        before += r.pages;
         r = request_need(a, ++i);
       }
-      if (!r.bad && first + r.pages <= avail && row + r.n <= a.T) {
+      if (!r.bad && before + r.pages <= avail && row + r.n <= a.T) {
         const uint32_t pos = r.len + (uint32_t)(t - row);
         const uint32_t at = pos / (uint32_t)a.page;
         const uint32_t off = pos - at * (uint32_t)a.page;
         int32_t *entry = a.table + (int64_t)i * a.width + at;
         const bool fresh = (int32_t)at >= r.held;
-        const int32_t id = fresh ? a.free_pages[first + at - r.held] : *entry;
+        const int32_t id = fresh ? a.free_pages[before + at - r.held] : *entry;
         // The held pages cover the cached tokens, so a new one begins with a
         // new token, whose thread enters it.
         if (fresh && off == 0) *entry = id;
@@ -248,7 +264,11 @@ pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t table_width,
                      free_count, T,   block_table, kv_len, held_out, cu_new, slots, taken,
                      dev_err};
   PAIR_BEGIN("pages_extend", s);
-  pages_extend_kernel<<<(unsigned)ceil_div(T, kExtendTokens), kExtendThreads, 0, s>>>(a);
+  if (T > kExtendSlots)
+    pages_extend_kernel<kExtendMany>
+        <<<(unsigned)ceil_div(T, kExtendMany * kExtendThreads), kExtendThreads, 0, s>>>(a);
+  else
+    pages_extend_kernel<1><<<(unsigned)ceil_div(T, kExtendThreads), kExtendThreads, 0, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
 }

@@ -41,15 +41,32 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 // their order. (Conversions to 64-bit integers go through the fp64 pipe: 80 %
 // busy with them, 256 rows of p and q took 104 us.)
 struct Weight {
-  uint32_t hi, lo;  // bits of the two sums, without their constants
+  uint32_t hi = 0, lo = 0;  // bits of the two sums, constants included
+  int n = 0;                // values added (at most 2^12, so that hi fits)
+  __device__ __forceinline__ void add(float x, float y) {
+    float2 t, s, r, u;
+    const float2 v = {x, y}, c8 = {8.f, 8.f}, m8 = {-8.f, -8.f}, one = {-1.f, -1.f};
+    const float2 c17 = {0x1p-17f, 0x1p-17f};
+#define PAIR_U64(f) reinterpret_cast<const uint64_t &>(f)
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(t)) : "l"(PAIR_U64(v)), "l"(PAIR_U64(c8)));
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(s)) : "l"(PAIR_U64(t)), "l"(PAIR_U64(m8)));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<uint64_t &>(r))
+        : "l"(PAIR_U64(s)), "l"(PAIR_U64(one)), "l"(PAIR_U64(v)));
+    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(u)) : "l"(PAIR_U64(r)), "l"(PAIR_U64(c17)));
+#undef PAIR_U64
+    hi += __float_as_uint(t.x) + __float_as_uint(t.y);
+    lo += __float_as_uint(u.x) + __float_as_uint(u.y);
+    n += 2;
+  }
   __device__ __forceinline__ long long value() const {
-    return ((long long)hi << 20) + lo;
+    return ((long long)(hi - n * 0x41000000u) << 20) + (lo - n * 0x37000000u);
   }
 };
-__device__ __forceinline__ Weight fixed_weight(float x) {
-  const float t = __fadd_rz(x, 8.f);
-  const float rest = x - (t - 8.f);
-  return {__float_as_uint(t) - 0x41000000u, __float_as_uint(__fadd_rz(rest, 0x1p-17f)) - 0x37000000u};
+__device__ __forceinline__ long long fixed_weight(float x) {
+  Weight w;
+  w.add(x, 0.f);
+  return w.value();
 }
 // a - b held to [0, 1]; NaN gives 0.
 __device__ __forceinline__ float sub_sat(float a, float b) {
@@ -69,7 +86,7 @@ struct Source {
   const T *p, *q;
   int V, skip;
   int mis, n_vec, whole0, whole1;  // vectors [whole0, whole1) lie in the row
-  bool q_alike;
+  int skip_vec;
 
   __device__ __forceinline__ Source(const T *p_, const T *q_, int V_, int skip_)
       : p(p_), q(q_), V(V_), skip(skip_) {
@@ -77,7 +94,9 @@ struct Source {
     n_vec = (V + mis + VEC - 1) / VEC;
     whole0 = mis ? 1 : 0;
     whole1 = (V + mis) / VEC;
-    q_alike = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15u) == 0;
+    if (q && ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(q)) & 15u) != 0)
+      whole1 = 0;
+    skip_vec = skip < 0 ? -1 : (skip + mis) / VEC;
   }
   // One vector, element by element; elements outside the row are 0.
   __device__ __forceinline__ void load(int v, float (&x)[VEC]) const {
@@ -89,46 +108,62 @@ struct Source {
         x[k] = sub_sat(as_float(p[e]), q ? as_float(q[e]) : 0.f);
     }
   }
-  static __device__ __forceinline__ long long sum(const float (&x)[VEC]) {
-    Weight s{0, 0};
+  __device__ __forceinline__ long long odd_sum(int v) const {
+    float f[VEC];
+    load(v, f);
+    Weight s;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const Weight w = fixed_weight(x[k]);
-      s.hi += w.hi;
-      s.lo += w.lo;
-    }
+    for (int k = 0; k < VEC; k += 2) s.add(f[k], f[k + 1]);
     return s.value();
   }
-  // Sums of the lane's vectors vb + 32 x + lane below v1, x < kPieces.
-  __device__ __forceinline__ void pieces(int vb, int v1, long long (&s)[kPieces]) const {
+  static __device__ __forceinline__ void add(const uint4 &a, const uint4 &b, Weight &s) {
+    const T *t = reinterpret_cast<const T *>(&a), *u = reinterpret_cast<const T *>(&b);
+#pragma unroll
+    for (int k = 0; k < VEC; k += 2)
+      s.add(sub_sat(as_float(t[k]), as_float(u[k])), sub_sat(as_float(t[k + 1]), as_float(u[k + 1])));
+  }
+  // The lane's vectors vb + 32 x + lane below v1, x < kPieces; bit x of the answer:
+  // this one is to be read element by element.
+  __device__ __forceinline__ unsigned fetch(int vb, int v1, uint4 (&a)[kPieces],
+                                            uint4 (&b)[kPieces]) const {
     const int lane = threadIdx.x & 31;
-    const uint4 zero = make_uint4(0, 0, 0, 0);
+    const uint4 *pv = reinterpret_cast<const uint4 *>(p - mis);
+    const uint4 *qv = reinterpret_cast<const uint4 *>(q - mis);
+    unsigned odd = 0;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int v = vb + 32 * x + lane;
+      const bool in = v >= whole0 && v < whole1 && v < v1 && v != skip_vec;
+      a[x] = b[x] = make_uint4(0, 0, 0, 0);
+      if (in) a[x] = __ldg(pv + v);
+      if (in && q) b[x] = __ldg(qv + v);
+      if (!in && v < v1) odd |= 1u << x;
+    }
+    return odd;
+  }
+  // Sums of these vectors, and the sum of all of the lane's in [v0, v1).
+  __device__ __forceinline__ void pieces(int vb, int v1, long long (&s)[kPieces]) const {
     uint4 a[kPieces], b[kPieces];
-    const bool two = q && q_alike;
+    const unsigned odd = fetch(vb, v1, a, b);
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) {
-      const int v = vb + 32 * x + lane;
-      const bool in = v >= whole0 && v < whole1 && v < v1 && !(q && !q_alike);
-      a[x] = b[x] = zero;
-      if (in) a[x] = __ldg(reinterpret_cast<const uint4 *>(p - mis) + v);
-      if (in && two) b[x] = __ldg(reinterpret_cast<const uint4 *>(q - mis) + v);
+      Weight w;
+      add(a[x], b[x], w);
+      s[x] = odd >> x & 1 ? odd_sum(vb + 32 * x + (threadIdx.x & 31)) : w.value();
     }
+  }
+  __device__ __forceinline__ long long segment(int v0, int v1) const {
+    long long total = 0;
+    for (int vb = v0; vb < v1; vb += 32 * kPieces) {
+      uint4 a[kPieces], b[kPieces];
+      unsigned odd = fetch(vb, v1, a, b);
+      Weight w;
 #pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      const int v = vb + 32 * x + lane;
-      const T *t = reinterpret_cast<const T *>(&a[x]), *u = reinterpret_cast<const T *>(&b[x]);
-      float f[VEC];
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        f[k] = sub_sat(as_float(t[k]), as_float(u[k]));
-        if (!q && v * VEC - mis + k == skip) f[k] = 0.f;
-      }
-      s[x] = sum(f);
-      if (v < v1 && (v < whole0 || v >= whole1 || (q && !q_alike))) {
-        load(v, f);
-        s[x] = sum(f);
-      }
+      for (int x = 0; x < kPieces; ++x) add(a[x], b[x], w);
+      total += w.value();  // (the odd ones' places hold zeros)
+      for (; odd; odd &= odd - 1) total += odd_sum(vb + 32 * (__ffs(odd) - 1) + (threadIdx.x & 31));
     }
+    return total;
   }
 };
 
@@ -167,7 +202,7 @@ __device__ __forceinline__ int find(const Source<T> &src, int v0, int v1, long l
       int tok = v * VEC - src.mis;
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {  // the first element whose sum passes `at`
-        c += fixed_weight(f[k]).value();
+        c += fixed_weight(f[k]);
         tok += c <= at;
       }
       return tok;
@@ -223,10 +258,11 @@ __device__ Decision decide(const VerifyArgs<T> &a, int i) {
 // dependent loads) while the others read, writes the accepted tokens, and,
 // where the draw falls into its CTA, goes over that warp's segment again while
 // the others are at the next request. Bound by HBM: one row of p, and of q where
-// a draft was refused, per request. 256 rows of 151,936 of both in fp32: 60 us,
-// 4.5 TB/s (with every warp doing everything, a request per cluster, 84); what
-// is missing are bytes in flight, 4 KB per warp and 24 warps per SM: with 8 or 2
-// vectors per lane, or a fourth CTA per SM by spilling, 74 to 120 us.
+// a draft was refused, per request. 256 rows of 151,936 of both in fp32: 58 us,
+// 4.7 TB/s (with every warp doing everything, a request per cluster, 84). Not
+// faster: 2, 3 or 8 vectors per lane in flight, vectors through shared memory, a
+// fourth CTA per SM, reading warps a request ahead of the exchange (60 to 120 us);
+// the clusters' last round, which is not full, costs as much as a full one.
 template <typename T>
 __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a) {
   __shared__ Decision s_dec[2];
@@ -283,13 +319,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
       const int buf = round++ & 1;
       if (!control) {
         const int v0 = min((rank * kVerifyWarps + warp) * per, n_vec), v1 = min(v0 + per, n_vec);
-        long long sum = 0;
-        for (int vb = v0; vb < v1; vb += 32 * kPieces) {
-          long long x[kPieces];
-          src.pieces(vb, v1, x);
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) sum += x[k];
-        }
+        long long sum = src.segment(v0, v1);
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == 0) s_warp[buf][warp] = sum;
       }
@@ -309,8 +339,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
         total += s_cta[buf][c];
       }
       if (total == 0 && pass == 0) {  // nothing left of the difference: p alone
-        src.q = nullptr;
-        src.skip = -1;
+        src = Source<T>(prow, nullptr, a.V, -1);
         continue;
       }
       if (!control) break;

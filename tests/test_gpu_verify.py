@@ -62,6 +62,26 @@ def test_verify(K, V, pad, with_q, dtype):
         assert 0 < (want["n"] == 1).sum() < len(K) and (want["n"] == np.asarray(K) + 1).any()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_verify_rows_that_lie_differently(dtype):
+    """q's rows begin at another place within 16 bytes than p's."""
+    c = case([3, 0, 5, -1, 2], 1001, dtype, True, seed=6)
+    wide = torch.full((c["q"].shape[0], 1010), float("nan"), dtype=dtype, device="cuda")
+    wide[:, 3:1004] = c["q"]
+    check(dict(c, q=wide[:, 3:1004]))
+    check(dict(c, p=wide[:, 3:1004], q=c["p"].contiguous()))
+
+
+@pytest.mark.parametrize("y", [0, 1, 3, 4, 7, 8, 511, 512, 998, 999])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_verify_looked_up_draft_anywhere_in_the_row(y, dtype):
+    c = case([1] * 40, 1000, dtype, False, seed=y)
+    c["ids"][:] = y
+    c["u"][:] = 1.0  # never accepted: drawn from p without the draft
+    want = check(c)
+    assert (want["n"] == 1).all() and not (want["ids"] == y).any()
+
+
 @pytest.mark.parametrize("with_q", [True, False])
 def test_verify_large_vocabulary(with_q):
     check(case([3, 3], 151936, torch.float32, with_q, seed=4))
