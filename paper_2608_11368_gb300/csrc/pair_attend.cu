@@ -239,24 +239,45 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
 
 constexpr int kJoinThreads = 256;
 
-// Joins the partial sums of a unit: the block of the CTA that has the unit's
-// beginning. Its other pieces are the first segments of the CTAs behind. A
-// warp takes a row; sums go in the order of the keys.
+// Blocks that share the rows of one of a launch's units: 32 rows each.
+__host__ __device__ inline int join_blocks(const Launch &l) {
+  int64_t rows = l.a.T * l.a.g;
+  if (rows > l.M) rows = l.M;
+  if (rows > l.a.rows_upto) rows = l.a.rows_upto;
+  return (int)((rows + 31) / 32);
+}
+
+// Joins the partial sums of the units that more than one CTA worked on, of one
+// launch or of two: blocks of the CTA that has a unit's beginning. The other
+// pieces are the first segments of the CTAs behind. Sums go in the order of the
+// keys. Bound by latency (notes, then statistics, then sums) and, after a launch
+// with many rows, by the 40 MB of its partial sums.
 template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M, int ctas) {
+__global__ void __launch_bounds__(kJoinThreads)
+    attend_join_kernel(const __grid_constant__ Launch l0, const __grid_constant__ Launch l1) {
+  const int first = l0.ctas * join_blocks(l0);  // blocks of the first launch's sums
+  const bool second = (int)blockIdx.x >= first;
+  const Args &a = second ? l1.a : l0.a;
+  const int M = second ? l1.M : l0.M, ctas = second ? l1.ctas : l0.ctas;
+  const int per = join_blocks(second ? l1 : l0);
+  const int block = blockIdx.x - (second ? first : 0);
+  const int cta = block / per, y = block - cta * per;
   __shared__ int slots[kMaxCtas];
   __shared__ int n_slots;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_previous();
-  const int mine = blockIdx.x * 2 + blockIdx.z;
-  const Desc d = a.desc[mine];
+  // A CTA has the beginning of one unit at most whose end it does not have.
+  const Desc d0 = a.desc[cta * 2], d1 = a.desc[cta * 2 + 1];
+  const bool is0 = d0.tiles != 0 && d0.t0 == 0;
+  const Desc d = is0 ? d0 : d1;
   if (d.tiles == 0 || d.t0 != 0) return;
+  const int mine = cta * 2 + (is0 ? 0 : 1);
   const Request req = request(a, d.i);
   if (warp == 0) {
     int n = 1;
     if (lane == 0) slots[0] = mine;
     bool more = true;
-    for (int c0 = blockIdx.x + 1; more && c0 < ctas; c0 += 32) {
+    for (int c0 = cta + 1; more && c0 < ctas; c0 += 32) {
       const int c = c0 + lane;
       Desc e{};
       if (c < ctas) e = a.desc[c * 2];
@@ -276,8 +297,8 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
   // CTAs) the warps share a row's, in runs, and the first adds up what they have.
   const bool share = n >= 2 * kWarps;
   const int k0 = share ? warp * n / kWarps : 0, k1 = share ? (warp + 1) * n / kWarps : n;
-  const int step = share ? gridDim.y : gridDim.y * kWarps;
-  for (int r = share ? blockIdx.y : blockIdx.y * kWarps + warp; r < rows; r += step) {
+  const int step = share ? per : per * kWarps;
+  for (int r = share ? y : y * kWarps + warp; r < rows; r += step) {
     float mx = -INFINITY;
     for (int k = lane; k < n; k += 32) mx = fmaxf(mx, a.part[slots[k] * part_floats(M, D) + r]);
     for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
@@ -321,23 +342,25 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(Args a, int M
 }
 
 template <int D>
-pair_status run_simt(const Args &a, cudaStream_t s) {
+pair_status run_simt(Launch *l, cudaStream_t s) {
+  const Args &a = l->a;
   constexpr int smem = sizeof(SimtSmem<D>);
   static_assert(smem <= 232448, "shared memory of a CTA");
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = useful_ctas(a, kSimtRows, (D <= 128 ? 2 : 1) * sm_count());
+  const int ctas = useful_ctas(a, kSimtRows, min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count()));
   PAIR_BEGIN("attend_simt", s);
   attend_simt_kernel<D><<<ctas, kSimtThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
-  return launch_join(a, D, kSimtRows, ctas, PAIR_F32, s);
+  l->M = kSimtRows;
+  l->ctas = ctas;
+  return PAIR_OK;
 }
 
 template <typename T, int D>
-pair_status run_join(const Args &a, int M, int ctas, cudaStream_t s) {
+pair_status run_join(const Launch &l0, const Launch &l1, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  const int64_t rows = a.T * a.g < M ? a.T * a.g : M;  // of a unit, at most
-  cfg.gridDim = dim3(ctas, (unsigned)ceil_div(rows, 16), 2);
+  cfg.gridDim = dim3(l0.ctas * join_blocks(l0) + l1.ctas * join_blocks(l1), 1, 1);
   cfg.blockDim = dim3(kJoinThreads, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr;
@@ -346,7 +369,7 @@ pair_status run_join(const Args &a, int M, int ctas, cudaStream_t s) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   PAIR_BEGIN("attend_join", s);
-  if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, a, M, ctas) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, l0, l1) != cudaSuccess) {
     cudaGetLastError();
     return PAIR_ERR_CUDA;
   }
@@ -361,7 +384,11 @@ pair_status by_size(int D, F f) {
   return f(std::integral_constant<int, 256>());
 }
 
-size_t desc_bytes() { return kMaxCtas * 2 * sizeof(Desc); }
+// The workspace: notes and partial sums of a launch with few or, in fp32, any rows,
+// then those of a launch with many.
+constexpr size_t kNotes = kMaxCtas * 2 * sizeof(Desc), kManyNotes = kMaxMany * 2 * sizeof(Desc);
+size_t few_floats(int D) { return kMaxCtas * 2 * part_floats(kFewTile, D); }
+size_t many_floats(int D) { return kMaxMany * 2 * part_floats(kManyRows, D); }
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -372,7 +399,6 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 int useful_ctas(const Args &a, int M, int fit) {
   const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
   const double keys = units * a.Hkv * (unit_cost(M) + (double)a.width * a.page + (double)M / a.g);
-  fit = fit < kMaxCtas ? fit : kMaxCtas;
   return keys < (double)fit * kMinKeys ? 1 + (int)(keys / kMinKeys) : fit;
 }
 
@@ -386,14 +412,15 @@ int sm_count() {
   return n;
 }
 
-pair_status launch_simt(const Args &a, int D, cudaStream_t s) {
-  return by_size(D, [&](auto d) { return run_simt<decltype(d)::value>(a, s); });
+pair_status launch_simt(Launch *l, int D, cudaStream_t s) {
+  return by_size(D, [&](auto d) { return run_simt<decltype(d)::value>(l, s); });
 }
 
-pair_status launch_join(const Args &a, int D, int M, int ctas, pair_dtype dt, cudaStream_t s) {
+static pair_status launch_join(const Launch &l0, const Launch &l1, int D, pair_dtype dt,
+                               cudaStream_t s) {
   return by_size(D, [&](auto d) {
-    return dt == PAIR_BF16 ? run_join<__nv_bfloat16, decltype(d)::value>(a, M, ctas, s)
-                           : run_join<float, decltype(d)::value>(a, M, ctas, s);
+    return dt == PAIR_BF16 ? run_join<__nv_bfloat16, decltype(d)::value>(l0, l1, s)
+                           : run_join<float, decltype(d)::value>(l0, l1, s);
   });
 }
 
@@ -409,7 +436,7 @@ size_t pair_attend_workspace_size(int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
   if (R < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || (D != 64 && D != 128 && D != 256) ||
       (dt != PAIR_F32 && dt != PAIR_BF16))
     return 0;
-  return desc_bytes() + kMaxCtas * 2 * part_floats(kMaxRows, D) * sizeof(float);
+  return kNotes + kManyNotes + (few_floats(D) + many_floats(D)) * sizeof(float);
 }
 
 pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
@@ -462,20 +489,25 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                out,
                lse,
                static_cast<Desc *>(ws),
-               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + desc_bytes()),
+               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + kNotes + kManyNotes),
                dev_err};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (dt == PAIR_F32) return launch_simt(a, D, s);
+  Launch few{a, 0, 0}, many{a, 0, 0};
+  many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + kNotes);
+  many.a.part += few_floats(D);
   // Which kernel a chunk goes to is decided by its rows, on the device; a
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
-  if (most_rows <= kFewRows || !many_applies(a, D)) return launch_few(a, D, s);
-  if (R == 1) return launch_many(a, D, s);
-  Args few = a, many = a;
-  few.rows_upto = kFewRows;
-  many.rows_over = kFewRows;
-  const pair_status st = launch_few(few, D, s);
-  return st != PAIR_OK ? st : launch_many(many, D, s);
+  const bool only_few = dt == PAIR_F32 || most_rows <= kFewRows || !many_applies(a, D);
+  if (!only_few && R > 1) {
+    few.a.rows_upto = kFewRows;
+    many.a.rows_over = kFewRows;
+  }
+  pair_status st = PAIR_OK;
+  if (dt == PAIR_F32) st = launch_simt(&few, D, s);
+  else if (only_few || R > 1) st = launch_few(&few, D, s);
+  if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
+  return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;
 }
 
 }  // extern "C"

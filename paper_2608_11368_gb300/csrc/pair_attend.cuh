@@ -26,8 +26,8 @@
 namespace pairk {
 namespace attend {
 
-constexpr int kMaxCtas = 480;    // of one call, at most
-constexpr int kMaxRows = 256;    // rows of a unit, at most
+constexpr int kMaxCtas = 480;    // of a launch with units of up to kFewTile rows
+constexpr int kMaxMany = 160;    // of a launch with units of kManyRows rows
 constexpr int kManyRows = 256;   // rows of a unit of the kernel for many rows
 constexpr int kFewTile = 64;     // rows of a unit of the kernel for few rows
 // Chunks of up to so many rows go to the kernel for few rows, longer ones to the
@@ -59,7 +59,7 @@ struct Args {
   float scale;
   void *out;
   float *lse;
-  struct Desc *desc;  // [kMaxCtas][2] segments of each CTA
+  struct Desc *desc;  // [CTAs][2] segments of each CTA
   float *part;        // partial sums, part_floats() each
   int32_t *dev_err;
 };
@@ -357,9 +357,10 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The pass that joins the partial sums is launched while the kernel before it
-// still runs (programmatic dependent launch): that kernel's blocks say when
-// they have no more work, the joining ones wait for its end.
+// Programmatic dependent launch. The kernel for many rows starts beside the one
+// for few, on whose results it does not depend (it waits for its end only before
+// its own, so that what comes after it comes after both); the pass that joins the
+// partial sums starts while the kernel before it drains, and waits for its end.
 __device__ __forceinline__ void let_next_start() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
@@ -367,12 +368,16 @@ __device__ __forceinline__ void wait_for_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// Host side: the kernels and the pass that joins their partial sums.
-pair_status launch_simt(const Args &a, int D, cudaStream_t s);
-pair_status launch_few(const Args &a, int D, cudaStream_t s);
+// Host side: the kernels, and the pass that joins the partial sums of up to two
+// launches.
+struct Launch {
+  Args a;
+  int M, ctas;  // rows of its units; 0 CTAs: there is no such launch
+};
+pair_status launch_simt(Launch *l, int D, cudaStream_t s);
+pair_status launch_few(Launch *l, int D, cudaStream_t s);
 bool many_applies(const Args &a, int D);
-pair_status launch_many(const Args &a, int D, cudaStream_t s);
-pair_status launch_join(const Args &a, int D, int M, int ctas, pair_dtype dt, cudaStream_t s);
+pair_status launch_many(Launch *l, int D, cudaStream_t s);
 int sm_count();
 int useful_ctas(const Args &a, int M, int fit);
 

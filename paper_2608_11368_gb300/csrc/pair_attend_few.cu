@@ -334,6 +334,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   const int cta = blockIdx.x, ctas = gridDim.x;
+  if (a.rows_upto < INT32_MAX) let_next_start();  // the kernel for many rows
   clear_notes(a, cta);
   clear_spare_rows<__nv_bfloat16, D, kThreads>(a, cta, ctas);
   if (cta == ctas - 1)
@@ -352,23 +353,26 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(
 }
 
 template <int D>
-pair_status run_few(const Args &a, cudaStream_t s) {
+pair_status run_few(Launch *l, cudaStream_t s) {
+  const Args &a = l->a;
   constexpr int smem = Few<D>::kBytes;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_few_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = useful_ctas(a, M, (D <= 128 ? 3 : 1) * sm_count());
+  const int ctas = useful_ctas(a, M, min(kMaxCtas, (D <= 128 ? 3 : 1) * sm_count()));
   PAIR_BEGIN("attend_few", s);
   attend_few_kernel<D><<<ctas, kThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
-  return launch_join(a, D, M, ctas, PAIR_BF16, s);
+  l->M = M;
+  l->ctas = ctas;
+  return PAIR_OK;
 }
 
 }  // namespace
 
-pair_status launch_few(const Args &a, int D, cudaStream_t s) {
-  if (D == 64) return run_few<64>(a, s);
-  if (D == 128) return run_few<128>(a, s);
-  return run_few<256>(a, s);
+pair_status launch_few(Launch *l, int D, cudaStream_t s) {
+  if (D == 64) return run_few<64>(l, s);
+  if (D == 128) return run_few<128>(l, s);
+  return run_few<256>(l, s);
 }
 
 }  // namespace attend

@@ -645,6 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tmem_relinquish();
     tmem_dealloc(sm.tmem, 512);
   }
+  if (a.rows_over >= 0) wait_for_previous();
 }
 
 // 4-D map of a cache, dimensions in the order of their strides: boxes of `box`
@@ -680,16 +681,32 @@ bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args &a, in
 }
 
 template <int D>
-pair_status run_many(const Args &a, const Maps &maps, cudaStream_t s) {
+pair_status run_many(Launch *l, const Maps &maps, cudaStream_t s) {
+  const Args &a = l->a;
   constexpr int smem = sizeof(Smem<D>) + 1024;
   static_assert(smem <= 232448, "shared memory of a CTA");
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_many_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const int ctas = useful_ctas(a, M, sm_count());
+  const int ctas = useful_ctas(a, M, min(kMaxMany, sm_count()));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas, 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = a.rows_over >= 0 ? 1 : 0;  // behind the launch for few rows
   PAIR_BEGIN("attend_many", s);
-  attend_many_kernel<D><<<ctas, kThreads, smem, s>>>(a, maps);
+  if (cudaLaunchKernelEx(&cfg, attend_many_kernel<D>, a, maps) != cudaSuccess) {
+    cudaGetLastError();
+    return PAIR_ERR_CUDA;
+  }
   PAIR_LAUNCH_CHECK(s);
-  return launch_join(a, D, M, ctas, PAIR_BF16, s);
+  l->M = M;
+  l->ctas = ctas;
+  return PAIR_OK;
 }
 
 bool many_maps(const Args &a, int D, Maps *maps) {
@@ -710,10 +727,10 @@ bool many_applies(const Args &a, int D) {
   return many_maps(a, D, &maps);
 }
 
-pair_status launch_many(const Args &a, int D, cudaStream_t s) {
+pair_status launch_many(Launch *l, int D, cudaStream_t s) {
   Maps maps;
-  if (!many_maps(a, D, &maps)) return PAIR_ERR_CUDA;
-  return D == 64 ? run_many<64>(a, maps, s) : run_many<128>(a, maps, s);
+  if (!many_maps(l->a, D, &maps)) return PAIR_ERR_CUDA;
+  return D == 64 ? run_many<64>(l, maps, s) : run_many<128>(l, maps, s);
 }
 
 }  // namespace attend
