@@ -1,7 +1,7 @@
 // pair_attend_paged for chunks with few rows (single tokens, drafts), bf16: one
 // pass over the cached keys and values, bound by HBM. 16 x 16 requests of up to
 // 4096 keys on 32/8 heads: a token each would read 2.4 GB; five rows each (20 per
-// key head) take 420 us, 5.8 TB/s; 32 x 16 skewed ones with a token each run at
+// key head) take 390 us, 6.2 TB/s; 32 x 16 skewed ones with a token each run at
 // the copy's rate (6.8 TB/s). mma.sync rather than tcgen05: a tile of 128 rows
 // would be 16 to 32 rows full, and its chain of products and softmax takes as
 // long as the bytes of a tile.
@@ -339,7 +339,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(
   clear_spare_rows<__nv_bfloat16, D, kThreads>(a, cta, ctas);
   if (cta == ctas - 1)
     report_requests(a);
-  Walk<M, Few<D>::BN> walk{find_share<kThreads>(a, M, cta, ctas, reinterpret_cast<int64_t *>(smem))};
+  Walk<M, Few<D>::BN> walk{
+      find_share<kThreads>(a, M, cta, ctas, reinterpret_cast<int64_t *>(smem))};
   Segment s;
   for (int seg = 0; walk.next(a, &s); ++seg) {
     if (s.rows <= 16)

@@ -11,9 +11,9 @@ using namespace tc;
 
 // CTA: warps 0-3 and 4-7 the softmax of one tile of 128 rows each (a row per
 // thread), warps 8 and 10 the producers of keys and of values (TMA), warp 9 the
-// MMA issuer, warp 11 looks values over. A row's 128 scores
-// stay in registers: the third warpgroup gives up registers to the other two
-// (208 x 256 + 80 x 128 of the 168 x 384 that the block is launched with).
+// MMA issuer, warp 11 looks values over. A row's 128 scores stay in registers:
+// the third warpgroup gives up registers to the other two (208 x 256 + 80 x 128
+// of the 168 x 384 that the block is launched with).
 constexpr int kThreads = 384;
 constexpr int M = kManyRows;  // two tiles of 128
 constexpr int BN = 128;       // keys of a tile
@@ -578,7 +578,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
 // operand of the second product), O_w += P_w V in TMEM throughout. Keys and
 // values come by TMA, one box per page piece, into the layout the products
 // read. Four chunks of 1025 to 2048 tokens behind 1000 to 6144 (32/8 heads of
-// 128): 422 us, 1.24 PFLOP/s, the tensor pipe 59 % active. Bound by shared
+// 128): 378 us, 1.38 PFLOP/s, the tensor pipe 63 % active. Bound by shared
 // memory's reads (a product Q K^T of 64 cycles reads 8 KB at 128 bytes a cycle,
 // beside TMA's writes) and by the step's chain: products, scores out of TMEM,
 // maximum, exponentials, weights into TMEM.

@@ -48,12 +48,18 @@ struct Weight {
     const float2 v = {x, y}, c8 = {8.f, 8.f}, m8 = {-8.f, -8.f}, one = {-1.f, -1.f};
     const float2 c17 = {0x1p-17f, 0x1p-17f};
 #define PAIR_U64(f) reinterpret_cast<const uint64_t &>(f)
-    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(t)) : "l"(PAIR_U64(v)), "l"(PAIR_U64(c8)));
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(s)) : "l"(PAIR_U64(t)), "l"(PAIR_U64(m8)));
+    asm("add.rz.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t &>(t))
+        : "l"(PAIR_U64(v)), "l"(PAIR_U64(c8)));
+    asm("add.rn.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t &>(s))
+        : "l"(PAIR_U64(t)), "l"(PAIR_U64(m8)));
     asm("fma.rn.f32x2 %0, %1, %2, %3;"
         : "=l"(reinterpret_cast<uint64_t &>(r))
         : "l"(PAIR_U64(s)), "l"(PAIR_U64(one)), "l"(PAIR_U64(v)));
-    asm("add.rz.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t &>(u)) : "l"(PAIR_U64(r)), "l"(PAIR_U64(c17)));
+    asm("add.rz.f32x2 %0, %1, %2;"
+        : "=l"(reinterpret_cast<uint64_t &>(u))
+        : "l"(PAIR_U64(r)), "l"(PAIR_U64(c17)));
 #undef PAIR_U64
     hi += __float_as_uint(t.x) + __float_as_uint(t.y);
     lo += __float_as_uint(u.x) + __float_as_uint(u.y);
@@ -120,7 +126,8 @@ struct Source {
     const T *t = reinterpret_cast<const T *>(&a), *u = reinterpret_cast<const T *>(&b);
 #pragma unroll
     for (int k = 0; k < VEC; k += 2)
-      s.add(sub_sat(as_float(t[k]), as_float(u[k])), sub_sat(as_float(t[k + 1]), as_float(u[k + 1])));
+      s.add(sub_sat(as_float(t[k]), as_float(u[k])),
+            sub_sat(as_float(t[k + 1]), as_float(u[k + 1])));
   }
   // The lane's vectors vb + 32 x + lane below v1, x < kPieces; bit x of the answer:
   // this one is to be read element by element.
@@ -457,7 +464,8 @@ extern "C" pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   if (dt == PAIR_BF16)
     return launch_verify<__nv_bfloat16>(
-        {T, R, V, 1, 1, static_cast<const __nv_bfloat16 *>(p), static_cast<const __nv_bfloat16 *>(q),
+        {T, R, V, 1, 1, static_cast<const __nv_bfloat16 *>(p),
+         static_cast<const __nv_bfloat16 *>(q),
          p_row, q_row, ids, cu_new, u, u_draw, out_ids, logp, n_emit, dev_err}, s);
   return launch_verify<float>({T, R, V, 1, 1, static_cast<const float *>(p),
                                static_cast<const float *>(q), p_row, q_row, ids, cu_new, u,
