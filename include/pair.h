@@ -606,9 +606,10 @@ PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_d
  * Workspace: pair_attend_workspace_size bytes, 256-byte aligned, any contents.
  * Errors: PAIR_ERR_INVALID_ARG, PAIR_ERR_UNSUPPORTED (another D),
  *      PAIR_ERR_WORKSPACE; device PAIR_DEV_ERR_PAGES: a page id outside
- *      [0, num_pages) or a kv_len that is negative or beyond the table row
- *      (that request's rows are unspecified), or offsets cu_new that decrease
- *      or pass T (all rows are). Nothing outside the arrays is read or written.
+ *      [0, num_pages) or a kv_len that is negative, beyond the table row or
+ *      above 2^31 - 4097 (that request's rows are unspecified), or offsets cu_new
+ *      that decrease or pass T (all rows are). Nothing outside the arrays is
+ *      read or written.
  *      PAIR_DEV_ERR_TIMEOUT as for pair_grad.
  * No output, nor ws, may overlap an input.
  * Deterministic for the same arguments on the same device.

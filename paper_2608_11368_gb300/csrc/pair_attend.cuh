@@ -42,6 +42,9 @@ constexpr float kLn2 = 0.69314718055994531f;
 __host__ __device__ constexpr int unit_cost(int M) {
   return M == kManyRows ? 800 : M == kFewTile ? 192 : 48;
 }
+// Keys of a request at most: tile numbers, and a unit's length with its fixed
+// cost, stay within 32 bits.
+constexpr int kMaxKeys = INT32_MAX - 4096;
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
 
 struct Args {
@@ -85,7 +88,7 @@ __device__ __forceinline__ Request request(const Args &a, int i) {
   const int64_t most = (int64_t)a.width * a.page;
   Request r{lo, sane ? hi - lo : 0, len < 0 ? 0 : (int32_t)(len > most ? most : len)};
   const int rows = r.n * a.g;
-  if (rows <= a.rows_over || rows > a.rows_upto) r.n = 0;
+  if (rows <= a.rows_over || rows > a.rows_upto || r.kv > kMaxKeys) r.n = 0;
   return r;
 }
 // By a whole block: requests whose entries do not fit together.
@@ -93,7 +96,8 @@ __device__ __forceinline__ void report_requests(const Args &a) {
   bool bad = false;
   for (int i = threadIdx.x; i < a.R; i += blockDim.x) {
     const int lo = a.cu[i], hi = a.cu[i + 1], len = a.kv_len[i];
-    bad |= lo < 0 || hi < lo || hi > a.T || len < 0 || len > (int64_t)a.width * a.page;
+    bad |= lo < 0 || hi < lo || hi > a.T || len < 0 || len > kMaxKeys ||
+           len > (int64_t)a.width * a.page;
   }
   if (bad || (threadIdx.x == 0 && a.cu[0] != 0)) flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
 }

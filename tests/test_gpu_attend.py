@@ -262,6 +262,29 @@ def test_attend_reports_pages_that_do_not_fit():
         assert B.STATUS_NAMES[st] == "PAIR_ERR_PAGES"
 
 
+def test_attend_reports_lengths_that_pass_32_bits():
+    """A table row of 2^31 tokens: a length that leaves no room for whole tiles
+    in 32 bits is reported, and the other request is served."""
+    from paper_2608_11368_gb300 import binding as B
+    for dtype in (torch.bfloat16, torch.float32):
+        t = build([(2, 40), (2, 40)], 4, 2, 64, 64, dtype)
+        x = {c: t[c][int(t["table"][0, 0]):, :1][:1].expand(1, 2 ** 30, 2, 64) for c in "kv"}
+        table = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+        def run(kv):
+            kv = torch.tensor(kv, dtype=torch.int32, device="cuda")
+            out, _ = B.pair_attend_paged(t["q"], x["k"], x["v"], table, kv, t["cu"], dev_err=err)
+            return B.pair_status_sync(err), out
+
+        st, good = run([40, 40])
+        assert st == 0 and bool(torch.isfinite(good).all())
+        for kv in (2 ** 31 - 1, 2 ** 31 - 4096):
+            st, out = run([40, kv])
+            assert B.STATUS_NAMES[st] == "PAIR_ERR_PAGES"
+            assert torch.equal(out[:2], good[:2])
+
+
 def test_attend_refuses():
     from paper_2608_11368_gb300 import binding as B
     t = build([(2, 40)], 4, 2, 64, 16, torch.bfloat16)
