@@ -476,10 +476,20 @@ def _ptr(t, name, dtype, shape, like, at):
     return t.data_ptr()
 
 
-def _out_ptr(t, name, dtype, shape, like, at):
+def _fresh(shape, dtype, like, stream):
+    """Tensor on like's device, of the memory of the stream that will write it:
+    memory of another one may still be in use there, or be given out again there
+    before the call has run."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _out_ptr(t, name, dtype, shape, like, at, stream):
     """Output tensor (allocated where it is None) and its pointer."""
     if t is None:
-        t = torch.empty(shape, dtype=dtype, device=like.device)
+        t = _fresh(shape, dtype, like, stream)
         return t, t.data_ptr()
     return t, _ptr(t, name, dtype, shape, like, at)
 
@@ -531,11 +541,11 @@ def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, pa
            _ptr(free_pages, "free_pages", i32, (F,), lens, at))
     count = _ptr(free_count, "free_count", i32, (1,), lens, at)
     table = _ptr(block_table, "block_table", i32, (R, width), lens, at)
-    kv_len, kv_p = _out_ptr(kv_len, "kv_len", i32, per, lens, at)
-    held_out, held_p = _out_ptr(held_out, "held_out", i32, per, lens, at)
-    cu_new, cu_p = _out_ptr(cu_new, "cu_new", i32, (R + 1,), lens, at)
-    slots, slots_p = _out_ptr(slots, "slots", torch.int64, (T,), lens, at)
-    taken, taken_p = _out_ptr(taken, "taken", i32, (1,), lens, at)
+    kv_len, kv_p = _out_ptr(kv_len, "kv_len", i32, per, lens, at, stream)
+    held_out, held_p = _out_ptr(held_out, "held_out", i32, per, lens, at, stream)
+    cu_new, cu_p = _out_ptr(cu_new, "cu_new", i32, (R + 1,), lens, at, stream)
+    slots, slots_p = _out_ptr(slots, "slots", torch.int64, (T,), lens, at, stream)
+    taken, taken_p = _out_ptr(taken, "taken", i32, (1,), lens, at, stream)
     _call("pair_pages_extend", lens, stream, R, int(page_size), width, *ins, F, count, T, table,
           kv_p, held_p, cu_p, slots_p, taken_p, _err_ptr(dev_err, lens, at))
     return kv_len, held_out, cu_new, slots, taken
@@ -580,11 +590,11 @@ def pair_attend_paged(q, k_cache, v_cache, block_table, kv_len, cu_new, scale=No
     table = _ptr(block_table, "block_table", i32, (R, width), q, at)
     lens = _ptr(kv_len, "kv_len", i32, (R,), q, at)
     cu = _ptr(cu_new, "cu_new", i32, (R + 1,), q, at)
-    out, out_p = _out_ptr(out, "out", q.dtype, (T, Hq, D), q, at)
-    lse, lse_p = _out_ptr(lse, "lse", torch.float32, (T, Hq), q, at)
+    out, out_p = _out_ptr(out, "out", q.dtype, (T, Hq, D), q, at, stream)
+    lse, lse_p = _out_ptr(lse, "lse", torch.float32, (T, Hq), q, at, stream)
     if ws is None:
         need = pair_attend_workspace_size(R, Hq, shape[2], D, dt)
-        ws = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        ws = _fresh((max(need, 256),), torch.uint8, q, stream)
     n = ws.numel()
     _call("pair_attend_paged", q, stream, T, R, Hq, shape[2], D, dt, qp, q.stride(0), q.stride(1),
           kc, ks, vc, vs, shape[0], shape[1], table, width, lens, cu,
@@ -608,9 +618,9 @@ def pair_verify_drafts(p, ids, cu_new, u, u_draw, q=None, out_ids=None, logp=Non
     ids_p = _ptr(ids, "ids", i32, (T,), p, at)
     cu = _ptr(cu_new, "cu_new", i32, (R + 1,), p, at)
     up, dp = _ptr(u, "u", f32, (T,), p, at), _ptr(u_draw, "u_draw", f32, (R,), p, at)
-    out_ids, out_p = _out_ptr(out_ids, "out_ids", i32, (T,), p, at)
-    logp, logp_p = _out_ptr(logp, "logp", f32, (T,), p, at)
-    n_emit, n_p = _out_ptr(n_emit, "n_emit", i32, (R,), p, at)
+    out_ids, out_p = _out_ptr(out_ids, "out_ids", i32, (T,), p, at, stream)
+    logp, logp_p = _out_ptr(logp, "logp", f32, (T,), p, at, stream)
+    n_emit, n_p = _out_ptr(n_emit, "n_emit", i32, (R,), p, at, stream)
     _call("pair_verify_drafts", p, stream, T, R, V, dt, pp, p.stride(0), qp, q_row, ids_p, cu, up,
           dp, out_p, logp_p, n_p, _err_ptr(dev_err, p, at))
     return out_ids, logp, n_emit

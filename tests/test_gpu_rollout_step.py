@@ -118,3 +118,37 @@ def test_step_in_a_graph():
         wv = rollout.verify_drafts(p.cpu().numpy(), ids.cpu().numpy(), want["cu"], u.cpu().numpy(),
                                    ud.cpu().numpy())
         assert np.array_equal(oid, wv["ids"]) and np.array_equal(emit, wv["n"])
+
+
+def test_outputs_and_workspace_belong_to_the_given_stream():
+    """With stream=, what a call makes is of that stream's memory: work that is
+    still to run on the current stream, in memory freed there, does not reach
+    it."""
+    from paper_2608_11368_gb300 import binding as B
+    dev = dict(device="cuda")
+    i32 = dict(dtype=torch.int32, **dev)
+    lens, n_new = torch.tensor([40, 41], **i32), torch.tensor([2, 2], **i32)
+    held, cu = torch.tensor([3, 3], **i32), torch.tensor([0, 2, 4], **i32)
+    table = torch.arange(6, **i32).view(2, 3)
+    free, count = torch.arange(6, 10, **i32), torch.tensor([4], **i32)
+    k = torch.randn(6, 16, 2, 64, **dev).bfloat16()
+    q = torch.randn(4, 4, 64, **dev).bfloat16()
+    p = torch.softmax(torch.randn(4, 500, **dev), 1)
+    ids, u, ud = torch.zeros(4, **i32), torch.rand(4, **dev), torch.rand(2, **dev)
+    kv = lens + n_new
+    calls = (lambda **s: B.pair_pages_extend(lens, held, n_new, free, count, table, 16, 4, **s),
+             lambda **s: B.pair_attend_paged(q, k, k, table, kv, cu, **s),
+             lambda **s: B.pair_verify_drafts(p, ids, cu, u, ud, **s))
+    s = torch.cuda.Stream()
+    for call in calls:
+        want = [x.clone() for x in call()]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        later = [torch.full_like(x, 77) for x in want]  # runs after the sleep
+        del later
+        got = call(stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+    need = B.pair_attend_workspace_size(2, 4, 2, 64, B.PAIR_BF16)
+    assert any(x["stream"] == s.cuda_stream and x["total_size"] >= need
+               for x in torch.cuda.memory_snapshot())
