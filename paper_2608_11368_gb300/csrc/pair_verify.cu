@@ -278,6 +278,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = a.C, rank = blockIdx.x % C, cluster = blockIdx.x / C;
   const bool control = warp == kVerifyWarps;
+  cluster_arrive();
   if (blockIdx.x == gridDim.x - 1) {  // rows that no request owns
     const int t0 = max(0, a.cu[a.R]);
     for (int64_t t = t0 + tid; t < a.T_rows; t += kVerifyThreads) {
@@ -290,6 +291,9 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
     if (lane == 0) s_dec[0] = d;
   }
   __syncthreads();
+  // Every CTA of the cluster runs before its shared memory is written to. (They
+  // arrive at their start, so the first decision's loads cover the wait.)
+  cluster_wait();
   int round = 0;  // of the exchange, alternating between two buffers
   for (int i = cluster, it = 0; i < a.R; i += a.clusters, ++it) {
     const Decision d = s_dec[it & 1];
@@ -338,6 +342,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
           const uint32_t to = mapa(smem_u32(&s_cta[buf][rank]), lane);
           asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(x) : "memory");
         }
+        __syncwarp();  // the barrier wants whole warps
       }
       cluster_sync();
       long long total = 0, before = 0;

@@ -316,6 +316,14 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
                "barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Its two halves, by every thread of converged warps: what lies between them
+// overlaps the wait.
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // Arrive once on the mbarrier at the same shared offset in every cluster CTA
 // of `mask` when all previously issued MMAs of this thread have completed.
 __device__ __forceinline__ void mma_commit_multicast(uint64_t *bar, uint16_t mask) {
