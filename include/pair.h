@@ -550,8 +550,10 @@ typedef struct {
  *      with a negative length or more tokens than its pages hold, one whose
  *      pages run out (of the list or of its table row), or a chunk that does
  *      not fit in T. Such a request gets no pages, its slots are -1 and its
- *      kv_len is len (0 if negative); the others are served. cu_new counts a
- *      negative n_new as 0 and stops at T.
+ *      kv_len is len (0 if negative); the others are served. Pages are given in
+ *      the requests' order: behind one whose pages run out of the list, a
+ *      request that needs pages gets none either, and one that needs none is
+ *      served. cu_new counts a negative n_new as 0 and stops at T.
  * Deterministic. One launch, no workspace.
  */
 PAIR_API pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t table_width,

@@ -21,7 +21,7 @@ def pages_extend(lens, held, n_new, free_pages, free_count, table, page, T):
         bad = (lens[i] < 0 or held[i] < 0 or n_new[i] < 0 or held[i] > width
                or held[i] * page < lens[i] or total > width)
         need = 0 if bad else max(total - int(held[i]), 0)
-        ok = not bad and used + need <= avail and row + n <= T
+        ok = not bad and (need == 0 or used + need <= avail) and row + n <= T
         error |= not ok
         kv_len[i] = lens[i] + n if ok else max(int(lens[i]), 0)
         held_out[i] = held[i] + (need if ok else 0)

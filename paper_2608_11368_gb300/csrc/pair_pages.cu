@@ -44,6 +44,14 @@ __device__ __forceinline__ Need request_need(const ExtendArgs &a, int i) {
   return r;
 }
 
+// Whether a request is served, given the sums of tokens and of pages before it. The
+// sum of pages counts requests that are not served too, so behind one whose pages
+// run out nobody is given any; who needs none is served all the same.
+__device__ __forceinline__ bool served(const ExtendArgs &a, const Need &r, int64_t row,
+                                       int64_t before, int32_t avail) {
+  return !r.bad && (r.pages == 0 || before + r.pages <= avail) && row + r.n <= a.T;
+}
+
 // The prefix sums of tokens and of pages over all requests are formed by
 // every block for itself (12 bytes per request, from L2 after the first), a run
 // of consecutive requests per thread, so one launch does. A block writes the
@@ -137,7 +145,7 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
         before += r.pages;
         r = request_need(a, ++i);
       }
-      if (!r.bad && before + r.pages <= avail && row + r.n <= a.T) {
+      if (served(a, r, row, before, avail)) {
         const uint32_t pos = r.len + (uint32_t)(t - row);
         const uint32_t at = pos / (uint32_t)a.page;
         const uint32_t off = pos - at * (uint32_t)a.page;
@@ -162,7 +170,7 @@ __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs
     if (blockIdx.x != 0 && (i1 <= r0 || i >= r1)) break;
     const bool mine = i >= r0 && i < r1;
     const Need r = request_need(a, i);
-    const bool ok = !r.bad && xp + r.pages <= avail && xn + r.n <= a.T;
+    const bool ok = served(a, r, xn, xp, avail);
     if (ok && r.pages) top = (int32_t)(xp + r.pages);
     if (mine) {
       a.kv_len[i] = ok ? r.len + r.n : max(r.len, 0);
