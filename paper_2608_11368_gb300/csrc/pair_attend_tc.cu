@@ -49,6 +49,14 @@ struct Maps {
   int box;                  // tokens of a box
 };
 
+// wait() by all lanes of a warp, which leave it together: a lane's poll can succeed
+// before another's, and the TMEM instructions (.aligned) want whole warps.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t phase, volatile int *abort,
+                                          int32_t *dev_err) {
+  const bool ok = wait(bar, phase, abort, dev_err);
+  return __all_sync(0xffffffffu, ok);
+}
+
 // A warp's arrival, for what its lanes have done (and fenced) before.
 __device__ __forceinline__ void warp_arrive(uint64_t *bar) {
   __syncwarp();
@@ -195,7 +203,7 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
         ++at;
       }
       if (mine && key < end) id = row[at];
-      if (!(ok = wait(&empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
+      if (!(ok = warp_wait(&empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
       uint64_t *bar = &full[ring.stage];
       const int n = __popc(__ballot_sync(0xffffffffu, load));
       if (lane == 0) mbar_expect_tx(bar, n * box * D * 2);
@@ -229,14 +237,17 @@ __device__ void produce(const Args &a, const Maps &maps, Smem<D> &sm, Walk<M, BN
 }
 
 // Waits, each lane of the first `n` for a barrier and phase of its own: one poll
-// of several costs a warp as much as one.
-__device__ __forceinline__ bool wait_lanes(int n, uint64_t *bar, uint32_t phase,
+// of several costs a warp as much as one. `ok`: what the lane's waits since the
+// last vote came to.
+__device__ __forceinline__ bool wait_lanes(int n, bool ok, uint64_t *bar, uint32_t phase,
                                            volatile int *abort, int32_t *dev_err) {
-  bool ok = true;
-  if ((int)(threadIdx.x & 31) < n) ok = wait(bar, phase, abort, dev_err);
+  if ((int)(threadIdx.x & 31) < n) ok &= wait(bar, phase, abort, dev_err);
   return __all_sync(0xffffffffu, ok);
 }
 
+// The warp votes on its waits once per step, in the first (a vote behind each of
+// them: 20 us of 374 for the four chunks); until then all lanes go the same way, and
+// products issued after a wait that gave up are of a call that has failed.
 template <int D>
 __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   using C = Tc<D>;
@@ -282,15 +293,15 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   while (ok && walk.next(a, &s)) {
     if (s.t0 == s.t1) continue;
     const int top = s.rows > 128;  // the last active tile
-    if (!(ok = wait(&sm.k_full[kr.stage], kr.phase, abort, a.dev_err))) break;
-    for (int w = 0; w <= top && ok; ++w) {
-      if (!(ok = wait(&sm.q_full[w], q_ph[w], abort, a.dev_err))) break;
+    ok &= wait(&sm.k_full[kr.stage], kr.phase, abort, a.dev_err);
+    for (int w = 0; w <= top; ++w) {
+      ok &= wait(&sm.q_full[w], q_ph[w], abort, a.dev_err);
       q_ph[w] ^= 1;
       tc_fence_after();
       scores(w, kr.stage, w == top);
     }
     kr.step();
-    for (int t = s.t0; t < s.t1 && ok; ++t) {
+    for (int t = s.t0; t < s.t1; ++t) {
       const bool more = t + 1 < s.t1;
       // Before the first products of a tile: weights, values, the next keys.
       const int lane = threadIdx.x & 31;
@@ -298,14 +309,14 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
                       : lane == 1 ? &sm.looked[vr.stage]
                                   : &sm.k_full[kr.stage];
       const uint32_t phase = lane == 0 ? p_ph[0] : lane == 1 ? vr.phase : kr.phase;
-      if (!(ok = wait_lanes(more ? 3 : 2, bar, phase, abort, a.dev_err))) break;
+      if (!(ok = wait_lanes(more ? 3 : 2, ok, bar, phase, abort, a.dev_err))) break;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (w > top) break;
-        if (w && !(ok = wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err))) break;
+        if (w) ok &= wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err);
         tc_fence_after();
         sums(w, vr.stage, 0, t == s.t0, false);
-        if (!(ok = wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err))) break;
+        ok &= wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err);
         p_ph[w] ^= 1;
         tc_fence_after();
         sums(w, vr.stage, 1, false, w == top);
@@ -316,11 +327,13 @@ __device__ void issue(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
       vr.step();
       if (more) kr.step();
     }
+    ok = __all_sync(0xffffffffu, ok);
   }
   if (elect_one()) mma_commit(&sm.done);
   __syncwarp();
   volatile int never = 0;
   wait(&sm.done, 0, &never, a.dev_err);
+  __syncwarp();
 }
 
 // Of every tile: waits for the values, and in an edge tile makes those of keys
@@ -335,8 +348,8 @@ __device__ void look_over(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
   Segment s;
   while (walk.next(a, &s)) {
     for (int t = s.t0; t < s.t1; ++t) {
-      if (!wait(&sm.v_full[ring.stage], ring.phase, abort, a.dev_err)) return;
-      if (edge_tile(s, t)) {
+      const bool ok = wait(&sm.v_full[ring.stage], ring.phase, abort, a.dev_err);
+      if (ok && edge_tile(s, t)) {
         const int from = max(0, s.least - t * BN), nk = min(BN, s.keys - t * BN);
         for (int atom = 0; atom < C::kAtoms; ++atom) {
           uint4 *base = reinterpret_cast<uint4 *>(sm.v[ring.stage] + atom * C::kAtom);
@@ -367,11 +380,17 @@ __device__ void look_over(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
         fence_async_smem();
       }
       warp_arrive(&sm.looked[ring.stage]);
+      if (!__all_sync(0xffffffffu, ok)) return;  // off the products' path
       ring.step();
     }
   }
 }
 
+// The lanes of a warp go through a segment together: TMEM is read and written by
+// whole warps. A wait that gave up is therefore noticed at the segment's end; until
+// then the warp goes on over scores of a call that has failed, its further waits
+// returning at once. (A vote behind each tile's wait: 346 us instead of 342 for four
+// chunks of 1025 to 2048 tokens.)
 template <int D>
 __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
   using C = Tc<D>;
@@ -417,7 +436,8 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
       for (int t = s.t0; t < s.t1; ++t) {
         const bool edge = edge_tile(s, t);
         const int key0 = t * BN;
-        if (!(ok = wait(&sm.s_full[w], s_ph, abort, a.dev_err))) break;
+        wait(&sm.s_full[w], s_ph, abort, a.dev_err);
+        __syncwarp();
         s_ph ^= 1;
         tc_fence_after();
         uint32_t x[4][32];
@@ -428,12 +448,9 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
         if (edge) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const int upto = seen - key0 - c * 32;
-            if (upto < 32) {
+            const int upto = seen - key0 - c * 32;  // by selects: rows end at different keys
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (k >= upto) x[c][k] = 0xff800000u;  // -inf
-            }
+            for (int k = 0; k < 32; ++k) x[c][k] = k >= upto ? 0xff800000u : x[c][k];  // -inf
           }
         }
         float mx4[4] = {m, m, m, m};
@@ -453,7 +470,8 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
           const float fix = ex2_approx(mx == -INFINITY ? 0.f : (m - mx) * scale);
           m = mx;
           l *= fix;
-          if (!(ok = wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
+          wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err);
+          __syncwarp();
           tc_fence_after();
 #pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
@@ -491,7 +509,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
-      if (!ok) break;
+      if (!(ok = !__any_sync(0xffffffffu, *abort))) break;
     }
     // All scores of this segment have been read, so its queries have: the next
     // segment's go in their place, and its first scores are formed while this
@@ -499,7 +517,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
     more = walk.next(a, &ahead);
     if (more) put_query(ahead);
     if (active && s.t0 < s.t1) {
-      if (!(ok = wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
+      if (!(ok = warp_wait(&sm.pv_done[w], pv_ph ^ 1, abort, a.dev_err))) break;
       tc_fence_after();
     }
     const bool whole = s.whole();
@@ -520,8 +538,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
 #pragma unroll
         for (int k = 0; k < 32; ++k) o[k] = 0.f;
       }
-      if (!mine) continue;
-      if (bad) {
+      if (mine && bad) {
 #pragma unroll
         for (int k = 0; k < 32; k += 8) {
           float v[8];
@@ -532,7 +549,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
           for (int e = 0; e < 8; ++e) o[k + e] = v[e];
         }
       }
-      if (whole) {
+      if (mine && whole) {
         __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(a.out) + (at.token * a.Hq + at.head) * D +
                             c * 32;
 #pragma unroll
@@ -551,7 +568,7 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
             *reinterpret_cast<uint4 *>(to + k + 8) = make_uint4(u[4], u[5], u[6], u[7]);
           }
         }
-      } else {
+      } else if (mine) {
 #pragma unroll
         for (int k = 0; k < 32; k += 8) {
           uint32_t u[8];
@@ -560,13 +577,13 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
           store32(part + 2 * M + r * D + c * 32 + k, u);
         }
       }
+      __syncwarp();  // rows in use and others, before the warp's next TMEM load
     }
     tc_fence_before();
-    if (!mine) continue;
-    if (!whole) {
+    if (mine && !whole) {
       part[r] = m2;
       part[M + r] = l;
-    } else if (a.lse) {
+    } else if (mine && a.lse) {
       a.lse[at.token * a.Hq + at.head] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
     }
   }
@@ -618,6 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefetch_tmap(&maps.k);
     prefetch_tmap(&maps.v);
   }
+  __syncwarp();
   if (warp == 9) tmem_alloc(&sm.tmem, 512);
   const Walk<M, BN> walk{find_share<kThreads>(a, M, cta, ctas, sm.scratch)};
   tc_fence_before();
@@ -637,6 +655,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     softmax<D>(a, sm, walk, cta);
   }
+  __syncwarp();
   let_next_start();
   tc_fence_before();
   __syncthreads();
