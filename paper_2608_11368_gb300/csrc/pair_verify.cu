@@ -381,11 +381,15 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
   }
 }
 
-// Clusters of C CTAs that fit on the device at once (cached per type and C).
+// Clusters of C CTAs that fit on device `dev`, the current one, at once (cached per
+// type, device and C). The attribute that allows large ones is the device's too: it
+// is set before an entry of that device is there.
 template <typename T>
-int resident_clusters(int C) {
-  static std::atomic<int> known[kVerifyMaxCluster + 1];
-  int n = known[C].load(std::memory_order_relaxed);
+int resident_clusters(int dev, int C) {
+  constexpr int kMaxDev = 128;
+  static std::atomic<int> known[kMaxDev][kVerifyMaxCluster + 1];
+  const bool cached = dev >= 0 && dev < kMaxDev;
+  int n = cached ? known[dev][C].load(std::memory_order_acquire) : 0;
   if (n > 0) return n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(C * 64, 1, 1);
@@ -402,7 +406,7 @@ int resident_clusters(int C) {
     cudaGetLastError();
     return 0;
   }
-  known[C].store(n, std::memory_order_relaxed);
+  if (cached) known[dev][C].store(n, std::memory_order_release);
   return n;
 }
 
@@ -412,10 +416,11 @@ pair_status launch_verify(VerifyArgs<T> a, cudaStream_t s) {
   // of a row's reading), rounds = requests / clusters that fit. A large C leaves
   // the fewest SMs without work in the last round, and brings a single
   // request's row in from many SMs; short rows are not worth many CTAs.
-  int best = 0, clusters = 0;
+  int best = 0, clusters = 0, dev = 0;
   double least = 0;
+  PAIR_CUDA_TRY(cudaGetDevice(&dev));
   for (int C = 1; C <= kVerifyMaxCluster && (C == 1 || C * kVerifyLeast <= a.V); C *= 2) {
-    const int n = resident_clusters<T>(C);
+    const int n = resident_clusters<T>(dev, C);
     if (n < 1) continue;
     const double t = (double)ceil_div(a.R, n) * (1.0 / C + 3000.0 / a.V);
     if (best == 0 || t < least) {
