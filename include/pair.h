@@ -646,7 +646,8 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  * In:  p [T][V], q [T][V] (dt; row strides p_row, q_row in elements; a
  *      chunk's last row of q is not read); q may be null: drafts that were
  *      looked up, q(y) = 1 at the draft and 0 elsewhere. ids [T], cu_new [R+1]
- *      int32; u [T], u_draw [R] float32 in [0, 1). V <= 2^22.
+ *      int32 (cu_new[0] may be above 0: some requests of a larger step); u [T],
+ *      u_draw [R] float32 in [0, 1). V <= 2^22.
  * Out: out_ids [T] int32: at row cu_new[i] + j the j-th emitted token, -1
  *      behind the last one and at rows no request owns; logp [T] float32
  *      (nullable): log p of that token under its row of p, 0 where out_ids is
@@ -656,8 +657,8 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  * Errors: PAIR_ERR_INVALID_ARG; device PAIR_DEV_ERR_TARGET_RANGE: a draft
  *      outside [0, V) (rejected, the draw is from p - q, from p without q);
  *      PAIR_DEV_ERR_PROBABILITY: all weights of p are 0 (the token is -1 and
- *      not counted); PAIR_DEV_ERR_PAGES: offsets that decrease or pass T (the
- *      request is left out).
+ *      not counted); PAIR_DEV_ERR_PAGES: offsets that are negative, decrease or
+ *      pass T (that request's n_emit is 0, and all rows are unspecified).
  * No output may overlap an input. Deterministic. One launch, no workspace.
  */
 PAIR_API pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_dtype dt,

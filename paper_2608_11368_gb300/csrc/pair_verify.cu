@@ -280,11 +280,14 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyArgs<T> a)
   const bool control = warp == kVerifyWarps;
   cluster_arrive();
   if (blockIdx.x == gridDim.x - 1) {  // rows that no request owns
-    const int t0 = max(0, a.cu[a.R]);
-    for (int64_t t = t0 + tid; t < a.T_rows; t += kVerifyThreads) {
-      a.out_ids[t] = -1;
-      if (a.logp) a.logp[t] = 0.f;
-    }
+    const auto clear = [&](int64_t t0, int64_t t1) {
+      for (int64_t t = t0 + tid; t < t1; t += kVerifyThreads) {
+        a.out_ids[t] = -1;
+        if (a.logp) a.logp[t] = 0.f;
+      }
+    };
+    clear(0, min((int64_t)a.cu[0], a.T_rows));
+    clear(max(0, a.cu[a.R]), a.T_rows);
   }
   if (control) {
     const Decision d = decide(a, cluster);

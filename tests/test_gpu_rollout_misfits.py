@@ -72,3 +72,27 @@ def test_extend_many_requests_after_pages_ran_out():
     pos = lens[:, None] + np.arange(n)
     want = np.take_along_axis(table, np.minimum(pos // page, 3), 1) * page + pos % page
     assert np.array_equal(slots.cpu(), np.where(ok[:, None], want, -1).ravel())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("first", [1, 5, 700])
+def test_verify_rows_before_the_first_request(first, dtype):
+    """Offsets that begin behind row 0 (some requests of a larger step): the rows
+    before belong to nobody and say so, the requests are served."""
+    from paper_2608_11368_gb300 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(first)
+    R, n, V = 6, 3, 500
+    T = first + R * n + 2
+    p = torch.softmax(3 * torch.randn((T, V), generator=g, device="cuda"), -1).to(dtype)
+    q = torch.softmax(3 * torch.randn((T, V), generator=g, device="cuda"), -1).to(dtype)
+    ids = torch.randint(0, V, (T,), generator=g, device="cuda").to(torch.int32)
+    u, ud = torch.rand(T, generator=g, device="cuda"), torch.rand(R, generator=g, device="cuda")
+    cu = i32(first + n * np.arange(R + 1))
+    err = i32([0])
+    out, logp = i32([77] * T), torch.full((T,), 77.0, device="cuda")
+    B.pair_verify_drafts(p, ids, cu, u, ud, q=q, out_ids=out, logp=logp, dev_err=err)
+    assert B.pair_status_sync(err) == 0
+    want = B.pair_verify_drafts(p[first:], ids[first:].contiguous(), cu - first,
+                                u[first:].contiguous(), ud, q=q[first:])
+    assert (out[:first] == -1).all() and (logp[:first] == 0).all()
+    assert torch.equal(out[first:], want[0]) and torch.equal(logp[first:], want[1])
