@@ -98,10 +98,11 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
     J = (torch.rand((prompts, G), generator=g, device="cuda") < pi).to(torch.uint8)
     go = J.view(R).to(torch.int32)
 
-    # Prompts: a group's rollouts share the pages that the prompt fills, written
-    # by its first one; the rest of the prompt is each rollout's own chunk.
+    # Prompts without their last token, which the first step takes: a group's
+    # rollouts share the pages that they fill, written by its first one; the rest of
+    # the prompt is each rollout's own chunk.
     prompt = torch.randint(0, V, (prompts, prompt_len), generator=g, device="cuda")
-    full = prompt_len // page * page
+    full = (prompt_len - 1) // page * page
     first = torch.zeros(R, dtype=torch.int32, device="cuda")
     first[::G] = full
     if full:
