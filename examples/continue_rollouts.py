@@ -124,7 +124,7 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
     ids_all = torch.full((R, steps * n + 1), -1, dtype=torch.int32, device="cuda")
     ids_all[:, 0] = last
     made = torch.zeros(R, dtype=torch.int64, device="cuda")
-    logp_old = torch.zeros(R, device="cuda")
+    logp_all = torch.zeros((R, steps * n + 1), device="cuda")
     lane = torch.arange(n, device="cuda")
     for _ in range(steps):
         # Drafts, one after the other, from the drafter's probabilities.
@@ -147,8 +147,8 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
         new = lane < emit[:, None]
         where = torch.where(new, made[:, None] + 1 + lane, 0)
         ids_all.scatter_(1, where, torch.where(new, out, ids_all[:, :1]))
+        logp_all.scatter_(1, where, torch.where(new, logp, 0.0))
         made += emit
-        logp_old += logp.sum(1)
         cache.lens = cache.lens + emit
         last = torch.where(emit > 0, out.gather(1, (emit.long() - 1).clamp_min(0)[:, None])[:, 0],
                            last)
@@ -165,6 +165,8 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
     T = int(cu_seq[-1])
     ids = torch.cat([s[:-1] for s in seq])
     y = torch.cat([s[1:] for s in seq]).contiguous()
+    logp_tokens = torch.cat([logp_all[i, 1:len(s)] for i, s in enumerate(seq)])
+    logp_old = logp_all.sum(1)
     q, _, _ = policy.qkv(ids)
     hidden, _ = B.pair_attend_paged(q, cache.k, cache.v, cache.table, cache.lens, cu_seq,
                                     max_new=int(made.max()), dev_err=err)
@@ -174,8 +176,9 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
         a.reshape(-1).contiguous(), logp_old, dev_err=err)
     status = B.pair_status_sync(err)
     return dict(status=status, J=J, made=made, start=start, lens=cache.lens, logp_old=logp_old,
-                logp_seq=logp_seq, a=a.reshape(-1), coef=coef, Jobj=Jobj, dH=dH, dW=dW,
-                hidden=hidden, y=y, cu=cu_seq, head=policy.head, steps=steps, drafts=drafts)
+                logp_tokens=logp_tokens, logp_seq=logp_seq, a=a.reshape(-1), coef=coef, Jobj=Jobj,
+                dH=dH, dW=dW, hidden=hidden, y=y, cu=cu_seq, head=policy.head, steps=steps,
+                drafts=drafts)
 
 
 if __name__ == "__main__":
