@@ -523,7 +523,9 @@ PAIR_API pair_status pair_grad_noalloc(int64_t T, int32_t d, int32_t V,
  * page * page_size + p % page_size (int64). Requests may share pages (a
  * group's rollouts their prompt's). Keys and values are two arrays with
  * strides of their own, in elements: for_page, for_token, for_head; the head
- * dimension is contiguous. Every order of the three is accepted.
+ * dimension is contiguous. Every order of the three is accepted. A stride over
+ * a single entry (one row, head, page or token of a page) is not looked at, in
+ * the caches as in the step's arrays.
  */
 typedef struct {
   int64_t for_page, for_token, for_head;

@@ -461,6 +461,11 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
       T * (Hq / Hkv) > INT32_MAX)
     return PAIR_ERR_INVALID_ARG;
   const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
+  // A stride over a single entry says nothing; a tensor map wants one all the same.
+  const auto over = [](int64_t stride, int64_t entries) { return entries > 1 ? stride : 256; };
+  q_row = over(q_row, T), q_head = over(q_head, Hq);
+  for (pair_cache_strides *x : {&ks, &vs})
+    *x = {over(x->for_page, num_pages), over(x->for_token, page_size), over(x->for_head, Hkv)};
   const int64_t strides[] = {q_row, q_head, ks.for_page, ks.for_token, ks.for_head, vs.for_page,
                              vs.for_token, vs.for_head};
   for (const int64_t x : strides)

@@ -292,10 +292,13 @@ pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt, 
       !v || !slots || num_pages < 1 || page_size < 1 || !k_cache || !v_cache)
     return PAIR_ERR_INVALID_ARG;
   const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
-  const int64_t strides[] = {k_row, k_head, v_row, v_head, ks.for_page, ks.for_token,
-                             ks.for_head, vs.for_page, vs.for_token, vs.for_head};
-  for (const int64_t x : strides)
-    if (x % per != 0) return PAIR_ERR_INVALID_ARG;
+  // A stride over a single entry says nothing.
+  const int64_t strides[][2] = {{k_row, T}, {v_row, T}, {k_head, Hkv}, {v_head, Hkv},
+                                {ks.for_page, num_pages}, {vs.for_page, num_pages},
+                                {ks.for_token, page_size}, {vs.for_token, page_size},
+                                {ks.for_head, Hkv}, {vs.for_head, Hkv}};
+  for (const auto &x : strides)
+    if (x[1] > 1 && x[0] % per != 0) return PAIR_ERR_INVALID_ARG;
   if (D % per != 0 || (int64_t)Hkv * D > INT32_MAX || !aligned16(k) || !aligned16(v) ||
       !aligned16(k_cache) || !aligned16(v_cache))
     return PAIR_ERR_INVALID_ARG;

@@ -470,7 +470,7 @@ extern "C" pair_status pair_verify_drafts(int64_t T, int32_t R, int32_t V, pair_
   reset_launches();
   if (T < 1 || T > INT32_MAX || R < 1 || R > (1 << 27) || V < 1 || V > (1 << 22) ||
       (dt != PAIR_F32 && dt != PAIR_BF16) || !p || !ids || !cu_new || !u || !u_draw ||
-      !out_ids || !n_emit || p_row < V || (q && q_row < V))
+      !out_ids || !n_emit || (T > 1 && (p_row < V || (q && q_row < V))))
     return PAIR_ERR_INVALID_ARG;
   const pair_status dv = check_device();
   if (dv != PAIR_OK) return dv;
