@@ -537,7 +537,8 @@ typedef struct {
  * max(0, ceil(kv_i / page_size) - held_i) new pages; requests take them from
  * the free list in their order, and they follow the held ones in the
  * request's table row.
- * In:  R >= 1 requests; page_size >= 1; table_width = columns of block_table;
+ * In:  R >= 1 requests (2^30 at most); page_size >= 1; table_width = columns of
+ *      block_table;
  *      len [R] tokens cached, held [R] pages held (at least ceil(len /
  *      page_size): rejected drafts leave a request with more), n_new [R] new
  *      tokens, each >= 0; free_pages [free_capacity] page ids and free_count
@@ -594,8 +595,8 @@ PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_d
  *     out = sum_k exp(s_k - lse) value_k.
  * A row that sees no key (kv_len - n + j < 0) and a row that no request owns
  * get out = 0, lse = -inf.
- * In:  q [T][Hq][D] (dt) with element strides q_row, q_head; Hq a multiple of
- *      Hkv (query head h reads key head h / (Hq / Hkv)); D 64, 128 or 256;
+ * In:  R up to 2^30; q [T][Hq][D] (dt) with element strides q_row, q_head; Hq a
+ *      multiple of Hkv (query head h reads key head h / (Hq / Hkv)); D 64, 128 or 256;
  *      block_table [R][table_width] int32, kv_len [R], cu_new [R+1] int32
  *      (cu_new[0] = 0) on the device. Strides and base pointers are multiples
  *      of 16 bytes. max_new: the longest chunk if the host knows it, else 0; it

@@ -454,7 +454,7 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                               int32_t max_new, void *out, float *lse, void *ws,
                               size_t ws_bytes, int32_t *dev_err, pair_stream_t stream) {
   reset_launches();
-  if (T < 1 || T > INT32_MAX || R < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || !q || !k_cache ||
+  if (T < 1 || T > INT32_MAX || R < 1 || R > kMaxRequests || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || !q || !k_cache ||
       !v_cache || num_pages < 1 || page_size < 1 || !block_table || table_width < 1 || !kv_len ||
       !cu_new || !out || !(fabsf(scale) <= 3.0e38f) || max_new < 0 ||
       (dt != PAIR_F32 && dt != PAIR_BF16) ||

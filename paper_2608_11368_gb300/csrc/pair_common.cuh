@@ -15,6 +15,10 @@ constexpr int kMaxPairs = 256;  // 2-CTA clusters of a persistent grid, at most
 constexpr int kOneHotBucket = 16;  // vocabulary rows per bucket of the one-hot dW part
 constexpr size_t kRingBytesPerCluster = 8 * 2 * 32768;
 
+// Requests of a generation step at most: indexes of a run of requests, rounded up to
+// whole runs, stay within 32 bits.
+constexpr int kMaxRequests = 1 << 30;
+
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Launch bookkeeping (per host thread): counts the kernels of the current

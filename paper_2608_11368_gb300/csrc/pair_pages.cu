@@ -261,7 +261,7 @@ pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t table_width,
                               int64_t *slots, int32_t *taken, int32_t *dev_err,
                               pair_stream_t stream) {
   reset_launches();
-  if (R < 1 || page_size < 1 || table_width < 1 || T < 1 || T > INT32_MAX ||
+  if (R < 1 || R > kMaxRequests || page_size < 1 || table_width < 1 || T < 1 || T > INT32_MAX ||
       free_capacity < 0 || !len || !held || !n_new || (!free_pages && free_capacity > 0) ||
       !free_count || !block_table || !kv_len || !held_out || !cu_new || !slots || !taken)
     return PAIR_ERR_INVALID_ARG;
