@@ -577,7 +577,8 @@ PAIR_API pair_status pair_pages_extend(int32_t R, int32_t page_size, int32_t tab
  * Out: k_cache, v_cache (strides ks, vs).
  * Errors: PAIR_ERR_INVALID_ARG; device PAIR_DEV_ERR_PAGES: a slot below -1 or
  *      from num_pages * page_size on (that row is left out). Two rows with the
- *      same slot leave one of them there, which one is not defined.
+ *      same slot leave 16-byte pieces of either there, which ones is not
+ *      defined.
  */
 PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt,
                                        const void *k, int64_t k_row, int64_t k_head,
@@ -600,12 +601,14 @@ PAIR_API pair_status pair_cache_append(int64_t T, int32_t Hkv, int32_t D, pair_d
  *      block_table [R][table_width] int32, kv_len [R], cu_new [R+1] int32
  *      (cu_new[0] = 0) on the device. Strides and base pointers are multiples
  *      of 16 bytes. max_new: the longest chunk if the host knows it, else 0; it
- *      leaves out launches that no chunk needs and changes no result (a longer
- *      chunk than it says is computed all the same, more slowly).
+ *      leaves out launches that no chunk needs (a longer chunk than it says is
+ *      computed all the same, more slowly). Another kernel may then form a
+ *      row, so with another max_new results agree up to the arithmetic's
+ *      rounding.
  * Out: out [T][Hq][D] (dt), lse [T][Hq] float32 (nullable).
  * Arithmetic: scores, softmax statistics and output sums in fp32. PAIR_BF16:
- *      the weights exp(s - max) go to the tensor cores in bf16, and out is
- *      rounded once. PAIR_F32: CUDA cores, fp32 throughout. Keys from kv_len
+ *      the weights exp(s - max) go to the tensor cores in bf16 (off by up to
+ *      2^-8 of themselves), and out is rounded once. PAIR_F32: CUDA cores, fp32 throughout. Keys from kv_len
  *      on are never used, whatever their pages hold, and a key that a row does
  *      not see has no part in it, NaN and infinity included.
  * Workspace: pair_attend_workspace_size bytes, 256-byte aligned, any contents.
@@ -645,7 +648,10 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  * fp32; NaN counts as 0, more than 1 as 1), C_v = w_0 + .. + w_v, the lowest
  * v with C_v > floor(u_draw[i] * C_{V-1}) (an fp64 product, at most
  * C_{V-1} - 1). The sums are integers, so the token depends on no order. If
- * every weight of the difference is 0, p alone is drawn from.
+ * every weight of the difference is 0, p alone is drawn from. The weights
+ * resolve 2^-40, but u and u_draw are fp32: numbers in steps of 2^-24, as
+ * generators commonly give them, move a token's chance in steps of 2^-24, and
+ * a token with a smaller one may never be drawn.
  * In:  p [T][V], q [T][V] (dt; row strides p_row, q_row in elements; a
  *      chunk's last row of q is not read); q may be null: drafts that were
  *      looked up, q(y) = 1 at the draft and 0 elsewhere. ids [T], cu_new [R+1]

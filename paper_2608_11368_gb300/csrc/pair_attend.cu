@@ -35,8 +35,8 @@ struct SimtSmem {
 // thread forms the scores of one key with its group's rows (the queries are
 // broadcast reads), then the output sums of its columns for 16 rows (8 at D =
 // 64), four keys at a time; rows that are not in use are left out. Bound by
-// latency at small sizes (four barriers and two exchanges per tile; 32 requests
-// of up to 640 keys, heads of 64: 21 us with the joining pass), else by
+// latency at small sizes (three barriers and two exchanges per tile; 32 requests
+// of up to 640 keys, heads of 64: 22 us with the joining pass), else by
 // shared-memory reads.
 template <int D>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {

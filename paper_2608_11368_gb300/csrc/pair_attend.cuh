@@ -36,9 +36,11 @@ constexpr int kFewTile = 64;     // rows of a unit of the kernel for few rows
 constexpr int kFewRows = 32;
 constexpr float kLn2 = 0.69314718055994531f;
 // A unit's fixed cost, in keys: what a CTA spends between two units and on
-// starting its tiles. 64 chunks of 32 to 256 tokens behind 100 to 3000 keys
-// (many rows): 474 us at 48 keys, 361 at 400, 322 at 800, 337 at 1600; 16 x 16
-// requests with drafts (few rows): 422 at 48, 404 at 128, 398 at 192.
+// starting its tiles. Measured on 32/8 heads of 128: 64 chunks of 32 to 256 tokens
+// behind 100 to 3000 keys (many rows): 474 us at 48 keys, 361 at 400, 322 at 800,
+// 337 at 1600; 16 x 16 requests with drafts (few rows): 422 at 48, 404 at 128, 398 at
+// 192. Heads of 64 and 256 go by the same values; the 48 of fp32's units of 16 rows
+// was not swept.
 __host__ __device__ constexpr int unit_cost(int M) {
   return M == kManyRows ? 800 : M == kFewTile ? 192 : 48;
 }

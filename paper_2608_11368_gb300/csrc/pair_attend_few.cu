@@ -5,6 +5,12 @@
 // the copy's rate (6.8 TB/s). mma.sync rather than tcgen05: a tile of 128 rows
 // would be 16 to 32 rows full, and its chain of products and softmax takes as
 // long as the bytes of a tile.
+//
+// The softmax weights enter the second product in bf16, as its operands are: each
+// is off by up to 2^-8 of itself, independently, while their sum takes them
+// unrounded in fp32. Against 64 bits a row of 700 keys is off by 1.7e-3 of its size,
+// of which the output's one rounding to bf16 is 1.6e-3; weights of 16 more bits
+// would take a second product per tile.
 #include "pair_attend.cuh"
 
 namespace pairk {

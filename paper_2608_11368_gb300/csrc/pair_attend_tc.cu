@@ -594,8 +594,12 @@ __device__ void softmax(const Args &a, Smem<D> &sm, Walk<M, BN> walk, int cta) {
 // TMEM, the weights back into TMEM in the place of the scores (bf16, the A
 // operand of the second product), O_w += P_w V in TMEM throughout. Keys and
 // values come by TMA, one box per page piece, into the layout the products
-// read. Four chunks of 1025 to 2048 tokens behind 1000 to 6144 (32/8 heads of
-// 128): 378 us, 1.38 PFLOP/s, the tensor pipe 63 % active. Bound by shared
+// read. The weights' rounding to bf16 (each off by up to 2^-8 of itself; their sums
+// stay in fp32, unrounded) adds to the output's: 2.3e-3 of its size against 64 bits,
+// 1.7e-3 if only the output were rounded; weights of 16 more bits would take the
+// second product twice, in the pipe that binds. Four chunks of 1025 to 2048 tokens
+// behind 1000 to 6144 (32/8 heads of 128, 0.52 TFLOP as the mean of two sets of
+// lengths): 397 us, 1.32 PFLOP/s, the tensor pipe 60 % active. Bound by shared
 // memory's reads (a product Q K^T of 64 cycles reads 8 KB at 128 bytes a cycle,
 // beside TMA's writes) and by the step's chain: products, scores out of TMEM,
 // maximum, exponentials, weights into TMEM.

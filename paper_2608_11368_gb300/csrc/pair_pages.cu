@@ -60,7 +60,7 @@ __device__ __forceinline__ bool served(const ExtendArgs &a, const Need &r, int64
 // read from the old table entries or from the free list, never from entries this
 // launch writes. Bound by latency: loads of the lengths, one block scan, the
 // bisection, two dependent loads, stores. 64 requests of one token take 4 us with
-// the launch, 4096 of one 9, 4096 of 128 on average 11.4 (a list of requests per
+// the launch, 4096 of one 9, 4096 of 128 on average 11.6 (a list of requests per
 // block and a warp to each: 38; a bisection per token: 18).
 template <int kPerLane>
 __global__ void __launch_bounds__(kExtendThreads) pages_extend_kernel(ExtendArgs a) {
@@ -207,7 +207,7 @@ constexpr int kAppendAhead = 4;  // 16-byte pieces of keys and of values in flig
 
 // A warp moves a token's keys and values; its slot is taken apart once. Bound by
 // HBM: every byte is read and written once (8192 tokens of 8 heads of 128 bf16:
-// 12.1 us, 5.5 TB/s; a thread per 16-byte piece, dividing for itself, 14.1).
+// 12.7 us, 5.3 TB/s; a thread per 16-byte piece, dividing for itself, 14.1).
 __global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(AppendArgs a) {
   const int lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);

@@ -265,8 +265,8 @@ __device__ Decision decide(const VerifyArgs<T> &a, int i) {
 // dependent loads) while the others read, writes the accepted tokens, and,
 // where the draw falls into its CTA, goes over that warp's segment again while
 // the others are at the next request. Bound by HBM: one row of p, and of q where
-// a draft was refused, per request. 256 rows of 151,936 of both in fp32: 58 us,
-// 4.7 TB/s (with every warp doing everything, a request per cluster, 84). Not
+// a draft was refused, per request. 256 rows of 151,936 of both in fp32: 59 us,
+// 4.6 TB/s (with every warp doing everything, a request per cluster, 84). Not
 // faster: 2, 3 or 8 vectors per lane in flight, vectors through shared memory, a
 // fourth CTA per SM, reading warps a request ahead of the exchange (60 to 120 us);
 // the clusters' last round, which is not full, costs as much as a full one.
