@@ -83,6 +83,9 @@ typedef enum {
 
 typedef enum { PAIR_F32 = 0, PAIR_BF16 = 1 } pair_dtype;
 
+/* Codes of a paged cache in 8 bits (pair_cache_q8). */
+typedef enum { PAIR_CACHE_I8 = 0, PAIR_CACHE_E4M3 = 1 } pair_cache_format;
+
 /* Bits of the device error word written by the kernels. */
 #define PAIR_DEV_ERR_NONPOSITIVE_INCLUSION 1
 #define PAIR_DEV_ERR_TARGET_RANGE 2
@@ -634,6 +637,86 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
                                        const int32_t *cu_new, float scale, int32_t max_new,
                                        void *out, float *lse, void *ws, size_t ws_bytes,
                                        int32_t *dev_err, pair_stream_t stream);
+
+/*
+ * The cache in 8 bits. Keys and values may be held as codes of 8 bits with one
+ * exponent byte per token and head, in pages as above; the calls are then
+ *     pair_cache_append_q8, pair_attend_paged_q8
+ * in the place of those without the suffix, and
+ *     pair_cache_read_q8  for the stored values of given slots.
+ * A row of D codes c with the exponent byte b holds the values c 2^(b - 127):
+ *     PAIR_CACHE_I8    whole numbers from -127 to 127 (int8),
+ *     PAIR_CACHE_E4M3  floating-point numbers of 4 exponent and 3 significand
+ *                      bits, up to 448 (for rows whose entries differ by
+ *                      orders of magnitude: each is off by 2^-4 of itself at
+ *                      most, where whole numbers are off by up to 2^-7 of the
+ *                      row's largest).
+ * b is the least byte with which the row's largest entry does not round beyond
+ * the largest code, and every code is its entry's nearest (halves to even), so
+ * codes do not depend on the device. b = 255: the row had a NaN or an infinity;
+ * it holds NaN. The scales are powers of two: a stored value is a bf16 number.
+ */
+typedef struct {
+  void *codes;                 /* int8 or e4m3, strides in elements (bytes) */
+  pair_cache_strides codes_at; /* multiples of 16, codes 16-byte aligned    */
+  uint8_t *exps;               /* one per page, token and head              */
+  pair_cache_strides exps_at;  /* any                                       */
+} pair_cache_q8;
+
+/*
+ * pair_cache_append_q8 -- pair_cache_append into caches in 8 bits.
+ * In:  dt type of k and v; D a multiple of 16 from 16 to 256; otherwise as for
+ *      pair_cache_append, strides of k and v in elements of dt.
+ * Out: codes and exponent bytes of k_cache, v_cache (fmt) at the slots.
+ * Errors: as for pair_cache_append (strides of codes: multiples of 16). Two
+ *      rows with the same slot leave pieces of either there, which ones is not
+ *      defined.
+ * Deterministic. One launch, no workspace.
+ */
+PAIR_API pair_status pair_cache_append_q8(int64_t T, int32_t Hkv, int32_t D, pair_dtype dt,
+                                          const void *k, int64_t k_row, int64_t k_head,
+                                          const void *v, int64_t v_row, int64_t v_head,
+                                          const int64_t *slots, int32_t num_pages,
+                                          int32_t page_size, pair_cache_format fmt,
+                                          pair_cache_q8 k_cache, pair_cache_q8 v_cache,
+                                          int32_t *dev_err, pair_stream_t stream);
+
+/*
+ * pair_cache_read_q8 -- the stored keys and values of T slots.
+ * In:  slots [T] int64, in any order, the same one any number of times; caches
+ *      as for pair_cache_append_q8.
+ * Out: k, v [T][Hkv][D] (dt) with strides as for pair_cache_append, 16-byte
+ *      aligned; rows with slot -1 get zeros. Exact in fp32 and in bf16, but for
+ *      values below bf16's normal numbers, which are rounded to nearest.
+ * Errors: as for pair_cache_append; a row with a slot that does not exist gets
+ *      zeros. No output may overlap an input or the other output.
+ * Deterministic. One launch, no workspace.
+ */
+PAIR_API pair_status pair_cache_read_q8(int64_t T, int32_t Hkv, int32_t D, const int64_t *slots,
+                                        int32_t num_pages, int32_t page_size,
+                                        pair_cache_format fmt, pair_cache_q8 k_cache,
+                                        pair_cache_q8 v_cache, pair_dtype dt, void *k,
+                                        int64_t k_row, int64_t k_head, void *v, int64_t v_row,
+                                        int64_t v_head, int32_t *dev_err, pair_stream_t stream);
+
+/*
+ * pair_attend_paged_q8 -- pair_attend_paged over caches in 8 bits: the same
+ * sums over the stored values, in the same arithmetic (the values are exact in
+ * it), with the same conventions, workspace (pair_attend_workspace_size for dt)
+ * and errors. dt is the type of q and out; no stride is asked of the exponent
+ * bytes. A row that holds NaN counts like a NaN: with a row that sees it, and
+ * with no other.
+ */
+PAIR_API pair_status pair_attend_paged_q8(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                          pair_dtype dt, const void *q, int64_t q_row,
+                                          int64_t q_head, pair_cache_format fmt,
+                                          pair_cache_q8 k_cache, pair_cache_q8 v_cache,
+                                          int32_t num_pages, int32_t page_size,
+                                          const int32_t *block_table, int32_t table_width,
+                                          const int32_t *kv_len, const int32_t *cu_new,
+                                          float scale, int32_t max_new, void *out, float *lse,
+                                          void *ws, size_t ws_bytes, int32_t *dev_err,
+                                          pair_stream_t stream);
 
 /*
  * pair_verify_drafts -- verification of drafted tokens against the target's

@@ -128,3 +128,29 @@ def verify_drafts(p, ids, cu, u, u_draw, q=None):
                 n_emit[i] += 1
             break
     return dict(ids=out, logp=logp, n=n_emit, bad_id=bad_id, bad_p=bad_p)
+
+
+def store_q8(x, fmt):
+    """Rows x [.., D] as they are held in 8 bits: (codes, exponent bytes), the
+    codes as the numbers they are ("i8" whole numbers, "e4m3" values of that
+    type). The exponent is looked for from below, one at a time."""
+    x = np.asarray(x, np.float64)
+    top = np.abs(x).max(-1)
+    bad = ~np.isfinite(top)
+    limit = 127.5 if fmt == "i8" else 464.0  # what is below rounds to 127, to 448
+    b = np.zeros(top.shape, np.int64)
+    for _ in range(255):
+        b += (b < 254) & (np.where(bad, 0.0, top) * 2.0 ** (127 - b) >= limit)
+    y = np.where(bad[..., None], 0.0, x) * 2.0 ** (127 - b)[..., None]
+    if fmt == "i8":
+        c = np.rint(y)
+    else:  # four significant bits down to 2^-6, steps of 2^-9 below
+        step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(y), 2.0 ** -6))) - 3)
+        c = np.rint(y / step) * step
+    return c, np.where(bad, 255, b)
+
+
+def values_q8(codes, exps):
+    """What codes and exponent bytes stand for."""
+    s = np.where(np.asarray(exps) == 255, np.nan, 2.0 ** (np.asarray(exps, np.float64) - 127))
+    return np.asarray(codes, np.float64) * s[..., None]

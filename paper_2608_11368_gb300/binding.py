@@ -21,6 +21,7 @@ HEADER = os.path.join(os.path.dirname(_PKG), "include", "pair.h")
 
 PAIR_OK = 0
 PAIR_F32, PAIR_BF16 = 0, 1
+PAIR_CACHE_I8, PAIR_CACHE_E4M3 = 0, 1
 PAIR_CENTER = 1
 PAIR_STANDARDIZE = 2
 STATUS_NAMES = {0: "PAIR_OK", 1: "PAIR_ERR_INVALID_ARG", 2: "PAIR_ERR_UNSUPPORTED",
@@ -42,6 +43,12 @@ class CacheStrides(ctypes.Structure):
     """pair_cache_strides (include/pair.h), in elements."""
     _fields_ = [("for_page", ctypes.c_int64), ("for_token", ctypes.c_int64),
                 ("for_head", ctypes.c_int64)]
+
+
+class CacheQ8(ctypes.Structure):
+    """pair_cache_q8 (include/pair.h)."""
+    _fields_ = [("codes", ctypes.c_void_p), ("codes_at", CacheStrides),
+                ("exps", ctypes.c_void_p), ("exps_at", CacheStrides)]
 
 
 _lib = None
@@ -110,6 +117,16 @@ def lib() -> ctypes.CDLL:
                                     CacheStrides, P, CacheStrides, I32, I32, P, I32, P, P, F32,
                                     I32, P, P, P, SZ, P, P]
     L.pair_attend_paged.restype = ctypes.c_int
+    L.pair_cache_append_q8.argtypes = [I64, I32, I32, ctypes.c_int, P, I64, I64, P, I64, I64, P,
+                                       I32, I32, ctypes.c_int, CacheQ8, CacheQ8, P, P]
+    L.pair_cache_append_q8.restype = ctypes.c_int
+    L.pair_cache_read_q8.argtypes = [I64, I32, I32, P, I32, I32, ctypes.c_int, CacheQ8, CacheQ8,
+                                     ctypes.c_int, P, I64, I64, P, I64, I64, P, P]
+    L.pair_cache_read_q8.restype = ctypes.c_int
+    L.pair_attend_paged_q8.argtypes = [I64, I32, I32, I32, I32, ctypes.c_int, P, I64, I64,
+                                       ctypes.c_int, CacheQ8, CacheQ8, I32, I32, P, I32, P, P,
+                                       F32, I32, P, P, P, SZ, P, P]
+    L.pair_attend_paged_q8.restype = ctypes.c_int
     L.pair_verify_drafts.argtypes = [I64, I32, I32, ctypes.c_int, P, I64, P, I64, P, P, P, P, P,
                                      P, P, P, P]
     L.pair_verify_drafts.restype = ctypes.c_int
@@ -526,6 +543,34 @@ def _cache(k_cache, v_cache, like, at):
     return (k, CacheStrides(*k_cache.stride()[:3]), v, CacheStrides(*v_cache.stride()[:3]), shape)
 
 
+_FORMATS = {torch.int8: PAIR_CACHE_I8, torch.float8_e4m3fn: PAIR_CACHE_E4M3}
+
+
+def _cache_q8(k_codes, k_exps, v_codes, v_exps, like, at):
+    """Format, both caches in 8 bits, their shape."""
+    if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
+        raise ValueError("k_codes must be [num_pages, page_size, Hkv, D]")
+    shape, dtype = k_codes.shape, k_codes.dtype
+    if dtype not in _FORMATS:
+        raise TypeError("k_codes must be int8 or float8_e4m3fn, got %s" % dtype)
+    both = []
+    for name, codes, exps in (("k", k_codes, k_exps), ("v", v_codes, v_exps)):
+        p = _strided(codes, name + "_codes", dtype, shape, like, at)
+        if not (type(exps) is torch.Tensor and exps.dtype is torch.uint8
+                and exps.shape == shape[:3] and exps.get_device() == at):
+            if not isinstance(exps, torch.Tensor) or not exps.is_cuda:
+                raise TypeError("%s_exps must be a CUDA tensor" % name)
+            if exps.dtype is not torch.uint8:
+                raise TypeError("%s_exps must be torch.uint8, got %s" % (name, exps.dtype))
+            if exps.shape != shape[:3]:
+                raise ValueError("%s_exps must have shape %s, got %s"
+                                 % (name, tuple(shape[:3]), tuple(exps.shape)))
+            _same_device(like, name + "_exps", exps)
+        both.append(CacheQ8(p, CacheStrides(*codes.stride()[:3]), exps.data_ptr(),
+                            CacheStrides(*exps.stride())))
+    return (_FORMATS[dtype], *both, shape)
+
+
 def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, page_size, T,
                       kv_len=None, held_out=None, cu_new=None, slots=None, taken=None,
                       dev_err=None, stream=None):
@@ -569,6 +614,47 @@ def pair_cache_append(k, v, slots, k_cache, v_cache, dev_err=None, stream=None):
     return k_cache, v_cache
 
 
+def pair_cache_append_q8(k, v, slots, k_codes, k_exps, v_codes, v_exps, dev_err=None, stream=None):
+    """Keys and values k, v [T, Hkv, D] into their slots [T] (int64, -1: left
+    out) of caches in 8 bits (see pair.h): codes [num_pages, page_size, Hkv, D]
+    int8 or float8_e4m3fn, exponent bytes [num_pages, page_size, Hkv] uint8. k, v
+    and the caches may be views with other strides. Returns the four arrays."""
+    T, H, D = k.shape
+    dt, at = _pair_dtype(k, "k"), _index(k, "k")
+    kp, vp = (_strided(k, "k", k.dtype, (T, H, D), k, at),
+              _strided(v, "v", k.dtype, (T, H, D), k, at))
+    slots_p = _ptr(slots, "slots", torch.int64, (T,), k, at)
+    fmt, kc, vc, shape = _cache_q8(k_codes, k_exps, v_codes, v_exps, k, at)
+    if shape[2] != H or shape[3] != D:
+        raise ValueError("k_codes must have %d heads of %d, got %s" % (H, D, tuple(shape)))
+    _call("pair_cache_append_q8", k, stream, T, H, D, dt, kp, k.stride(0), k.stride(1), vp,
+          v.stride(0), v.stride(1), slots_p, shape[0], shape[1], fmt, kc, vc,
+          _err_ptr(dev_err, k, at))
+    return k_codes, k_exps, v_codes, v_exps
+
+
+def pair_cache_read_q8(slots, k_codes, k_exps, v_codes, v_exps, dtype=torch.bfloat16, k=None,
+                       v=None, dev_err=None, stream=None):
+    """Stored keys and values of the given slots [T] (int64, -1: zeros) of caches
+    in 8 bits (see pair.h), in `dtype` (float32 or bfloat16) or into k, v [T,
+    Hkv, D] (views with other strides too). Returns (k, v)."""
+    at, T = _index(slots, "slots"), slots.numel()
+    slots_p = _ptr(slots, "slots", torch.int64, (T,), slots, at)
+    fmt, kc, vc, (pages, page, H, D) = _cache_q8(k_codes, k_exps, v_codes, v_exps, slots, at)
+    given = k if k is not None else v
+    dtype = dtype if given is None else given.dtype
+    outs = []
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            t = _fresh((T, H, D), dtype, slots, stream)
+        outs += [t, _strided(t, name, dtype, (T, H, D), slots, at)]
+    k, kp, v, vp = outs
+    _call("pair_cache_read_q8", slots, stream, T, H, D, slots_p, pages, page, fmt, kc, vc,
+          _pair_dtype(k, "k"), kp, k.stride(0), k.stride(1), vp, v.stride(0), v.stride(1),
+          _err_ptr(dev_err, slots, at))
+    return k, v
+
+
 def pair_attend_workspace_size(R, Hq, Hkv, D, dtype) -> int:
     return int(lib().pair_attend_workspace_size(int(R), int(Hq), int(Hkv), int(D), int(dtype)))
 
@@ -598,6 +684,36 @@ def pair_attend_paged(q, k_cache, v_cache, block_table, kv_len, cu_new, scale=No
     n = ws.numel()
     _call("pair_attend_paged", q, stream, T, R, Hq, shape[2], D, dt, qp, q.stride(0), q.stride(1),
           kc, ks, vc, vs, shape[0], shape[1], table, width, lens, cu,
+          D ** -0.5 if scale is None else float(scale), int(max_new), out_p, lse_p,
+          _ptr(ws, "ws", torch.uint8, (n,), q, at), n, _err_ptr(dev_err, q, at))
+    return out, lse
+
+
+def pair_attend_paged_q8(q, k_codes, k_exps, v_codes, v_exps, block_table, kv_len, cu_new,
+                         scale=None, max_new=0, out=None, lse=None, ws=None, dev_err=None,
+                         stream=None):
+    """pair_attend_paged over caches in 8 bits (see pair.h): codes [num_pages,
+    page_size, Hkv, D] int8 or float8_e4m3fn, exponent bytes [num_pages,
+    page_size, Hkv] uint8 (views with other strides too). Returns (out [T, Hq, D],
+    lse [T, Hq] float32)."""
+    T, Hq, D = q.shape
+    dt, at, i32 = _pair_dtype(q, "q"), _index(q, "q"), torch.int32
+    qp = _strided(q, "q", q.dtype, (T, Hq, D), q, at)
+    fmt, kc, vc, shape = _cache_q8(k_codes, k_exps, v_codes, v_exps, q, at)
+    if shape[3] != D:
+        raise ValueError("k_codes must have heads of %d, got %s" % (D, tuple(shape)))
+    R, width = block_table.shape
+    table = _ptr(block_table, "block_table", i32, (R, width), q, at)
+    lens = _ptr(kv_len, "kv_len", i32, (R,), q, at)
+    cu = _ptr(cu_new, "cu_new", i32, (R + 1,), q, at)
+    out, out_p = _out_ptr(out, "out", q.dtype, (T, Hq, D), q, at, stream)
+    lse, lse_p = _out_ptr(lse, "lse", torch.float32, (T, Hq), q, at, stream)
+    if ws is None:
+        need = pair_attend_workspace_size(R, Hq, shape[2], D, dt)
+        ws = _fresh((max(need, 256),), torch.uint8, q, stream)
+    n = ws.numel()
+    _call("pair_attend_paged_q8", q, stream, T, R, Hq, shape[2], D, dt, qp, q.stride(0),
+          q.stride(1), fmt, kc, vc, shape[0], shape[1], table, width, lens, cu,
           D ** -0.5 if scale is None else float(scale), int(max_new), out_p, lse_p,
           _ptr(ws, "ws", torch.uint8, (n,), q, at), n, _err_ptr(dev_err, q, at))
     return out, lse

@@ -1,8 +1,9 @@
-// pair_attend_paged: entry point, the fp32 kernel on the CUDA cores, and the
-// pass that joins partial sums.
+// pair_attend_paged and pair_attend_paged_q8: entry points, the fp32 kernel on the
+// CUDA cores, and the pass that joins partial sums.
 #include <math.h>
 
 #include "pair_attend.cuh"
+#include "pair_cache_q8.cuh"
 
 namespace pairk {
 namespace attend {
@@ -16,18 +17,32 @@ __device__ __forceinline__ void from_float(__nv_bfloat16 *o, float x) {
   *o = __float2bfloat16_rn(x);
 }
 
-template <int D>
+__device__ __forceinline__ float4 load_query(const float *q) {
+  return *reinterpret_cast<const float4 *>(q);
+}
+__device__ __forceinline__ float4 load_query(const __nv_bfloat16 *q) {
+  const uint2 u = *reinterpret_cast<const uint2 *>(q);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
+                     __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+}
+
+// F: the cache's codes, or q8::kPlain for one in fp32.
+template <int D, int F>
 struct SimtSmem {
+  static constexpr bool kHeld = F != q8::kPlain;
   static constexpr int kKeys = D == 64 ? 64 : 32;
   static constexpr int kStages = 3;
-  float k[kStages][kKeys][D + 4];
-  float v[kStages][kKeys][D];
+  using E = std::conditional_t<kHeld, uint8_t, float>;  // an entry of the cache
+  static constexpr int kPer = 16 / sizeof(E);           // of them in 16 bytes
+  E k[kStages][kKeys][D + kPer];
+  E v[kStages][kKeys][D];
   float q[kSimtRows][D];
   float p[kSimtRows][kKeys];
   float m[kSimtRows], l[kSimtRows], fix[kSimtRows];
   int64_t row[2][2][kKeys];  // offsets of a tile's keys and values
   int seen[kSimtRows];
   int64_t scratch[kSimtThreads / 32 + 2];
+  float e[kHeld ? kStages : 1][2][kHeld ? kKeys : 1];  // scales of a tile's rows
 };
 
 // fp32 products on the CUDA cores, 16 rows against tiles of keys and values
@@ -38,12 +53,17 @@ struct SimtSmem {
 // latency at small sizes (three barriers and two exchanges per tile; 32 requests
 // of up to 640 keys, heads of 64: 22 us with the joining pass), else by
 // shared-memory reads.
-template <int D>
+//
+// Over a cache in 8 bits the tiles hold the codes, which become fp32 where they are
+// read; a key's scale multiplies its scores, a value's its weights.
+template <typename T, int D, int F>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   extern __shared__ __align__(16) uint8_t raw[];
-  using S = SimtSmem<D>;
+  using S = SimtSmem<D, F>;
+  using E = typename S::E;
   S &sm = *reinterpret_cast<S *>(raw);
   constexpr int M = kSimtRows, BN = S::kKeys, NST = S::kStages, V4 = D / 4;
+  constexpr int PER = S::kPer, VE = D / PER;  // entries of 16 bytes; such pieces of a row
   constexpr int QR = M * BN / kSimtThreads;                      // rows of a thread's scores
   constexpr int QG = M / QR;                                     // groups of them
   constexpr int CPT = D >= kSimtThreads ? D / kSimtThreads : 1;  // columns per thread
@@ -52,11 +72,11 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cta = blockIdx.x, ctas = gridDim.x;
   clear_notes(a, cta);
-  clear_spare_rows<float, D, kSimtThreads>(a, cta, ctas);
+  clear_spare_rows<T, D, kSimtThreads>(a, cta, ctas);
   if (cta == ctas - 1) report_requests(a);
   Walk<M, BN> walk{find_share<kSimtThreads>(a, M, cta, ctas, sm.scratch)};
-  const float *q = static_cast<const float *>(a.q);
-  const float *kc = static_cast<const float *>(a.kc), *vc = static_cast<const float *>(a.vc);
+  const T *q = static_cast<const T *>(a.q);
+  const E *kc = static_cast<const E *>(a.kc), *vc = static_cast<const E *>(a.vc);
   const float scale = a.scale * kLog2e;
   const int col = tid % (kSimtThreads / RG), rg = tid / (kSimtThreads / RG);
   Segment s;
@@ -71,14 +91,19 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         const int id = key < s.keys ? page_of(a, s.i, key, &off) : -1;
         sm.row[t & 1][0][tid] = id < 0 ? -1 : cache_row(a, a.ks, id, off, s.h);
         sm.row[t & 1][1][tid] = id < 0 ? -1 : cache_row(a, a.vs, id, off, s.h);
+        if constexpr (S::kHeld) {
+          float *e = sm.e[(t - s.t0) % NST][0] + tid;
+          e[0] = id < 0 ? 0.f : q8::scale_of(a.ke[cache_row(a, a.kes, id, off, s.h)]);
+          e[BN] = id < 0 ? 0.f : q8::scale_of(a.ve[cache_row(a, a.ves, id, off, s.h)]);
+        }
       }
     };
     auto fetch = [&](int t) {
       if (t < s.t1) {
         const int st = (t - s.t0) % NST;
 #pragma unroll 4
-        for (int x = tid; x < BN * V4; x += kSimtThreads) {
-          const int k = x / V4, c = x % V4 * 4;
+        for (int x = tid; x < BN * VE; x += kSimtThreads) {
+          const int k = x / VE, c = x % VE * PER;
           const int64_t ko = sm.row[t & 1][0][k], vo = sm.row[t & 1][1][k];
           cp_async16(tc::smem_u32(&sm.k[st][k][c]), kc + (ko < 0 ? 0 : ko + c), ko >= 0);
           cp_async16(tc::smem_u32(&sm.v[st][k][c]), vc + (vo < 0 ? 0 : vo + c), vo >= 0);
@@ -93,7 +118,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < s.rows) {
         const RowAt at = row_at(a, s.row0, s.r0, s.h, r);
-        u = *reinterpret_cast<const float4 *>(q + at.token * a.q_row + at.head * a.q_head + c);
+        u = load_query(q + at.token * a.q_row + at.head * a.q_head + c);
       }
       *reinterpret_cast<float4 *>(&sm.q[r][c]) = u;
     }
@@ -121,15 +146,32 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       {
         const int k = tid % BN, g0 = tid / BN;  // rows g0, g0 + QG, ..
         float acc[QR] = {};
-#pragma unroll 4
-        for (int d = 0; d < D; d += 4) {
-          const float4 x = *reinterpret_cast<const float4 *>(&sm.k[st][k][d]);
+        auto add = [&](const float4 &x, int d) {
 #pragma unroll
           for (int r = 0; r < QR; ++r) {
             if (r * QG >= s.rows) break;
             const float4 y = *reinterpret_cast<const float4 *>(&sm.q[r * QG + g0][d]);
             acc[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc[r]))));
           }
+        };
+        if constexpr (S::kHeld) {
+#pragma unroll 1
+          for (int d = 0; d < D; d += 16) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(&sm.k[st][k][d]);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              float x[4];
+              q8::decode4<F>(w[c], x);
+              add(make_float4(x[0], x[1], x[2], x[3]), d + c * 4);
+            }
+          }
+          const float e = sm.e[st][0][k];
+#pragma unroll
+          for (int r = 0; r < QR; ++r) acc[r] *= e;
+        } else {
+#pragma unroll 4
+          for (int d = 0; d < D; d += 4) add(*reinterpret_cast<const float4 *>(&sm.k[st][k][d]), d);
         }
 #pragma unroll
         for (int r = 0; r < QR; ++r)
@@ -162,6 +204,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         for (int x = 0; x < BN / 32; ++x) {
           sc[r][x] = exp2f(sc[r][x] - ref);
           sum[r] += sc[r][x];
+          if constexpr (S::kHeld) sc[r][x] *= sm.e[st][1][lane + 32 * x];
           sm.p[warp * (M / 4) + r][lane + 32 * x] = sc[r][x];
         }
       }
@@ -193,7 +236,10 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
-          for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[st][k + y][col + c * kSimtThreads];
+          for (int c = 0; c < CPT; ++c) {
+            const E x = sm.v[st][k + y][col + c * kSimtThreads];
+            if constexpr (S::kHeld) v[y][c] = q8::decode1<F>(x); else v[y][c] = x;
+          }
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
           if (r * RG >= s.rows) break;
@@ -218,9 +264,9 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         if (rr >= s.rows) continue;
         const RowAt at = row_at(a, s.row0, s.r0, s.h, rr);
         const float l = sm.l[rr], inv = l == 0.f ? 0.f : 1.f / l;
-        float *out = static_cast<float *>(a.out) + (at.token * a.Hq + at.head) * D;
+        T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D;
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) out[col + c * kSimtThreads] = o[r][c] * inv;
+        for (int c = 0; c < CPT; ++c) from_float(out + col + c * kSimtThreads, o[r][c] * inv);
         if (col == 0 && a.lse)
           a.lse[at.token * a.Hq + at.head] =
               l == 0.f ? -INFINITY : (sm.m[rr] + log2f(l)) * kLn2;
@@ -345,16 +391,17 @@ __global__ void __launch_bounds__(kJoinThreads)
   }
 }
 
-template <int D>
+template <typename T, int D, int F>
 pair_status run_simt(Launch *l, cudaStream_t s) {
   const Args &a = l->a;
-  constexpr int smem = sizeof(SimtSmem<D>);
+  constexpr int smem = sizeof(SimtSmem<D, F>);
   static_assert(smem <= 232448, "shared memory of a CTA");
-  PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<D>,
+  const auto kernel = attend_simt_kernel<T, D, F>;
+  PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const int ctas = useful_ctas(a, kSimtRows, min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count()));
-  PAIR_BEGIN("attend_simt", s);
-  attend_simt_kernel<D><<<ctas, kSimtThreads, smem, s>>>(a);
+  PAIR_BEGIN(F == q8::kPlain ? "attend_simt" : "attend_simt_q8", s);
+  kernel<<<ctas, kSimtThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
   l->M = kSimtRows;
   l->ctas = ctas;
@@ -418,8 +465,16 @@ int sm_count() {
   return n;
 }
 
-pair_status launch_simt(Launch *l, int D, cudaStream_t s) {
-  return by_size(D, [&](auto d) { return run_simt<decltype(d)::value>(l, s); });
+pair_status launch_simt(Launch *l, int D, int fmt, pair_dtype dt, cudaStream_t s) {
+  return by_size(D, [&](auto d) {
+    constexpr int n = decltype(d)::value;
+    if (dt == PAIR_BF16)
+      return fmt == q8::kI8 ? run_simt<__nv_bfloat16, n, q8::kI8>(l, s)
+                            : run_simt<__nv_bfloat16, n, q8::kE4M3>(l, s);
+    return fmt == q8::kPlain ? run_simt<float, n, q8::kPlain>(l, s)
+           : fmt == q8::kI8  ? run_simt<float, n, q8::kI8>(l, s)
+                             : run_simt<float, n, q8::kE4M3>(l, s);
+  });
 }
 
 static pair_status launch_join(const Launch &l0, const Launch &l1, int D, pair_dtype dt,
@@ -428,6 +483,91 @@ static pair_status launch_join(const Launch &l0, const Launch &l1, int D, pair_d
     return dt == PAIR_BF16 ? run_join<__nv_bfloat16, decltype(d)::value>(l0, l1, s)
                            : run_join<float, decltype(d)::value>(l0, l1, s);
   });
+}
+
+// A call of either entry point. fmt q8::kPlain: caches in the type of q.
+static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                pair_dtype dt, const void *q, int64_t q_row, int64_t q_head,
+                                int fmt, const pair_cache_q8 &k, const pair_cache_q8 &v,
+                                int32_t num_pages, int32_t page_size, const int32_t *block_table,
+                                int32_t table_width, const int32_t *kv_len, const int32_t *cu_new,
+                                float scale, int32_t max_new, void *out, float *lse, void *ws,
+                                size_t ws_bytes, int32_t *dev_err, pair_stream_t stream) {
+  reset_launches();
+  const bool held = fmt != q8::kPlain;
+  if (T < 1 || T > INT32_MAX || R < 1 || R > kMaxRequests || Hkv < 1 || Hq < Hkv ||
+      Hq % Hkv != 0 || !q || !k.codes || !v.codes || (held && (!k.exps || !v.exps)) || num_pages < 1 || page_size < 1 ||
+      !block_table || table_width < 1 || !kv_len || !cu_new || !out || !(fabsf(scale) <= 3.0e38f) ||
+      max_new < 0 || (dt != PAIR_F32 && dt != PAIR_BF16) || T * (Hq / Hkv) > INT32_MAX)
+    return PAIR_ERR_INVALID_ARG;
+  const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
+  // A stride over a single entry says nothing; a tensor map wants one all the same.
+  const auto over = [](int64_t stride, int64_t entries) { return entries > 1 ? stride : 256; };
+  const auto all_over = [&](const pair_cache_strides &x) {
+    return pair_cache_strides{over(x.for_page, num_pages), over(x.for_token, page_size),
+                              over(x.for_head, Hkv)};
+  };
+  q_row = over(q_row, T), q_head = over(q_head, Hq);
+  const pair_cache_strides ks = all_over(k.codes_at), vs = all_over(v.codes_at);
+  if (q_row % per != 0 || q_head % per != 0) return PAIR_ERR_INVALID_ARG;
+  for (const pair_cache_strides *x : {&ks, &vs})
+    for (const int64_t y : {x->for_page, x->for_token, x->for_head})
+      if (y % (held ? 16 : per) != 0) return PAIR_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(k.codes, 16) || !aligned(v.codes, 16) || !aligned(out, 16))
+    return PAIR_ERR_INVALID_ARG;
+  const size_t need = pair_attend_workspace_size(R, Hq, Hkv, D, dt);
+  if (need == 0) return PAIR_ERR_UNSUPPORTED;
+  if (!ws || ws_bytes < need || !aligned(ws, 256)) return PAIR_ERR_WORKSPACE;
+  const pair_status dv = check_device();
+  if (dv != PAIR_OK) return dv;
+  const Args a{T,
+               R,
+               Hq,
+               Hkv,
+               Hq / Hkv,
+               -1,
+               INT32_MAX,
+               q,
+               q_row,
+               q_head,
+               k.codes,
+               v.codes,
+               ks,
+               vs,
+               num_pages,
+               page_size,
+               block_table,
+               table_width,
+               kv_len,
+               cu_new,
+               scale,
+               out,
+               lse,
+               static_cast<Desc *>(ws),
+               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + kNotes + kManyNotes),
+               dev_err,
+               k.exps,
+               v.exps,
+               k.exps_at,
+               v.exps_at};
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  Launch few{a, 0, 0}, many{a, 0, 0};
+  many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + kNotes);
+  many.a.part += few_floats(D);
+  // Which kernel a chunk goes to is decided by its rows, on the device; a
+  // launch is left out where the host knows that no chunk can be its.
+  const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
+  const bool simt = dt == PAIR_F32 || held;
+  const bool only_few = simt || most_rows <= kFewRows || !many_applies(a, D);
+  if (!only_few && R > 1) {
+    few.a.rows_upto = kFewRows;
+    many.a.rows_over = kFewRows;
+  }
+  pair_status st = PAIR_OK;
+  if (simt) st = launch_simt(&few, D, fmt, dt, s);
+  else if (only_few || R > 1) st = launch_few(&few, D, s);
+  if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
+  return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;
 }
 
 }  // namespace attend
@@ -453,73 +593,28 @@ pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int
                               const int32_t *kv_len, const int32_t *cu_new, float scale,
                               int32_t max_new, void *out, float *lse, void *ws,
                               size_t ws_bytes, int32_t *dev_err, pair_stream_t stream) {
-  reset_launches();
-  if (T < 1 || T > INT32_MAX || R < 1 || R > kMaxRequests || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || !q || !k_cache ||
-      !v_cache || num_pages < 1 || page_size < 1 || !block_table || table_width < 1 || !kv_len ||
-      !cu_new || !out || !(fabsf(scale) <= 3.0e38f) || max_new < 0 ||
-      (dt != PAIR_F32 && dt != PAIR_BF16) ||
-      T * (Hq / Hkv) > INT32_MAX)
+  return attend_paged(T, R, Hq, Hkv, D, dt, q, q_row, q_head, q8::kPlain,
+                      {const_cast<void *>(k_cache), ks, nullptr, {}},
+                      {const_cast<void *>(v_cache), vs, nullptr, {}}, num_pages, page_size,
+                      block_table, table_width, kv_len, cu_new, scale, max_new, out, lse, ws,
+                      ws_bytes, dev_err, stream);
+}
+
+pair_status pair_attend_paged_q8(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
+                                 pair_dtype dt, const void *q, int64_t q_row, int64_t q_head,
+                                 pair_cache_format fmt, pair_cache_q8 k_cache,
+                                 pair_cache_q8 v_cache, int32_t num_pages, int32_t page_size,
+                                 const int32_t *block_table, int32_t table_width,
+                                 const int32_t *kv_len, const int32_t *cu_new, float scale,
+                                 int32_t max_new, void *out, float *lse, void *ws,
+                                 size_t ws_bytes, int32_t *dev_err, pair_stream_t stream) {
+  if ((int)fmt != q8::kI8 && (int)fmt != q8::kE4M3) {
+    reset_launches();
     return PAIR_ERR_INVALID_ARG;
-  const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
-  // A stride over a single entry says nothing; a tensor map wants one all the same.
-  const auto over = [](int64_t stride, int64_t entries) { return entries > 1 ? stride : 256; };
-  q_row = over(q_row, T), q_head = over(q_head, Hq);
-  for (pair_cache_strides *x : {&ks, &vs})
-    *x = {over(x->for_page, num_pages), over(x->for_token, page_size), over(x->for_head, Hkv)};
-  const int64_t strides[] = {q_row, q_head, ks.for_page, ks.for_token, ks.for_head, vs.for_page,
-                             vs.for_token, vs.for_head};
-  for (const int64_t x : strides)
-    if (x % per != 0) return PAIR_ERR_INVALID_ARG;
-  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16))
-    return PAIR_ERR_INVALID_ARG;
-  const size_t need = pair_attend_workspace_size(R, Hq, Hkv, D, dt);
-  if (need == 0) return PAIR_ERR_UNSUPPORTED;
-  if (!ws || ws_bytes < need || !aligned(ws, 256)) return PAIR_ERR_WORKSPACE;
-  const pair_status dv = check_device();
-  if (dv != PAIR_OK) return dv;
-  const Args a{T,
-               R,
-               Hq,
-               Hkv,
-               Hq / Hkv,
-               -1,
-               INT32_MAX,
-               q,
-               q_row,
-               q_head,
-               k_cache,
-               v_cache,
-               ks,
-               vs,
-               num_pages,
-               page_size,
-               block_table,
-               table_width,
-               kv_len,
-               cu_new,
-               scale,
-               out,
-               lse,
-               static_cast<Desc *>(ws),
-               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + kNotes + kManyNotes),
-               dev_err};
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  Launch few{a, 0, 0}, many{a, 0, 0};
-  many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + kNotes);
-  many.a.part += few_floats(D);
-  // Which kernel a chunk goes to is decided by its rows, on the device; a
-  // launch is left out where the host knows that no chunk can be its.
-  const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
-  const bool only_few = dt == PAIR_F32 || most_rows <= kFewRows || !many_applies(a, D);
-  if (!only_few && R > 1) {
-    few.a.rows_upto = kFewRows;
-    many.a.rows_over = kFewRows;
   }
-  pair_status st = PAIR_OK;
-  if (dt == PAIR_F32) st = launch_simt(&few, D, s);
-  else if (only_few || R > 1) st = launch_few(&few, D, s);
-  if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
-  return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;
+  return attend_paged(T, R, Hq, Hkv, D, dt, q, q_row, q_head, fmt, k_cache, v_cache, num_pages,
+                      page_size, block_table, table_width, kv_len, cu_new, scale, max_new, out, lse,
+                      ws, ws_bytes, dev_err, stream);
 }
 
 }  // extern "C"

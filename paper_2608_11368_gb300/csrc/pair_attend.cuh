@@ -67,6 +67,9 @@ struct Args {
   struct Desc *desc;  // [CTAs][2] segments of each CTA
   float *part;        // partial sums, part_floats() each
   int32_t *dev_err;
+  // Caches in 8 bits: exponent bytes (null: caches in the queries' type).
+  const uint8_t *ke, *ve;
+  pair_cache_strides kes, ves;
 };
 
 // A segment of a CTA: key tiles [t0, t1) of the unit's `tiles`.
@@ -380,7 +383,7 @@ struct Launch {
   Args a;
   int M, ctas;  // rows of its units; 0 CTAs: there is no such launch
 };
-pair_status launch_simt(Launch *l, int D, cudaStream_t s);
+pair_status launch_simt(Launch *l, int D, int fmt, pair_dtype dt, cudaStream_t s);
 pair_status launch_few(Launch *l, int D, cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);

@@ -1,0 +1,256 @@
+"""pair_attend_paged_q8 against the 64-bit form over the stored values: single
+tokens, drafted chunks and long chunks, head layouts, page sizes, cache orders, rows
+that see nothing, whatever lies in places that are not seen.
+
+The stored values are exact in every arithmetic that the kernels use (whole numbers
+or e4m3 times a power of two), so the error bounds are those of attention over a bf16
+or fp32 cache, from the same steps. fp32: a score is a dot product of D terms, off by
+at most D 2^-24 size (size = scale sum |q_d k_d|); sums over m keys add m 2^-24,
+exponentials and rescalings 16 2^-24; relative to mag = sum p |v| twice (weights and
+normaliser). bf16: scores with twice the unit (accumulation on the tensor cores need
+not round to nearest), weights and output rounded once each, by up to eps / 2 = 2^-8
+relative to mag and to |out| <= mag."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rollout
+
+pytestmark = pytest.mark.gpu
+
+CODES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+def build(reqs, Hq, Hkv, D, page, dtype, fmt, layout="token", seed=0, spare=0, shared=0, odd=True):
+    """Device inputs for requests [(n, kv)]; pages in random order. What nobody
+    owns holds random codes under NaN exponents."""
+    rng = np.random.default_rng(seed)
+    R = len(reqs)
+    need = [-(-kv // page) for _, kv in reqs]
+    own = [max(x - shared, 0) for x in need]
+    pages = sum(own) + shared + 2
+    order = rng.permutation(pages)
+    table = np.zeros((R, max(1, max(need))), np.int32)
+    at = shared
+    for i in range(R):
+        table[i, :min(shared, need[i])] = order[:min(shared, need[i])]
+        table[i, shared:need[i]] = order[at:at + own[i]]
+        at += own[i]
+    cu = np.concatenate([[0], np.cumsum([n for n, _ in reqs])])
+    T = max(1, int(cu[-1]) + spare)
+    used = np.zeros((pages, page), bool)
+    for i, (_, kv) in enumerate(reqs):
+        pos = np.arange(kv)
+        used[table[i][pos // page], pos % page] = True
+    held = []
+    for _ in "kv":
+        x = rng.standard_normal((pages, page, Hkv, D))
+        x *= np.exp(0.5 * rng.standard_normal((pages, page, Hkv, 1)))
+        c, e = rollout.store_q8(x, fmt)
+        if fmt == "i8":
+            raw = c.astype(np.int8).view(np.uint8)
+        else:
+            raw = torch.from_numpy(c).to(torch.float8_e4m3fn).view(torch.uint8).numpy().copy()
+        raw[~used] = rng.integers(0, 256, raw[~used].shape) if odd else 0
+        e[~used] = 255 if odd else 0
+        e = e.astype(np.uint8)
+        if layout == "head":
+            c = torch.from_numpy(np.ascontiguousarray(raw.transpose(0, 2, 1, 3))).cuda()
+            e = torch.from_numpy(np.ascontiguousarray(e.transpose(0, 2, 1))).cuda()
+            held += [c.view(CODES[fmt]).permute(0, 2, 1, 3), e.permute(0, 2, 1)]
+        else:
+            held += [torch.from_numpy(raw).cuda().view(CODES[fmt]), torch.from_numpy(e).cuda()]
+    q = torch.from_numpy(2.0 * rng.standard_normal((T, Hq, D))).cuda().to(dtype)
+    i32 = lambda x: torch.from_numpy(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    return dict(q=q, held=held, table=i32(table), kv=i32([kv for _, kv in reqs]), cu=i32(cu))
+
+
+def reference(t, scale):
+    f = lambda x: x.double().cpu().numpy()  # noqa: E731
+    k, ke, v, ve = t["held"]
+    # NaN codes lie in places that nobody owns only; a NaN exponent says so anyway.
+    vals = [rollout.values_q8(np.nan_to_num(f(c.to(torch.float32))), e.cpu().numpy())
+            for c, e in ((k, ke), (v, ve))]
+    return rollout.attend_paged(f(t["q"]), *vals, t["table"].cpu().numpy(), t["kv"].cpu().numpy(),
+                                t["cu"].cpu().numpy(), scale)
+
+
+def check(t, scale=None, rows=None, ref=None, lost=0.0, **kw):
+    from paper_2608_11368_gb300 import binding as B
+    D = t["q"].shape[2]
+    scale = D ** -0.5 if scale is None else scale
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out, lse = B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"], t["cu"],
+                                      scale=scale, dev_err=err, **kw)
+    assert B.pair_status_sync(err) == 0
+    ro, rl, mag, size = reference(t, scale) if ref is None else ref
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    m = int(t["kv"].max())
+    bf = t["q"].dtype == torch.bfloat16
+    sums = (2.0 if bf else 1.0) * 2.0 ** -24 * (D * size + m + 16)
+    rel = 2 * sums + (2 * 2.0 ** -8 * 1.01 if bf else 0.0)
+    if rows is None:
+        rows = np.ones(len(out), bool)
+    assert not np.isnan(out[rows]).any()
+    assert (np.isinf(lse) == np.isinf(rl))[rows].all()
+    fin = np.isfinite(rl) & rows[:, None]
+    assert (out[~np.isfinite(rl) & rows[:, None]] == 0).all()
+    lse_all, lse, rl = lse, np.where(fin, lse, 0.0), np.where(fin, rl, 0.0)
+    assert (np.abs(lse - rl)[fin] <= sums[fin] + 2.0 ** -22 * np.abs(rl[fin])).all()
+    assert (np.abs(out - ro)[fin] <= (rel[..., None] * mag)[fin] + 1e-30 + lost).all()
+    return out, lse_all
+
+
+SHAPES = {
+    "token": [(1, 1)],
+    "tokens": [(1, 1), (1, 15), (1, 16), (1, 17), (1, 63), (1, 64), (1, 65), (1, 700)],
+    "drafts": [(5, 5), (5, 64), (3, 130), (8, 8), (2, 1000), (5, 257)],
+    "chunk": [(40, 40), (129, 300), (1, 77), (64, 64)],
+    "long": [(300, 700), (257, 257)],
+    "none": [(0, 0), (0, 33), (4, 2), (1, 0), (3, 3), (0, 5), (130, 7)],
+}
+
+
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (8, 1, 128), (3, 3, 128), (10, 2, 64), (2, 1, 256)])
+@pytest.mark.parametrize("what", sorted(SHAPES))
+def test_attend(what, heads, dtype, fmt):
+    Hq, Hkv, D = heads
+    check(build(SHAPES[what], Hq, Hkv, D, 16, dtype, fmt, seed=len(what)))
+
+
+@pytest.mark.parametrize("page", [1, 5, 8, 24, 32, 64, 128, 256])
+@pytest.mark.parametrize("layout", ["token", "head"])
+@pytest.mark.parametrize("dtype,fmt", [(torch.bfloat16, "i8"), (torch.bfloat16, "e4m3"),
+                                       (torch.float32, "e4m3")])
+def test_attend_pages_and_orders(page, layout, dtype, fmt):
+    check(build([(1, 130), (5, 97), (70, 200), (0, 0), (200, 333)], 4, 2, 128, page, dtype, fmt,
+                layout=layout, seed=page, spare=3))
+
+
+@pytest.mark.parametrize("n", [1, 7, 150])
+def test_attend_shared_prompt(n):
+    check(build([(n, 400 + n + 3 * i) for i in range(6)], 4, 2, 128, 16, torch.bfloat16, "i8",
+                shared=20, seed=n))
+
+
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("reqs", [[(1, 9001)], [(4, 20000), (1, 3)], [(100, 12000)], [(600, 9000)]])
+def test_attend_split_over_the_length(reqs, fmt):
+    check(build(reqs, 8, 2, 128, 16, torch.bfloat16, fmt, seed=3))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-4, 2.0])
+@pytest.mark.parametrize("n", [1, 70])
+def test_attend_scales(scale, n):
+    check(build([(n, 300)], 4, 2, 128, 16, torch.bfloat16, "i8", seed=1), scale=scale)
+
+
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [3, 40, 200])
+def test_rows_with_nan_reach_those_that_see_them(n, dtype, fmt):
+    """A key or a value held as NaN: rows that see it are NaN, the others are not."""
+    from paper_2608_11368_gb300 import binding as B
+    kv, D = n + 90, 128
+    for which in (1, 3):  # the exponents of keys, of values
+        t = build([(n, kv), (n, kv)], 4, 2, D, 16, dtype, fmt, seed=n)
+        ref = reference(t, D ** -0.5)
+        key = kv - n // 2 - 1  # seen by the later rows of request 0
+        at = int(t["table"][0, key // 16]), key % 16
+        t["held"][which][at[0], at[1], 1] = 255
+        out, _ = B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"], t["cu"])
+        sees = np.zeros((2 * n, 4), bool)
+        sees[key - (kv - n):n, 2:] = True  # query heads 2 and 3 read key head 1
+        got = np.isnan(out.double().cpu().numpy())
+        assert got[sees].all() and not got[~sees].any()
+        err = np.abs(np.where(sees[..., None], 0, out.double().cpu().numpy() - ref[0]))
+        assert (err <= 0.02 * ref[2] + 1e-30).all()
+
+
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("n", [1, 40])
+def test_keys_and_values_of_very_different_sizes(n, fmt):
+    """Exponents over their whole range: tiny values beside large ones, zero rows,
+    scores of hundreds. Weights are fp32 numbers relative to the largest, which is 1:
+    one below 2^-126, the least normal number, may vanish, in the weight itself or in
+    a factor that brings a part of the sums to another part's maximum. A key loses
+    2 * 2^-126 of its value at most, 500 of them the sum of that; the normaliser is at
+    least 1. (Values reach 2^92 times the largest code.)"""
+    D = 64
+    t = build([(n, 500)], 4, 2, D, 16, torch.bfloat16, fmt, seed=n)
+    rng = np.random.default_rng(5)
+    ke, ve = t["held"][1], t["held"][3]
+    used = (ke != 255).cpu().numpy()
+    small = rng.integers(0, 128, used.shape)
+    ke.copy_(torch.from_numpy(np.where(used & (rng.random(used.shape) < 0.5), small,
+                                       ke.cpu().numpy()).astype(np.uint8)))
+    wild = rng.integers(0, 220, used.shape)
+    ve.copy_(torch.from_numpy(np.where(used, wild, ve.cpu().numpy()).astype(np.uint8)))
+    check(t, lost=500 * 2 * 2.0 ** -126 * 2.0 ** 92 * (127 if fmt == "i8" else 448))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_queries_that_are_rows_of_a_wider_array(dtype):
+    t = build([(1, 100), (4, 50), (80, 90)], 4, 2, 64, 16, dtype, "i8", seed=2)
+    T = t["q"].shape[0]
+    wide = torch.zeros((T, 3, 4, 64), dtype=dtype, device="cuda")
+    wide[:, 1] = t["q"]
+    t["q"] = wide[:, 1]
+    check(t)
+
+
+def test_more_rows_than_max_new_says():
+    t = build([(3, 50), (120, 200)], 4, 2, 128, 16, torch.bfloat16, "e4m3")
+    ref = reference(t, 128 ** -0.5)
+    for most in (0, 1, 3, 120, 500):
+        check(t, ref=ref, max_new=most)
+
+
+def test_bad_pages_and_lengths_are_reported():
+    """A request with a page that does not exist, or a length beyond its table row;
+    the others are as they were."""
+    from paper_2608_11368_gb300 import binding as B
+    for n in (1, 50):
+        for what in ("page", "below", "length"):
+            t = build([(n, 200), (n, 210), (n, 220)], 4, 2, 128, 16, torch.bfloat16, "i8", seed=n)
+            ref = reference(t, 128 ** -0.5)
+            if what == "length":
+                t["kv"][1] = 10000
+            else:
+                t["table"][1, 3] = 10 ** 6 if what == "page" else -5
+            err = torch.zeros(1, dtype=torch.int32, device="cuda")
+            out, _ = B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"], t["cu"],
+                                            dev_err=err)
+            assert B.pair_status_sync(err) == 10
+            o = out.double().cpu().numpy()
+            for i in (0, 2):
+                rows = slice(i * n, (i + 1) * n)
+                assert (np.abs(o[rows] - ref[0][rows]) <= 0.02 * ref[2][rows]).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 150])
+def test_same_results_every_time_on_any_stream_and_captured(n):
+    from paper_2608_11368_gb300 import binding as B
+    t = build([(n, 2000 + 100 * i) for i in range(9)], 8, 2, 128, 16, torch.bfloat16, "i8", seed=n)
+    call = lambda **kw: B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"],  # noqa: E731
+                                               t["cu"], max_new=n, **kw)
+    first = [x.clone() for x in call()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = call(stream=side)
+    side.synchronize()
+    out, lse = torch.empty_like(first[0]), torch.empty_like(first[1])
+    ws = torch.empty(B.pair_attend_workspace_size(9, 8, 2, 128, B.PAIR_BF16), dtype=torch.uint8,
+                     device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out=out, lse=lse, ws=ws)
+    for fill in (0, 255, 77):  # whatever the workspace holds
+        ws.fill_(fill)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    assert torch.equal(other[0], first[0]) and torch.equal(other[1], first[1])
