@@ -17,15 +17,6 @@ __device__ __forceinline__ void from_float(__nv_bfloat16 *o, float x) {
   *o = __float2bfloat16_rn(x);
 }
 
-__device__ __forceinline__ float4 load_query(const float *q) {
-  return *reinterpret_cast<const float4 *>(q);
-}
-__device__ __forceinline__ float4 load_query(const __nv_bfloat16 *q) {
-  const uint2 u = *reinterpret_cast<const uint2 *>(q);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
-                     __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
-}
-
 // F: the cache's codes, or q8::kPlain for one in fp32.
 template <int D, int F>
 struct SimtSmem {
@@ -56,7 +47,7 @@ struct SimtSmem {
 //
 // Over a cache in 8 bits the tiles hold the codes, which become fp32 where they are
 // read; a key's scale multiplies its scores, a value's its weights.
-template <typename T, int D, int F>
+template <int D, int F>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   extern __shared__ __align__(16) uint8_t raw[];
   using S = SimtSmem<D, F>;
@@ -72,10 +63,10 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int cta = blockIdx.x, ctas = gridDim.x;
   clear_notes(a, cta);
-  clear_spare_rows<T, D, kSimtThreads>(a, cta, ctas);
+  clear_spare_rows<float, D, kSimtThreads>(a, cta, ctas);
   if (cta == ctas - 1) report_requests(a);
   Walk<M, BN> walk{find_share<kSimtThreads>(a, M, cta, ctas, sm.scratch)};
-  const T *q = static_cast<const T *>(a.q);
+  const float *q = static_cast<const float *>(a.q);
   const E *kc = static_cast<const E *>(a.kc), *vc = static_cast<const E *>(a.vc);
   const float scale = a.scale * kLog2e;
   const int col = tid % (kSimtThreads / RG), rg = tid / (kSimtThreads / RG);
@@ -118,7 +109,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < s.rows) {
         const RowAt at = row_at(a, s.row0, s.r0, s.h, r);
-        u = load_query(q + at.token * a.q_row + at.head * a.q_head + c);
+        u = *reinterpret_cast<const float4 *>(q + at.token * a.q_row + at.head * a.q_head + c);
       }
       *reinterpret_cast<float4 *>(&sm.q[r][c]) = u;
     }
@@ -264,9 +255,9 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         if (rr >= s.rows) continue;
         const RowAt at = row_at(a, s.row0, s.r0, s.h, rr);
         const float l = sm.l[rr], inv = l == 0.f ? 0.f : 1.f / l;
-        T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D;
+        float *out = static_cast<float *>(a.out) + (at.token * a.Hq + at.head) * D;
 #pragma unroll
-        for (int c = 0; c < CPT; ++c) from_float(out + col + c * kSimtThreads, o[r][c] * inv);
+        for (int c = 0; c < CPT; ++c) out[col + c * kSimtThreads] = o[r][c] * inv;
         if (col == 0 && a.lse)
           a.lse[at.token * a.Hq + at.head] =
               l == 0.f ? -INFINITY : (sm.m[rr] + log2f(l)) * kLn2;
@@ -391,12 +382,13 @@ __global__ void __launch_bounds__(kJoinThreads)
   }
 }
 
-template <typename T, int D, int F>
+template <int D, int F>
 pair_status run_simt(Launch *l, cudaStream_t s) {
-  const Args &a = l->a;
+  Args &a = l->a;
+  a.unit_cost = kSimtCost;
   constexpr int smem = sizeof(SimtSmem<D, F>);
   static_assert(smem <= 232448, "shared memory of a CTA");
-  const auto kernel = attend_simt_kernel<T, D, F>;
+  const auto kernel = attend_simt_kernel<D, F>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const int ctas = useful_ctas(a, kSimtRows, min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count()));
@@ -451,7 +443,7 @@ bool aligned(const void *p, uintptr_t to) {
 // worth at most: the host knows the table's width, not the lengths.
 int useful_ctas(const Args &a, int M, int fit) {
   const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
-  const double keys = units * a.Hkv * (unit_cost(M) + (double)a.width * a.page + (double)M / a.g);
+  const double keys = units * a.Hkv * (a.unit_cost + (double)a.width * a.page + (double)M / a.g);
   return keys < (double)fit * kMinKeys ? 1 + (int)(keys / kMinKeys) : fit;
 }
 
@@ -465,15 +457,12 @@ int sm_count() {
   return n;
 }
 
-pair_status launch_simt(Launch *l, int D, int fmt, pair_dtype dt, cudaStream_t s) {
+pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s) {
   return by_size(D, [&](auto d) {
     constexpr int n = decltype(d)::value;
-    if (dt == PAIR_BF16)
-      return fmt == q8::kI8 ? run_simt<__nv_bfloat16, n, q8::kI8>(l, s)
-                            : run_simt<__nv_bfloat16, n, q8::kE4M3>(l, s);
-    return fmt == q8::kPlain ? run_simt<float, n, q8::kPlain>(l, s)
-           : fmt == q8::kI8  ? run_simt<float, n, q8::kI8>(l, s)
-                             : run_simt<float, n, q8::kE4M3>(l, s);
+    return fmt == q8::kPlain ? run_simt<n, q8::kPlain>(l, s)
+           : fmt == q8::kI8  ? run_simt<n, q8::kI8>(l, s)
+                             : run_simt<n, q8::kE4M3>(l, s);
   });
 }
 
@@ -549,7 +538,8 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                k.exps,
                v.exps,
                k.exps_at,
-               v.exps_at};
+               v.exps_at,
+               0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   Launch few{a, 0, 0}, many{a, 0, 0};
   many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + kNotes);
@@ -557,14 +547,15 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   // Which kernel a chunk goes to is decided by its rows, on the device; a
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
-  const bool simt = dt == PAIR_F32 || held;
-  const bool only_few = simt || most_rows <= kFewRows || !many_applies(a, D);
+  const bool simt = dt == PAIR_F32;
+  const bool only_few = simt || held || most_rows <= kFewRows || !many_applies(a, D);
   if (!only_few && R > 1) {
     few.a.rows_upto = kFewRows;
     many.a.rows_over = kFewRows;
   }
   pair_status st = PAIR_OK;
-  if (simt) st = launch_simt(&few, D, fmt, dt, s);
+  if (simt) st = launch_simt(&few, D, fmt, s);
+  else if (held) st = launch_few_q8(&few, D, fmt, most_rows, s);
   else if (only_few || R > 1) st = launch_few(&few, D, s);
   if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
   return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;

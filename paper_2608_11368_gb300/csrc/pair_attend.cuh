@@ -41,9 +41,7 @@ constexpr float kLn2 = 0.69314718055994531f;
 // 337 at 1600; 16 x 16 requests with drafts (few rows): 422 at 48, 404 at 128, 398 at
 // 192. Heads of 64 and 256 go by the same values; the 48 of fp32's units of 16 rows
 // was not swept.
-__host__ __device__ constexpr int unit_cost(int M) {
-  return M == kManyRows ? 800 : M == kFewTile ? 192 : 48;
-}
+constexpr int kManyCost = 800, kFewCost = 192, kSimtCost = 48;
 // Keys of a request at most: tile numbers, and a unit's length with its fixed
 // cost, stay within 32 bits.
 constexpr int kMaxKeys = INT32_MAX - 4096;
@@ -70,6 +68,7 @@ struct Args {
   // Caches in 8 bits: exponent bytes (null: caches in the queries' type).
   const uint8_t *ke, *ve;
   pair_cache_strides kes, ves;
+  int32_t unit_cost;  // fixed cost of a unit of this launch, in keys
 };
 
 // A segment of a CTA: key tiles [t0, t1) of the unit's `tiles`.
@@ -113,9 +112,9 @@ struct Line {
   int64_t base;   // of a unit, without its rows' own tokens
   int32_t units;  // row tiles per key head
   int32_t M;
-  __device__ __forceinline__ Line(const Request &r, int M_, int g) : M(M_) {
-    base = (int64_t)2 * g * (unit_cost(M_) + max(0, r.kv - r.n));
-    units = (int32_t)(((int64_t)r.n * g + M - 1) / M);
+  __device__ __forceinline__ Line(const Request &r, int M_, const Args &a) : M(M_) {
+    base = (int64_t)2 * a.g * (a.unit_cost + max(0, r.kv - r.n));
+    units = (int32_t)(((int64_t)r.n * a.g + M - 1) / M);
   }
   // Length of the first k units, and of unit k.
   __device__ __forceinline__ int64_t upto(int64_t k) const { return k * base + M * k * (k + 1); }
@@ -124,7 +123,7 @@ struct Line {
 
 __device__ __forceinline__ int64_t request_cost(const Args &a, int i, int M) {
   const Request r = request(a, i);
-  const Line l(r, M, a.g);
+  const Line l(r, M, a);
   return (int64_t)a.Hkv * l.upto(l.units);
 }
 
@@ -159,7 +158,7 @@ __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *sc
   x += before - sum;  // exclusive
   int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * kMinKeys)));
   if (a.R == 1) {  // units of one length, nearly: no CTA across two of them
-    const int64_t units = (int64_t)a.Hkv * Line(request(a, 0), M, a.g).units;
+    const int64_t units = (int64_t)a.Hkv * Line(request(a, 0), M, a).units;
     if (n > units && units > 0) n -= n % units;
   }
   Share s{0, 0, 0, 0};
@@ -219,7 +218,7 @@ struct Walk {
     while (s.from < s.to) {
       if (!started) {  // the only search: the unit that the share begins in
         r = request(a, s.i);
-        const Line l(r, M, a.g);
+        const Line l(r, M, a);
         const int64_t per_head = l.upto(l.units), off = s.from - s.at;
         h = (int)(off / per_head);
         const int64_t x = off - h * per_head;
@@ -241,12 +240,12 @@ struct Walk {
               if (++s.i >= a.R) return false;
               r = request(a, s.i);
             } while (r.n == 0);
-            units = Line(r, M, a.g).units;
+            units = Line(r, M, a).units;
           }
         }
         begin = s.from;
       }
-      const int64_t cost = Line(r, M, a.g).of(k);
+      const int64_t cost = Line(r, M, a).of(k);
       const int64_t x0 = s.from - begin, x1 = min(cost, x0 + (s.to - s.from));
       g->i = s.i;
       g->h = h;
@@ -383,8 +382,10 @@ struct Launch {
   Args a;
   int M, ctas;  // rows of its units; 0 CTAs: there is no such launch
 };
-pair_status launch_simt(Launch *l, int D, int fmt, pair_dtype dt, cudaStream_t s);
+pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s);
 pair_status launch_few(Launch *l, int D, cudaStream_t s);
+// Caches in 8 bits; most_rows: of a chunk, as far as the host knows.
+pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);
 int sm_count();

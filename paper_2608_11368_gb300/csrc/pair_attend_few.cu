@@ -361,7 +361,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) attend_few_kernel(
 
 template <int D>
 pair_status run_few(Launch *l, cudaStream_t s) {
-  const Args &a = l->a;
+  Args &a = l->a;
+  a.unit_cost = kFewCost;
   constexpr int smem = Few<D>::kBytes;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_few_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));

@@ -705,7 +705,8 @@ bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args &a, in
 
 template <int D>
 pair_status run_many(Launch *l, const Maps &maps, cudaStream_t s) {
-  const Args &a = l->a;
+  Args &a = l->a;
+  a.unit_cost = kManyCost;
   constexpr int smem = sizeof(Smem<D>) + 1024;
   static_assert(smem <= 232448, "shared memory of a CTA");
   PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_many_kernel<D>,
