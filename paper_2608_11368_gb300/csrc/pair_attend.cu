@@ -539,6 +539,7 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                v.exps,
                k.exps_at,
                v.exps_at,
+               false,
                0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   Launch few{a, 0, 0}, many{a, 0, 0};

@@ -68,6 +68,7 @@ struct Args {
   // Caches in 8 bits: exponent bytes (null: caches in the queries' type).
   const uint8_t *ke, *ve;
   pair_cache_strides kes, ves;
+  bool narrow;        // strides of pages and tokens fit in 32 bits
   int32_t unit_cost;  // fixed cost of a unit of this launch, in keys
 };
 

@@ -81,13 +81,11 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
   return u;
 }
 
-__device__ __forceinline__ void st_shared64(uint32_t at, const void *p) {
-  asm volatile("st.shared.b64 [%0], %1;" ::"r"(at), "l"(p) : "memory");
-}
-__device__ __forceinline__ const uint8_t *ld_shared_ptr(uint32_t at) {
-  const uint8_t *p;
-  asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(at) : "memory");
-  return p;
+// p + x * stride, in one instruction: a stride that fits in 32 bits.
+__device__ __forceinline__ const uint8_t *wide(const uint8_t *p, int x, int64_t stride) {
+  const uint8_t *q;
+  asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(q) : "r"(x), "r"((uint32_t)stride), "l"(p));
+  return q;
 }
 
 // The codes of a word in fp16: bytes 0, 1 and bytes 2, 3.
@@ -104,14 +102,18 @@ __device__ __forceinline__ void to_half(uint32_t w, uint32_t &lo, uint32_t &hi) 
   }
 }
 
-// The codes in the low (hi = 0) or the high bytes of both halves of x in bf16.
+// The codes in the low (hi = 0) or the high bytes of both halves of x in bf16, over
+// kValueUnit.
+template <int F>
+constexpr float kValueUnit = F == kI8 ? 64.f : 1.f;
 template <int F, int hi>
 __device__ __forceinline__ uint32_t to_bf16(uint32_t x) {
   if constexpr (F == kI8) {
-    // Seven bits under 0x43 are 128 + those; the sign bit there makes 128 into 256.
+    // A byte u = code + 128 is as a bf16 number u 2^-133: below 128 a subnormal one, from
+    // there on one of the least exponent, in the same steps. Times 2^127, less 2.
     const uint32_t y = hi ? x >> 8 : x;
-    return bits(__hsub2(bf2_of((y & 0x007f007fu) | 0x43004300u),
-                        bf2_of((y & 0x00800080u) | 0x43004300u)));
+    return bits(__hfma2(bf2_of((y & 0x00ff00ffu) ^ 0x00800080u), bf2_of(0x7f007f00u),
+                        bf2_of(0xc000c000u)));
   } else {
     // Exponent and significand at bf16's places are the number times 2^-120 (numbers
     // below e4m3's normal ones too: bf16's multiply takes them as they are). The two
@@ -167,7 +169,9 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
   float *factor = reinterpret_cast<float *>(smem + L::kFactor);
   const uint32_t ring = smem_u32(smem + L::kRing) + warp * NST * 2 * L::kPart;
   const uint32_t ptrs = smem_u32(smem + L::kPtr) + warp * 2 * kSlice * 8;
-  const uint8_t *kc = static_cast<const uint8_t *>(a.kc), *vc = static_cast<const uint8_t *>(a.vc);
+  const uint8_t *kc0 = static_cast<const uint8_t *>(a.kc) + s.h * a.ks.for_head;
+  const uint8_t *vc0 = static_cast<const uint8_t *>(a.vc) + s.h * a.vs.for_head;
+  const uint8_t *ke0 = a.ke + s.h * a.kes.for_head, *ve0 = a.ve + s.h * a.ves.for_head;
 
   // This lane's key of a slice, and its way in the table.
   const int end = min(s.keys, s.t1 * BN), first = s.t0 * BN + warp * kSlice;
@@ -196,10 +200,20 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
       flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
       pg = 0;
     }
-    kb = __ldg(a.ke + cache_row(a, a.kes, pg, o, s.h));
-    vb = __ldg(a.ve + cache_row(a, a.ves, pg, o, s.h));
-    st_shared64(ptrs + lane * 8, kc + cache_row(a, a.ks, pg, o, s.h));
-    st_shared64(ptrs + (kSlice + lane) * 8, vc + cache_row(a, a.vs, pg, o, s.h));
+    const uint8_t *kp, *vp;
+    if (a.narrow) {
+      kb = __ldg(wide(wide(ke0, pg, a.kes.for_page), o, a.kes.for_token));
+      vb = __ldg(wide(wide(ve0, pg, a.ves.for_page), o, a.ves.for_token));
+      kp = wide(wide(kc0, pg, a.ks.for_page), o, a.ks.for_token);
+      vp = wide(wide(vc0, pg, a.vs.for_page), o, a.vs.for_token);
+    } else {
+      kb = __ldg(ke0 + cache_row(a, a.kes, pg, o, 0));
+      vb = __ldg(ve0 + cache_row(a, a.ves, pg, o, 0));
+      kp = kc0 + cache_row(a, a.ks, pg, o, 0);
+      vp = vc0 + cache_row(a, a.vs, pg, o, 0);
+    }
+    asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(ptrs + lane * 16), "l"(kp), "l"(vp)
+                 : "memory");
     __syncwarp();
     constexpr int P = L::kPieces, RP = 32 / P;  // rows of one round of copies
     const int c = lane % P;
@@ -207,8 +221,12 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
 #pragma unroll
     for (int x = 0; x < kSlice / RP; ++x) {
       const int r = x * RP + lane / P;
-      cp_async16(kd + place<D, false>(r, c), ld_shared_ptr(ptrs + r * 8) + c * 16, true);
-      cp_async16(vd + place<D, true>(r, c), ld_shared_ptr(ptrs + (kSlice + r) * 8) + c * 16, true);
+      asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];"
+                   : "=l"(kp), "=l"(vp)
+                   : "r"(ptrs + r * 16)
+                   : "memory");
+      cp_async16(kd + place<D, false>(r, c), wide(kp, c, 16), true);
+      cp_async16(vd + place<D, true>(r, c), wide(vp, c, 16), true);
     }
   };
   __syncthreads();  // the segment before is through
@@ -322,8 +340,6 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
     }
     // sc[i][j][c]: key 16 i + g + 8 (c / 2), row 8 j + 2 t + c % 2. In log2 units, relative
     // to the row's reference, which is 0 at first.
-    const bool edge = key0 + kSlice > least;
-    float over = -INFINITY;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const float k0 = __shfl_sync(0xffffffffu, ke, i * 16 + g);
@@ -331,13 +347,26 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v = fmaf(sc[i][j][c] * (c < 2 ? k0 : k1), cs[j][c & 1], -m[j][c & 1]);
-          if (edge && key0 + i * 16 + g + 8 * (c >> 1) >= seen[j][c & 1]) v = -INFINITY;
-          sc[i][j][c] = v;
-          over = fmaxf(over, v);
-        }
+        for (int c = 0; c < 4; ++c)
+          sc[i][j][c] = fmaf(sc[i][j][c] * (c < 2 ? k0 : k1), cs[j][c & 1], -m[j][c & 1]);
     }
+    const bool edge = key0 + kSlice > least;
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (key0 + i * 16 + g + 8 * (c >> 1) >= seen[j][c & 1]) sc[i][j][c] = -INFINITY;
+    }
+    float over = sc[0][0][0];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) over = fmaxf(over, sc[i][j][c]);
     // The reference is the first slice's maximum (a row that sees none of its keys sees
     // none behind it) and stays while no maximum has grown by more than 2^8 over it:
     // weights up to 256 are as good as weights up to 1.
@@ -371,20 +400,27 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
     for (int i = 0; i < MT; ++i) {
       const float v0 = __shfl_sync(0xffffffffu, ve, i * 16 + g);
       const float v1 = __shfl_sync(0xffffffffu, ve, i * 16 + 8 + g);
-      uint32_t p[NT][2];
+      float w[NT][4];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        float w[4];
+      for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const float e = ex2_approx(sc[i][j][c]);
           l[j][c & 1] += e;
-          w[c] = e * (c < 2 ? v0 : v1);
-          // A key that the row does not see: its scale may be NaN.
-          if (edge && key0 + i * 16 + g + 8 * (c >> 1) >= seen[j][c & 1]) w[c] = 0.f;
+          w[j][c] = e * (c < 2 ? v0 : v1);
         }
-        p[j][0] = transposed(bits(__floats2bfloat162_rn(w[0], w[1])));
-        p[j][1] = transposed(bits(__floats2bfloat162_rn(w[2], w[3])));
+      if (edge) {  // the scale of a value that a row does not see may be NaN
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (key0 + i * 16 + g + 8 * (c >> 1) >= seen[j][c & 1]) w[j][c] = 0.f;
+      }
+      uint32_t p[NT][2];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        p[j][0] = transposed(bits(__floats2bfloat162_rn(w[j][0], w[j][1])));
+        p[j][1] = transposed(bits(__floats2bfloat162_rn(w[j][2], w[j][3])));
       }
       // Values of the lane's keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: 16 columns (8 for heads
       // of 64), two of a product's 16 at a time.
@@ -453,8 +489,8 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) {
       const float2 e = ml[k * R + r];
-      const float f = ex2_approx(e.x - ref);
-      sum = fmaf(e.y, f, sum);
+      const float w = ex2_approx(e.x - ref), f = kValueUnit<F> * w;
+      sum = fmaf(e.y, w, sum);
 #pragma unroll
       for (int c = 0; c < 8; c += 2) {
         const float2 y =
@@ -520,6 +556,9 @@ pair_status run_few(Launch *l, cudaStream_t s) {
   const auto kernel = attend_q8_few_kernel<D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   a.unit_cost = 192;
+  a.narrow = true;
+  for (const pair_cache_strides *x : {&a.ks, &a.vs, &a.kes, &a.ves})
+    a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
   const int ctas = useful_ctas(a, M, min(kMaxCtas, per_sm * sm_count()));
   PAIR_BEGIN("attend_q8_few", s);
   kernel<<<ctas, kThreads, smem, s>>>(a);
