@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   const int per = join_blocks(second ? l1 : l0);
   const int block = blockIdx.x - (second ? first : 0);
   const int cta = block / per, y = block - cta * per;
-  __shared__ int slots[kMaxCtas];
+  __shared__ int slots[kMaxWorkers];
   __shared__ int n_slots;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_previous();
@@ -430,6 +430,9 @@ pair_status by_size(int D, F f) {
 // The workspace: notes and partial sums of a launch with few or, in fp32, any rows,
 // then those of a launch with many.
 constexpr size_t kNotes = kMaxCtas * 2 * sizeof(Desc), kManyNotes = kMaxMany * 2 * sizeof(Desc);
+// Over caches in 8 bits warps have shares and notes of their own; the partial sums behind
+// them take the rest.
+constexpr size_t kHeldNotes = kMaxWorkers * 2 * sizeof(Desc);
 size_t few_floats(int D) { return kMaxCtas * 2 * part_floats(kFewTile, D); }
 size_t many_floats(int D) { return kMaxMany * 2 * part_floats(kManyRows, D); }
 
@@ -441,10 +444,10 @@ bool aligned(const void *p, uintptr_t to) {
 
 // CTAs (or pairs) of a launch: as many as fit at once, or as the work can be
 // worth at most: the host knows the table's width, not the lengths.
-int useful_ctas(const Args &a, int M, int fit) {
+int useful_ctas(const Args &a, int M, int fit, int least) {
   const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
   const double keys = units * a.Hkv * (a.unit_cost + (double)a.width * a.page + (double)M / a.g);
-  return keys < (double)fit * kMinKeys ? 1 + (int)(keys / kMinKeys) : fit;
+  return keys < (double)fit * least ? 1 + (int)(keys / least) : fit;
 }
 
 int sm_count() {
@@ -509,6 +512,7 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   if (!ws || ws_bytes < need || !aligned(ws, 256)) return PAIR_ERR_WORKSPACE;
   const pair_status dv = check_device();
   if (dv != PAIR_OK) return dv;
+  const size_t notes = held && dt == PAIR_BF16 ? kHeldNotes : kNotes;
   const Args a{T,
                R,
                Hq,
@@ -533,7 +537,7 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                out,
                lse,
                static_cast<Desc *>(ws),
-               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + kNotes + kManyNotes),
+               reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + notes + kManyNotes),
                dev_err,
                k.exps,
                v.exps,
@@ -543,8 +547,8 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   Launch few{a, 0, 0}, many{a, 0, 0};
-  many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + kNotes);
-  many.a.part += few_floats(D);
+  many.a.desc = reinterpret_cast<Desc *>(static_cast<uint8_t *>(ws) + notes);
+  many.a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need) - many_floats(D);
   // Which kernel a chunk goes to is decided by its rows, on the device; a
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
@@ -556,7 +560,11 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   }
   pair_status st = PAIR_OK;
   if (simt) st = launch_simt(&few, D, fmt, s);
-  else if (held) st = launch_few_q8(&few, D, fmt, most_rows, s);
+  else if (held)
+    st = launch_few_q8(&few, D, fmt, most_rows,
+                       (int)(((only_few ? reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need)
+                                        : many.a.part) - few.a.part) / part_floats(kFewTile, D)),
+                       s);
   else if (only_few || R > 1) st = launch_few(&few, D, s);
   if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
   return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;

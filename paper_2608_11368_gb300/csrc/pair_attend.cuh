@@ -28,6 +28,7 @@ namespace attend {
 
 constexpr int kMaxCtas = 480;    // of a launch with units of up to kFewTile rows
 constexpr int kMaxMany = 160;    // of a launch with units of kManyRows rows
+constexpr int kMaxWorkers = 1920;  // warps with shares of their own, in a launch of them
 constexpr int kManyRows = 256;   // rows of a unit of the kernel for many rows
 constexpr int kFewTile = 64;     // rows of a unit of the kernel for few rows
 // Chunks of up to so many rows go to the kernel for few rows, longer ones to the
@@ -46,6 +47,7 @@ constexpr int kManyCost = 800, kFewCost = 192, kSimtCost = 48;
 // cost, stay within 32 bits.
 constexpr int kMaxKeys = INT32_MAX - 4096;
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
+constexpr int kMinWarp = 64;     // or a warp, where those have shares
 
 struct Args {
   int64_t T;
@@ -135,8 +137,10 @@ struct Share {
   int32_t i;
 };
 
-// By a whole block of NT threads; scratch: NT / 32 + 2 int64 of shared memory.
-template <int NT>
+// By a whole block of NT threads; scratch: NT / 32 + 2 N int64 of shared memory. N
+// shares of a block, from that of its first warp on: warp w's is the w-th of them, and
+// `cta` that share's number (the block's, where N is 1).
+template <int NT, int N = 1>
 __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *scratch) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int W = NT / 32;
@@ -157,31 +161,39 @@ __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *sc
     total += scratch[w];
   }
   x += before - sum;  // exclusive
-  int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * kMinKeys)));
+  int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * (N > 1 ? kMinWarp : kMinKeys))));
   if (a.R == 1) {  // units of one length, nearly: no CTA across two of them
     const int64_t units = (int64_t)a.Hkv * Line(request(a, 0), M, a).units;
     if (n > units && units > 0) n -= n % units;
   }
+  const int k0 = N > 1 ? warp : 0;  // the share that is returned
+  // total * c / n, rounded down.
+  const int64_t each = total / n;
+  const uint32_t rest = (uint32_t)(total - each * n);
+  const auto cut = [&](int c) { return each * c + rest * (uint32_t)c / (uint32_t)n; };
   Share s{0, 0, 0, 0};
-  if (cta < n) {
-    s.from = (int64_t)((__int128)total * cta / n);
-    s.to = (int64_t)((__int128)total * (cta + 1) / n);
-  }
-  if (s.from < s.to && s.from >= x && s.from < x + sum) {
-    int64_t at = x;
-    int i = i0;
-    for (; i < i1; ++i) {
-      const int64_t c = request_cost(a, i, M);
-      if (s.from < at + c) break;
-      at += c;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int c = cta - k0 + k;
+    if (c >= n) continue;
+    const int64_t from = cut(c), to = cut(c + 1);
+    if (k == k0) s.from = from, s.to = to;
+    if (from < to && from >= x && from < x + sum) {
+      int64_t at = x;
+      int i = i0;
+      for (; i < i1; ++i) {
+        const int64_t c1 = request_cost(a, i, M);
+        if (from < at + c1) break;
+        at += c1;
+      }
+      scratch[W + 2 * k] = at;
+      scratch[W + 2 * k + 1] = i;
     }
-    scratch[W] = at;
-    scratch[W + 1] = i;
   }
   __syncthreads();
   if (s.from < s.to) {
-    s.at = scratch[W];
-    s.i = (int32_t)scratch[W + 1];
+    s.at = scratch[W + 2 * k0];
+    s.i = (int32_t)scratch[W + 2 * k0 + 1];
   }
   return s;
 }
@@ -386,11 +398,13 @@ struct Launch {
 pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s);
 pair_status launch_few(Launch *l, int D, cudaStream_t s);
 // Caches in 8 bits; most_rows: of a chunk, as far as the host knows.
-pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, cudaStream_t s);
+// slots: partial sums of kFewTile rows that the workspace has room for.
+pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, int slots,
+                          cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);
 int sm_count();
-int useful_ctas(const Args &a, int M, int fit);
+int useful_ctas(const Args &a, int M, int fit, int least = kMinKeys);
 
 }  // namespace attend
 }  // namespace pairk

@@ -124,22 +124,33 @@ __device__ __forceinline__ uint32_t to_bf16(uint32_t x) {
   }
 }
 
-// Shared memory of a CTA whose units have up to M rows.
+// A warp's way along its share, and its segment after the one at hand: in shared memory,
+// which lane 0 writes; registers are short.
+template <int M>
+struct Place {
+  Walk<M, BN> walk;
+  Segment next;
+  bool more;
+  __device__ __forceinline__ void step(const Args &a) {
+    if ((threadIdx.x & 31) == 0) more = walk.next(a, &next);
+    __syncwarp();
+  }
+};
+
+// Shared memory of a warp whose units have up to M rows.
 template <int D, int M>
 struct Few {
   static constexpr int kStages = 2;
-  static constexpr int kPart = kSlice * D;         // bytes of a slice of keys or values
-  static constexpr int kPieces = D / 16;           // 16-byte pieces of a row
-  static constexpr int kSteps = D / 16;            // steps of 16 columns in K Q^T
-  static constexpr int kPtr = 0;                   // addresses: [kWarps][2][kSlice]
-  static constexpr int kFactor = kPtr + kWarps * 2 * kSlice * 8;  // [M] scales of the queries
-  static constexpr int kQ = kFactor + M * 4;       // [M / 8][kSteps / 2][32 lanes] 16 bytes
-  static constexpr int kRing = kQ + M * D * 2;     // [kWarps][kStages] slices
-  static constexpr int kLine = D + 4;              // floats of a row of the warps' sums, which
-  static constexpr int kMl = kRing + kWarps * M * kLine * 4;  // take the ring's place: sums,
-  static constexpr int kSums = kMl + kWarps * M * 8;          // statistics
-  static constexpr int kEnd = kRing + kWarps * kStages * 2 * kPart;
-  static constexpr int kBytes = kEnd > kSums ? kEnd : kSums;
+  static constexpr int kPart = kSlice * D;     // bytes of a slice of keys or values
+  static constexpr int kPieces = D / 16;       // 16-byte pieces of a row
+  static constexpr int kSteps = D / 16;        // steps of 16 columns in K Q^T
+  static constexpr int kRing = 0;              // [kStages][keys, values]
+  static constexpr int kPtr = kRing + kStages * 2 * kPart;  // [kSlice] addresses of both
+  static constexpr int kQ = kPtr + kSlice * 16;  // [M / 8][kSteps / 2][32 lanes] 16 bytes
+  static constexpr int kFactor = kQ + M * D * 2;  // [M] scales of the queries
+  static constexpr int kPlace = kFactor + M * 4;  // a Place
+  static constexpr int kWarpBytes = (kPlace + (int)sizeof(Place<M>) + 127) / 128 * 128;
+  static constexpr int kBytes = kWarps * kWarpBytes;
 };
 
 // Where a 16-byte piece of a row lies in a slice, so that the reads below find all
@@ -155,89 +166,104 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
   }
 }
 
-// A segment whose tile has at most 8 NT rows in use. Warp w has the slices w, w + 4, .. of
-// 32 keys. The warps share nothing while they work: each brings its own slices into a
-// ring of its own, by 16-byte asynchronous copies, and waits for nobody.
-template <int D, int F, int M, int NT>
-__device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uint8_t *smem,
-                                            int cta, int seg) {
+// Where a warp's copies are: its lane's key of the next slice, and that key's way in the
+// block table.
+struct Stream {
+  const int32_t *row;
+  int32_t key, end, at, off, id;
+  int32_t slices, stage;
+  uint32_t kb, vb;  // exponent bytes of the lane's key in the slice on its way
+};
+
+// The slices of a segment, and the page of this lane's first key.
+__device__ __forceinline__ void begin_stream(const Args &a, const Segment &s, Stream &m) {
+  const int first = s.t0 * BN;
+  m.row = a.table + (int64_t)s.i * a.width;
+  m.end = min(s.keys, s.t1 * BN);
+  m.slices = first < m.end ? (m.end - first + kSlice - 1) / kSlice : 0;
+  m.key = first + (threadIdx.x & 31);
+  m.at = m.key / a.page;
+  m.off = m.key - m.at * a.page;
+  m.id = m.key < m.end ? m.row[m.at] : 0;
+}
+__device__ __forceinline__ void look_ahead(const Args &a, Stream &m, int by, int by_off) {
+  m.key += kSlice;
+  m.at += by;
+  m.off += by_off;
+  if (m.off >= a.page) {
+    m.off -= a.page;
+    ++m.at;
+  }
+  m.id = m.key < m.end ? m.row[m.at] : 0;
+}
+// Starts the copies of the slice that was looked up, and reads its exponents. Keys that do
+// not exist are the cache's first: they are masked.
+template <int D, int M>
+__device__ __forceinline__ void fetch(const Args &a, const Segment &s, Stream &m, uint32_t base) {
   using L = Few<D, M>;
-  constexpr int NST = L::kStages, MT = kSlice / 16;
-  constexpr int DT = D / 16;  // tiles of 16 columns in O^T
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int g = lane >> 2, t = lane & 3;
-  float *factor = reinterpret_cast<float *>(smem + L::kFactor);
-  const uint32_t ring = smem_u32(smem + L::kRing) + warp * NST * 2 * L::kPart;
-  const uint32_t ptrs = smem_u32(smem + L::kPtr) + warp * 2 * kSlice * 8;
+  const int lane = threadIdx.x & 31;
   const uint8_t *kc0 = static_cast<const uint8_t *>(a.kc) + s.h * a.ks.for_head;
   const uint8_t *vc0 = static_cast<const uint8_t *>(a.vc) + s.h * a.vs.for_head;
   const uint8_t *ke0 = a.ke + s.h * a.kes.for_head, *ve0 = a.ve + s.h * a.ves.for_head;
-
-  // This lane's key of a slice, and its way in the table.
-  const int end = min(s.keys, s.t1 * BN), first = s.t0 * BN + warp * kSlice;
-  const int slices = first < end ? (end - first + BN - 1) / BN : 0;
-  int key = first + lane, at = key / a.page, off = key - at * a.page;
-  const int by = BN / a.page, by_off = BN - by * a.page;
-  const int32_t *row = a.table + (int64_t)s.i * a.width;
-  int id = key < end ? row[at] : 0;
-  auto look_ahead = [&] {
-    key += BN;
-    at += by;
-    off += by_off;
-    if (off >= a.page) {
-      off -= a.page;
-      ++at;
-    }
-    id = key < end ? row[at] : 0;
-  };
-  // Starts the copies of the slice that was looked up, and reads its exponents. Keys
-  // that do not exist are the cache's first: they are masked.
-  uint32_t kb = 0, vb = 0;
-  auto fetch = [&](int stage) {
-    int pg = id, o = off;
-    if (key >= end) pg = 0, o = 0;
-    if ((unsigned)pg >= (unsigned)a.num_pages) {
-      flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
-      pg = 0;
-    }
-    const uint8_t *kp, *vp;
-    if (a.narrow) {
-      kb = __ldg(wide(wide(ke0, pg, a.kes.for_page), o, a.kes.for_token));
-      vb = __ldg(wide(wide(ve0, pg, a.ves.for_page), o, a.ves.for_token));
-      kp = wide(wide(kc0, pg, a.ks.for_page), o, a.ks.for_token);
-      vp = wide(wide(vc0, pg, a.vs.for_page), o, a.vs.for_token);
-    } else {
-      kb = __ldg(ke0 + cache_row(a, a.kes, pg, o, 0));
-      vb = __ldg(ve0 + cache_row(a, a.ves, pg, o, 0));
-      kp = kc0 + cache_row(a, a.ks, pg, o, 0);
-      vp = vc0 + cache_row(a, a.vs, pg, o, 0);
-    }
-    asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(ptrs + lane * 16), "l"(kp), "l"(vp)
-                 : "memory");
-    __syncwarp();
-    constexpr int P = L::kPieces, RP = 32 / P;  // rows of one round of copies
-    const int c = lane % P;
-    const uint32_t kd = ring + stage * 2 * L::kPart, vd = kd + L::kPart;
+  int pg = m.id, o = m.off;
+  if (m.key >= m.end) pg = 0, o = 0;
+  if ((unsigned)pg >= (unsigned)a.num_pages) {
+    flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
+    pg = 0;
+  }
+  const uint8_t *kp, *vp;
+  if (a.narrow) {
+    m.kb = __ldg(wide(wide(ke0, pg, a.kes.for_page), o, a.kes.for_token));
+    m.vb = __ldg(wide(wide(ve0, pg, a.ves.for_page), o, a.ves.for_token));
+    kp = wide(wide(kc0, pg, a.ks.for_page), o, a.ks.for_token);
+    vp = wide(wide(vc0, pg, a.vs.for_page), o, a.vs.for_token);
+  } else {
+    m.kb = __ldg(ke0 + cache_row(a, a.kes, pg, o, 0));
+    m.vb = __ldg(ve0 + cache_row(a, a.ves, pg, o, 0));
+    kp = kc0 + cache_row(a, a.ks, pg, o, 0);
+    vp = vc0 + cache_row(a, a.vs, pg, o, 0);
+  }
+  const uint32_t ptrs = base + L::kPtr;
+  asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(ptrs + lane * 16), "l"(kp), "l"(vp)
+               : "memory");
+  __syncwarp();
+  constexpr int P = L::kPieces, RP = 32 / P;  // rows of one round of copies
+  const int c = lane % P;
+  const uint32_t kd = base + L::kRing + m.stage * 2 * L::kPart, vd = kd + L::kPart;
 #pragma unroll
-    for (int x = 0; x < kSlice / RP; ++x) {
-      const int r = x * RP + lane / P;
-      asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];"
-                   : "=l"(kp), "=l"(vp)
-                   : "r"(ptrs + r * 16)
-                   : "memory");
-      cp_async16(kd + place<D, false>(r, c), wide(kp, c, 16), true);
-      cp_async16(vd + place<D, true>(r, c), wide(vp, c, 16), true);
-    }
-  };
-  __syncthreads();  // the segment before is through
-  if (slices > 0) fetch(0);
-  cp_async_commit();
-  if (slices > 1) look_ahead();
+  for (int x = 0; x < kSlice / RP; ++x) {
+    const int r = x * RP + lane / P;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];"
+                 : "=l"(kp), "=l"(vp)
+                 : "r"(ptrs + r * 16)
+                 : "memory");
+    cp_async16(kd + place<D, false>(r, c), wide(kp, c, 16), true);
+    cp_async16(vd + place<D, true>(r, c), wide(vp, c, 16), true);
+  }
+}
+
+// A warp's segment of up to 8 NT rows. Its first slice is on its way; when it ends, the
+// first slice of the segment `next` is (if there is one).
+template <int D, int F, int M, int NT>
+__device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Stream &m,
+                                            const Place<M> &place_of, uint8_t *smem, float *part) {
+  using L = Few<D, M>;
+  constexpr int MT = kSlice / 16;
+  constexpr int DT = D / 16;  // tiles of 16 columns in O^T
+  const int lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  const uint32_t base = smem_u32(smem);
+  float *factor = reinterpret_cast<float *>(smem + L::kFactor);
+  const int by = kSlice / a.page, by_off = kSlice - by * a.page;
+  const int slices = m.slices, first = s.t0 * BN;
+  __syncwarp();
 
   // Queries in fp16, in the order in which the products take them: step k of 16 columns
   // takes of lane (g, t) the columns 16 (t + 4 (k / 4)) + 4 (k % 4) + {0, 1, 2, 3} of
   // row g, the places of the four codes of a word.
-  for (int j = warp; j < NT; j += kWarps) {
+  if (slices > 1) look_ahead(a, m, by, by_off);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
     const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q);
     const int r = j * 8 + g;
     uint4 u[D / 32];
@@ -248,8 +274,9 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
     for (int x = 0; x < D / 32; ++x) {
       u[x] = r < s.rows ? *reinterpret_cast<const uint4 *>(src + 64 * (x >> 1) + 8 * (x & 1))
                         : make_uint4(0, 0, 0, 0);
-      for (const uint32_t y : {u[x].x, u[x].y, u[x].z, u[x].w})
-        top = max(top, max(y & 0x7fff0000u, (y & 0x7fffu) << 16));
+      const uint32_t y[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top = max(top, max(y[k] & 0x7fff0000u, (y[k] & 0x7fffu) << 16));
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -269,16 +296,16 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
       dst[x * 32] = make_uint4(h[0], h[1], h[2], h[3]);
     }
   }
-  __syncthreads();
+  __syncwarp();
 
-  float o[DT][NT][4], m[NT][2], l[NT][2], cs[NT][2];
+  float o[DT][NT][4], mx[NT][2], l[NT][2], cs[NT][2];
   int seen[NT][2];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = j * 8 + 2 * t + c;
-      m[j][c] = l[j][c] = 0.f;
+      mx[j][c] = l[j][c] = 0.f;
       cs[j][c] = factor[r] * (a.scale * kLog2e);
       seen[j][c] = min(s.seen(r, a.g), s.kv);
     }
@@ -288,19 +315,22 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[i][j][c] = 0.f;
-  const uint32_t q_at = smem_u32(smem + L::kQ) + lane * 16;
+  const uint32_t q_at = base + L::kQ + lane * 16;
   const int least = s.least;
 
 #pragma unroll 1
   for (int x = 0; x < slices; ++x) {
-    const float ke = q8::scale_of(kb), ve = q8::scale_of(vb);  // of this lane's key
+    const float ke = q8::scale_of(m.kb), ve = q8::scale_of(m.vb);  // of this lane's key
     cp_async_wait<0>();
     __syncwarp();
-    const uint32_t ks = ring + (x % NST) * 2 * L::kPart, vs = ks + L::kPart;
-    const int key0 = first + x * BN;
-    if (x + 1 < slices) fetch((x + 1) % NST);
+    const uint32_t ks = base + L::kRing + m.stage * 2 * L::kPart, vs = ks + L::kPart;
+    const int key0 = first + x * kSlice;
+    m.stage ^= 1;
+    if (x + 1 < slices) {
+      fetch<D, M>(a, s, m, base);
+      if (x + 2 < slices) look_ahead(a, m, by, by_off);
+    }
     cp_async_commit();
-    if (x + 2 < slices) look_ahead();
     // Scores of 32 keys with 8 NT rows.
     float sc[MT][NT][4];
 #pragma unroll
@@ -348,7 +378,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-          sc[i][j][c] = fmaf(sc[i][j][c] * (c < 2 ? k0 : k1), cs[j][c & 1], -m[j][c & 1]);
+          sc[i][j][c] = fmaf(sc[i][j][c] * (c < 2 ? k0 : k1), cs[j][c & 1], -mx[j][c & 1]);
     }
     const bool edge = key0 + kSlice > least;
     if (edge) {
@@ -382,7 +412,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
           for (int w = 4; w < 32; w *= 2) up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, w));
           if (up == -INFINITY) up = 0.f;
           const float fix = x == 0 ? 0.f : ex2_approx(-up);
-          m[j][c] += up;
+          mx[j][c] += up;
           l[j][c] *= fix;
 #pragma unroll
           for (int i = 0; i < DT; ++i) {
@@ -454,132 +484,147 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, uin
       }
     }
   }
-  __syncthreads();  // nobody reads a ring any more
-  // The warps' sums meet in shared memory: [warp][8 NT][kLine]. Column d is at d with
-  // its bits 1 and 2 turned by its bits 5 and 6, so that the eight lanes of a row
-  // find different banks.
-  float *all = reinterpret_cast<float *>(smem + L::kRing);
-  float2 *ml = reinterpret_cast<float2 *>(smem + L::kMl);
-  constexpr int R = 8 * NT;
-  const auto turned = [](int d) { return d ^ ((d >> 4) & 6); };
+  // The next segment's first slice, then this one's sums: lane (g, t) has 16 columns (8
+  // for heads of 64) of the rows 8 j + 2 t and the one behind.
+  if (place_of.more) {
+    begin_stream(a, place_of.next, m);
+    if (m.slices > 0) fetch<D, M>(a, place_of.next, m, base);
+    cp_async_commit();
+  }
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int r = warp * R + j * 8 + 2 * t + c;
+      const int r = j * 8 + 2 * t + c;
 #pragma unroll
       for (int w = 4; w < 32; w *= 2) l[j][c] += __shfl_xor_sync(0xffffffffu, l[j][c], w);
-      if (g == 0) ml[r] = make_float2(l[j][c] == 0.f ? -INFINITY : m[j][c], l[j][c]);
+      if (r >= s.rows) continue;
+      const float sum = l[j][c], top = sum == 0.f ? -INFINITY : mx[j][c];
+      constexpr int C = D == 64 ? 8 : 16;  // columns side by side
+      if (!part) {
+        const RowAt w = row_at(a, s.row0, s.r0, s.h, r);
+        const float inv = sum == 0.f ? 0.f : kValueUnit<F> / sum;
+        __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(a.out) +
+                            (w.token * a.Hq + w.head) * D + C * g;
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        const int d = D == 64 ? 8 * g + 2 * i : 16 * (g + 8 * (i >> 3)) + 2 * (i & 7);
-        *reinterpret_cast<float2 *>(all + r * L::kLine + turned(d)) =
-            make_float2(o[i][j][c], o[i][j][c + 2]);
+        for (int y = 0; y < DT * 2 / 8; ++y) {
+          uint32_t u[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            u[k] = bits(__floats2bfloat162_rn(o[y * 4 + k][j][c] * inv,
+                                              o[y * 4 + k][j][c + 2] * inv));
+          *reinterpret_cast<uint4 *>(to + (y >> 1) * 128 + (y & 1) * 8) =
+              make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        if (g == 0 && a.lse)
+          a.lse[w.token * a.Hq + w.head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      } else {
+        if (g == 0) {
+          part[r] = top;
+          part[M + r] = sum;
+        }
+        float *to = part + 2 * M + r * D + C * g;
+#pragma unroll
+        for (int y = 0; y < DT / 2; ++y)
+          *reinterpret_cast<float4 *>(to + (y >> 2) * 128 + (y & 3) * 4) = make_float4(
+              o[y * 2][j][c] * kValueUnit<F>, o[y * 2][j][c + 2] * kValueUnit<F>,
+              o[y * 2 + 1][j][c] * kValueUnit<F>, o[y * 2 + 1][j][c + 2] * kValueUnit<F>);
       }
     }
-  __syncthreads();
-  const bool whole = s.whole();
-  float *part = whole ? nullptr : a.part + note_partial(a, s, cta, seg) * part_floats(M, D);
-  for (int x = tid; x < s.rows * (D / 8); x += kThreads) {
-    const int r = x / (D / 8), col = x % (D / 8) * 8;
-    float mx = -INFINITY, sum = 0.f, v[8] = {};
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) mx = fmaxf(mx, ml[k * R + r].x);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-      const float2 e = ml[k * R + r];
-      const float w = ex2_approx(e.x - ref), f = kValueUnit<F> * w;
-      sum = fmaf(e.y, w, sum);
-#pragma unroll
-      for (int c = 0; c < 8; c += 2) {
-        const float2 y =
-            *reinterpret_cast<const float2 *>(all + (k * R + r) * L::kLine + turned(col + c));
-        v[c] = fmaf(y.x, f, v[c]);
-        v[c + 1] = fmaf(y.y, f, v[c + 1]);
-      }
-    }
-    if (whole) {
-      const RowAt w = row_at(a, s.row0, s.r0, s.h, r);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint4 u;
-      u.x = bits(__floats2bfloat162_rn(v[0] * inv, v[1] * inv));
-      u.y = bits(__floats2bfloat162_rn(v[2] * inv, v[3] * inv));
-      u.z = bits(__floats2bfloat162_rn(v[4] * inv, v[5] * inv));
-      u.w = bits(__floats2bfloat162_rn(v[6] * inv, v[7] * inv));
-      *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) +
-                                 (w.token * a.Hq + w.head) * D + col) = u;
-      if (col == 0 && a.lse)
-        a.lse[w.token * a.Hq + w.head] = sum == 0.f ? -INFINITY : (mx + log2f(sum)) * kLn2;
-    } else {
-      if (col == 0) {
-        part[r] = mx;
-        part[M + r] = sum;
-      }
-      float4 *dst = reinterpret_cast<float4 *>(part + 2 * M + r * D + col);
-      dst[0] = make_float4(v[0], v[1], v[2], v[3]);
-      dst[1] = make_float4(v[4], v[5], v[6], v[7]);
-    }
-  }
 }
 
+// CTAs of an SM.
+template <int D, int M>
+constexpr int kPerSm = D == 256 ? 1 : M == 8 ? 3 : 2;
+
+// Every warp has a share of the work of its own (a CTA is no more than its four warps):
+// a unit is worked on by one warp from end to end, in 32 keys at a time, but where shares
+// meet. Nothing waits for another warp.
 template <int D, int F, int M>
-__global__ void __launch_bounds__(kThreads, M == 16 && D <= 128 ? 3 : D <= 128 ? 2 : 1)
-    attend_q8_few_kernel(Args a) {
+__global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(Args a) {
+  using L = Few<D, M>;
   extern __shared__ __align__(128) uint8_t smem[];
-  const int cta = blockIdx.x, ctas = gridDim.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int worker = blockIdx.x * kWarps + warp, workers = gridDim.x * kWarps;
   if (a.rows_upto < INT32_MAX) let_next_start();  // the kernel for many rows
-  clear_notes(a, cta);
-  clear_spare_rows<__nv_bfloat16, D, kThreads>(a, cta, ctas);
-  if (cta == ctas - 1) report_requests(a);
-  Walk<M, BN> walk{find_share<kThreads>(a, M, cta, ctas, reinterpret_cast<int64_t *>(smem))};
-  Segment s;
-  for (int seg = 0; walk.next(a, &s); ++seg) {
-    if (s.rows <= 8)
-      few_segment<D, F, M, 1>(a, s, smem, cta, seg);
+  if (lane < 2) a.desc[worker * 2 + lane] = {0, 0, 0, 0, 0, 0, 0, 0};
+  clear_spare_rows<__nv_bfloat16, D, kThreads>(a, blockIdx.x, gridDim.x);
+  if (blockIdx.x == gridDim.x - 1) report_requests(a);
+  const Share share = find_share<kThreads, kWarps>(a, M, worker, workers,
+                                                   reinterpret_cast<int64_t *>(smem));
+  __syncthreads();  // the scratch is the rings' place
+  uint8_t *mine = smem + warp * L::kWarpBytes;
+  Place<M> &p = *reinterpret_cast<Place<M> *>(mine + L::kPlace);
+  if (lane == 0) p.walk = Walk<M, BN>(share);
+  p.step(a);
+  Stream m;
+  m.stage = 0;
+  if (p.more) {
+    begin_stream(a, p.next, m);
+    if (m.slices > 0) fetch<D, M>(a, p.next, m, smem_u32(mine));
+    cp_async_commit();
+  }
+  for (int seg = 0; p.more; ++seg) {
+    const Segment s = p.next;
+    __syncwarp();
+    p.step(a);
+    float *part = nullptr;
+    if (!s.whole()) {
+      const int64_t slot = worker * 2 + (seg ? 1 : 0);
+      if (lane == 0) a.desc[slot] = {s.i, s.h, s.rt, s.t0, s.t1, s.tiles, 0, 0};
+      part = a.part + slot * part_floats(M, D);
+    }
+    if (M == 8 || s.rows <= 8)
+      few_segment<D, F, M, 1>(a, s, m, p, mine, part);
     else if (M == 16 || s.rows <= 16)
-      few_segment<D, F, M, 2>(a, s, smem, cta, seg);
+      few_segment<D, F, M, M < 16 ? 1 : 2>(a, s, m, p, mine, part);
     else if (s.rows <= 24)
-      few_segment<D, F, M, M / 8 < 3 ? 1 : 3>(a, s, smem, cta, seg);
+      few_segment<D, F, M, M < 24 ? 1 : 3>(a, s, m, p, mine, part);
     else
-      few_segment<D, F, M, M / 8>(a, s, smem, cta, seg);
+      few_segment<D, F, M, M < 32 ? 1 : 4>(a, s, m, p, mine, part);
+    __syncwarp();  // all lanes have seen `more`
   }
   let_next_start();
 }
 
 template <int D, int F, int M>
-pair_status run_few(Launch *l, cudaStream_t s) {
+pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   Args &a = l->a;
-  constexpr int smem = Few<D, M>::kBytes, per_sm = M == 16 && D <= 128 ? 3 : D <= 128 ? 2 : 1;
-  static_assert(per_sm * (smem + 1024) <= 233472, "shared memory of an SM");
-  static_assert(M <= kFewTile, "partial sums fit in the workspace");
+  constexpr int smem = Few<D, M>::kBytes;
+  static_assert(kPerSm<D, M> * (smem + 1024) <= 233472, "shared memory of an SM");
   const auto kernel = attend_q8_few_kernel<D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  a.unit_cost = 192;
+  a.unit_cost = 96;
   a.narrow = true;
   for (const pair_cache_strides *x : {&a.ks, &a.vs, &a.kes, &a.ves})
     a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
-  const int ctas = useful_ctas(a, M, min(kMaxCtas, per_sm * sm_count()));
+  const int fit = min(slots * (kFewTile / M) / 2,  // two partial sums each
+                      min(kMaxWorkers, kPerSm<D, M> * kWarps * sm_count()));
+  const int ctas =
+      (int)ceil_div(useful_ctas(a, M, fit / kWarps * kWarps, kMinWarp), kWarps);
   PAIR_BEGIN("attend_q8_few", s);
   kernel<<<ctas, kThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
   l->M = M;
-  l->ctas = ctas;
+  l->ctas = ctas * kWarps;
   return PAIR_OK;
 }
 
 template <int F>
-pair_status run_few(Launch *l, int D, int64_t most_rows, cudaStream_t s) {
-  const bool small = most_rows <= 16;
-  if (D == 64) return small ? run_few<64, F, 16>(l, s) : run_few<64, F, 32>(l, s);
-  if (D == 128) return small ? run_few<128, F, 16>(l, s) : run_few<128, F, 32>(l, s);
-  return run_few<256, F, 16>(l, s);
+pair_status run_few(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s) {
+  if (D == 64)
+    return most_rows <= 8 ? run_few<64, F, 8>(l, slots, s) : run_few<64, F, 32>(l, slots, s);
+  if (D == 128)
+    return most_rows <= 8 ? run_few<128, F, 8>(l, slots, s) : run_few<128, F, 32>(l, slots, s);
+  return run_few<256, F, 16>(l, slots, s);
 }
 
 }  // namespace
 
-pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, cudaStream_t s) {
-  return fmt == kI8 ? run_few<kI8>(l, D, most_rows, s) : run_few<kE4M3>(l, D, most_rows, s);
+pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, int slots,
+                          cudaStream_t s) {
+  return fmt == kI8 ? run_few<kI8>(l, D, most_rows, slots, s)
+                    : run_few<kE4M3>(l, D, most_rows, slots, s);
 }
 
 }  // namespace attend
