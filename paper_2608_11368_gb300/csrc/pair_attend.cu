@@ -553,20 +553,24 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
   const bool simt = dt == PAIR_F32;
-  const bool only_few = simt || held || most_rows <= kFewRows || !many_applies(a, D);
+  const bool only_few = simt || most_rows <= kFewRows ||
+                        !(held ? many_applies_q8(a, D) : many_applies(a, D));
   if (!only_few && R > 1) {
     few.a.rows_upto = kFewRows;
     many.a.rows_over = kFewRows;
   }
   pair_status st = PAIR_OK;
-  if (simt) st = launch_simt(&few, D, fmt, s);
-  else if (held)
-    st = launch_few_q8(&few, D, fmt, most_rows,
-                       (int)(((only_few ? reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need)
-                                        : many.a.part) - few.a.part) / part_floats(kFewTile, D)),
-                       s);
-  else if (only_few || R > 1) st = launch_few(&few, D, s);
-  if (st == PAIR_OK && !only_few) st = launch_many(&many, D, s);
+  if (simt) {
+    st = launch_simt(&few, D, fmt, s);
+  } else if (held && (only_few || R > 1)) {
+    const float *end = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need);
+    const int64_t room = (only_few ? end : many.a.part) - few.a.part;
+    st = launch_few_q8(&few, D, fmt, most_rows, (int)(room / part_floats(kFewTile, D)), s);
+  } else if (only_few || R > 1) {
+    st = launch_few(&few, D, s);
+  }
+  if (st == PAIR_OK && !only_few)
+    st = held ? launch_many_q8(&many, D, fmt, s) : launch_many(&many, D, s);
   return st == PAIR_OK ? launch_join(few, many, D, dt, s) : st;
 }
 

@@ -403,6 +403,8 @@ pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, int slot
                           cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);
+bool many_applies_q8(const Args &a, int D);
+pair_status launch_many_q8(Launch *l, int D, int fmt, cudaStream_t s);
 int sm_count();
 int useful_ctas(const Args &a, int M, int fit, int least = kMinKeys);
 
