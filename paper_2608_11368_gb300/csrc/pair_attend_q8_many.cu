@@ -3,10 +3,9 @@
 //
 // A code times its row's power of two is a bf16 number, so a tile of stored values is
 // exact and the products, the softmax and the epilogue are those over a bf16 cache. A
-// former copies its rows' codes into shared memory (16 bytes per lane, asynchronously),
-// one tile ahead; a lane then reads what it copied itself, so nobody waits for
-// anybody's copy, forms 16 numbers of a piece (five instructions for four whole
-// numbers, ten for four of e4m3) and stores them where the products read them.
+// former reads 16 codes per lane out of shared memory, where TMA brings a tile of them,
+// forms the numbers (five instructions for four whole ones, ten for four of e4m3) and
+// stores them where the products read them.
 #include <cuda_fp16.h>
 
 #include "pair_attend_tc.cuh"
@@ -19,33 +18,52 @@ using q8::kE4M3;
 using q8::kI8;
 
 // CTA: warps 0-3 and 4-7 the softmax of a tile of 128 rows each, warp 9 the MMA issuer, warp
-// 8 the scout, which finds the pages, warps 10 to 15 the formers. Registers: 200 x 256 + 56
+// 8 the scout, which finds the pages, warps 10 to 15 the formers. Registers: 192 x 256 + 64
 // x 256 of the 128 x 512 that the block is launched with.
 constexpr int kThreadsQ8 = 512;
 constexpr int kFormers = 6;
 constexpr int kOctets = BN / 8;  // of 8 keys, which lie in one page
 
-// What a former has to know of a tile: where its keys and values lie.
+// A warp's way along the CTA's share, in shared memory, stepped by its lane 0: registers
+// are short.
+struct Way {
+  Walk<M, BN> walk;
+  Segment s;
+  bool more;
+};
+struct SharedWalk {
+  Way &way;
+  __device__ __forceinline__ bool next(const Args &a, Segment *s) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) way.more = way.walk.next(a, &way.s);
+    __syncwarp();
+    *s = way.s;
+    return way.more;
+  }
+};
+
+// What a former has to know of a tile beside its codes.
 struct Info {
-  const uint8_t *src[kOctets][2];  // first row of each octet, keys and values
-  uint8_t exps[2][BN];
-  int32_t unseen, nk;  // keys that some row does not see, that do not exist: from here on
-  int32_t more;        // there is a tile
+  uint8_t exps[2][BN];  // of keys, of values
+  int32_t unseen, nk;   // keys that some row does not see, that do not exist: from here on
+  int32_t more;         // there is a tile
 };
 
 template <int D>
 struct SmemQ8 {
+  static constexpr bool kLean = true;  // waits of the issuer
   static constexpr int kKeyStages = 2, kValueStages = 2;  // rings of tiles
   uint8_t q[2][Tc<D>::kTile];
   uint8_t k[kKeyStages][Tc<D>::kTile];
   uint8_t v[kValueStages][Tc<D>::kTile];
-  uint4 codes[2][BN * D / 16];  // of the next tile of keys, of values
+  uint8_t codes[2][BN * D];  // of the next tile of keys, of values
   Info info[2];
   uint64_t k_full[kKeyStages], k_empty[kKeyStages];
   uint64_t looked[kValueStages], v_empty[kValueStages];
-  uint64_t info_full[2], info_empty[2];
+  uint64_t info_full[2], info_empty[2], codes_full[2], codes_empty[2];
   uint64_t done, q_full[2], s_full[2], p_ready[2][2], pv_done[2];
   int64_t scratch[kThreadsQ8 / 32 + 2];
+  Way way[2];  // the scout's and the issuer's
   uint32_t tmem;
   int abort, any_bad;
 };
@@ -55,6 +73,30 @@ __device__ __forceinline__ uint32_t bits(__nv_bfloat162 x) {
 }
 __device__ __forceinline__ __nv_bfloat162 bf2_of(uint32_t x) {
   return *reinterpret_cast<const __nv_bfloat162 *>(&x);
+}
+
+__device__ __forceinline__ uint32_t ld_shared32(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ uint32_t ld_shared8(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ uint4 ld_shared128(uint32_t at) {
+  uint4 u;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+               : "r"(at)
+               : "memory");
+  return u;
+}
+__device__ __forceinline__ void st_shared128(uint32_t at, uint32_t x, uint32_t y, uint32_t z,
+                                             uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
 }
 
 // Tiles hold the stored values over kHeldUnit, so that a whole number takes one
@@ -100,25 +142,31 @@ __device__ __forceinline__ uint2 form4(uint32_t w, uint32_t f, uint32_t g) {
   return x;
 }
 
-// Warp 8: the pages of every tile, two tiles ahead of the formers at most. Lanes 0 to 15
-// look up an octet each, all of them the exponents of four keys and values.
+// Warp 8: brings the codes of every tile into shared memory by TMA, a box of tokens of one
+// page per lane, and the exponents of its keys and values.
 template <int D>
-__device__ void scout(const Args &a, SmemQ8<D> &sm, Walk<M, BN> walk) {
+__device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk walk) {
   const int lane = threadIdx.x & 31;
-  volatile int *abort = &sm.abort;
+  const auto wait = [&](uint64_t *bar, uint32_t phase) {
+    const bool ok = wait_lean(smem_u32(bar), phase, smem_u32(&sm.abort), a.dev_err);
+    return __all_sync(0xffffffffu, ok);
+  };
   Ring<2> ring;
+  Ring<1> codes;
   Segment s;
-  const int by = BN / a.page, by_off = BN - by * a.page;
+  const int box = maps.box, by = BN / a.page, by_off = BN - by * a.page;
+  const int box_bits = __ffs(box) - 1;
+  const bool mine = lane * box < BN;
   bool ok = true;
   while (ok && walk.next(a, &s)) {
     const int32_t *table = a.table + (int64_t)s.i * a.width;
-    int key = s.t0 * BN + (lane & 15) * 8, at = key / a.page, off = key - at * a.page;
-    int id = key < s.keys ? table[at] : 0;
+    int key = s.t0 * BN + lane * box, at = key / a.page, off = key - at * a.page;
+    int id = mine && key < s.keys ? table[at] : 0;
     for (int t = s.t0; t < s.t1; ++t) {
-      const bool there = key < s.keys;
+      const bool load = mine && key < s.keys;
       int pg = id;
       const int o = off;
-      if (there && (unsigned)pg >= (unsigned)a.num_pages) {
+      if (load && (unsigned)pg >= (unsigned)a.num_pages) {
         flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
         pg = 0;
       }
@@ -130,29 +178,39 @@ __device__ void scout(const Args &a, SmemQ8<D> &sm, Walk<M, BN> walk) {
         off -= a.page;
         ++at;
       }
-      if (t + 1 < s.t1) id = key < s.keys ? table[at] : 0;
+      if (t + 1 < s.t1) id = mine && key < s.keys ? table[at] : 0;
+      const int boxes = __popc(__ballot_sync(0xffffffffu, load));
+      auto bring = [&](int kv) {
+        if (!wait(&sm.codes_empty[kv], codes.phase ^ 1)) return false;
+        if (lane == 0) mbar_expect_tx(&sm.codes_full[kv], boxes * box * D);
+        __syncwarp();
+        if (load) {
+          const int8_t *where = kv ? maps.v_at : maps.k_at;
+          const int c1 = where[0] == 1 ? pg : where[1] == 1 ? o : s.h;
+          const int c2 = where[0] == 2 ? pg : where[1] == 2 ? o : s.h;
+          const int c3 = where[0] == 3 ? pg : where[1] == 3 ? o : s.h;
+          tma_load_4d(sm.codes[kv] + lane * box * D, kv ? &maps.v : &maps.k, &sm.codes_full[kv],
+                      0, c1, c2, c3);
+        }
+        return true;
+      };
+      if (!(ok = bring(0))) break;
       const int nk = min(BN, s.keys - t * BN);
       uint32_t e[2] = {0, 0};
 #pragma unroll
       for (int x = 0; x < 4; ++x) {  // keys lane + 32 x
-        const int from = (lane >> 3) + 4 * x;
+        const int k = lane + 32 * x, from = k >> box_bits, in = k & (box - 1);
         const int p = __shfl_sync(0xffffffffu, pg, from), q = __shfl_sync(0xffffffffu, o, from);
-        uint32_t k = 127, v = 127;
-        if (lane + 32 * x < nk) {
-          k = __ldg(a.ke + cache_row(a, a.kes, p, q + (lane & 7), s.h));
-          v = __ldg(a.ve + cache_row(a, a.ves, p, q + (lane & 7), s.h));
+        uint32_t eb = 127, vb = 127;
+        if (k < nk) {
+          eb = __ldg(a.ke + cache_row(a, a.kes, p, q + in, s.h));
+          vb = __ldg(a.ve + cache_row(a, a.ves, p, q + in, s.h));
         }
-        e[0] |= k << 8 * x;
-        e[1] |= v << 8 * x;
+        e[0] |= eb << 8 * x;
+        e[1] |= vb << 8 * x;
       }
-      if (!(ok = warp_wait(&sm.info_empty[ring.stage], ring.phase ^ 1, abort, a.dev_err))) break;
+      if (!(ok = wait(&sm.info_empty[ring.stage], ring.phase ^ 1))) break;
       Info &info = sm.info[ring.stage];
-      if (lane < kOctets) {
-        info.src[lane][0] = static_cast<const uint8_t *>(a.kc) +
-                            (there ? cache_row(a, a.ks, pg, o, s.h) : 0);
-        info.src[lane][1] = static_cast<const uint8_t *>(a.vc) +
-                            (there ? cache_row(a, a.vs, pg, o, s.h) : 0);
-      }
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
@@ -164,11 +222,23 @@ __device__ void scout(const Args &a, SmemQ8<D> &sm, Walk<M, BN> walk) {
       }
       warp_arrive(&sm.info_full[ring.stage]);
       ring.step();
+      if (!(ok = bring(1))) break;
+      codes.step();
     }
   }
-  if (ok && warp_wait(&sm.info_empty[ring.stage], ring.phase ^ 1, abort, a.dev_err)) {
+  if (ok && wait(&sm.info_empty[ring.stage], ring.phase ^ 1)) {
     if (lane == 0) sm.info[ring.stage].more = 0;
     warp_arrive(&sm.info_full[ring.stage]);
+  }
+  // Nothing may still be on its way into shared memory when the CTA ends. On the regular
+  // path all codes have been consumed; after an abort the last ones are waited for, each
+  // barrier's latest use that was begun.
+  if (!ok) {
+    volatile int never = 0;
+    for (int kv = 0; kv < 2; ++kv) {
+      wait_limit(&sm.codes_full[kv], codes.phase ^ 1, &never, a.dev_err, 10000000);
+      wait_limit(&sm.codes_full[kv], codes.phase, &never, a.dev_err, 10000000);
+    }
   }
 }
 
@@ -182,105 +252,112 @@ struct Former {
   SmemQ8<D> &sm;
   const int w, lane;
 
-  // The codes of a tile, zeros where there is no key.
-  __device__ __forceinline__ void copy(int kv, const Info &info) {
-    const int64_t step = (lane & 7) * (kv ? a.vs : a.ks).for_token + (lane >> 3) * 16;
-    const uint32_t dst = smem_u32(&sm.codes[kv][w * PP * 32 + lane]);
-#pragma unroll
-    for (int o = 0; o < kOwn; ++o) {
-      const int octet = o * kFormers + w;
-      if (octet >= kOctets) continue;
-      const bool there = octet * 8 + (lane & 7) < info.nk;
-      const uint8_t *src = info.src[octet][kv] + (there ? step : 0);
-#pragma unroll
-      for (int y = 0; y < PP; ++y)
-        cp_async16(dst + (o * kFormers * PP + y) * 512, src + (there ? y * 64 : 0), there);
-    }
-    cp_async_commit();
+  __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t phase) {
+    const bool ok = wait_lean(smem_u32(bar), phase, smem_u32(&sm.abort), a.dev_err);
+    return __all_sync(0xffffffffu, ok);
   }
-  // Forms a tile out of its codes. (The same code for keys and values: it has to fit in
-  // the instruction caches beside the softmax's.)
-  __device__ __forceinline__ void put(int kv, uint8_t *to, const Info &info) {
-    const int c = (lane >> 3) * 2, r7 = lane & 7;
-    uint8_t *row = to + (w * 8 + r7) * 128;
-    const uint32_t c0 = (c ^ r7) << 4, c1 = ((c + 1) ^ r7) << 4;
-    const uint4 *codes = &sm.codes[kv][w * PP * 32 + lane];
-    const uint8_t *exps = &info.exps[kv][w * 8 + r7];
-#pragma unroll 1
-    for (int o = w; o < kOctets; o += kFormers, codes += kFormers * PP * 32,
-             row += kFormers * 8 * 128, exps += kFormers * 8) {
-      uint4 u[PP];
+  // Stores a piece's 16 numbers: chunks c and c + 1, c = 2 (lane / 8), of an atom's row at
+  // `at` (turned by the row).
+  template <bool rest>
+  __device__ __forceinline__ void form(uint32_t at, const uint4 &u, uint32_t fg, uint32_t more) {
+    const uint32_t f = __byte_perm(fg, 0, 0x1010), g = __byte_perm(fg, 0, 0x3232);
+    uint2 x[4] = {form4<F>(u.x, f, g), form4<F>(u.y, f, g), form4<F>(u.z, f, g),
+                  form4<F>(u.w, f, g)};
+    if (rest) {
 #pragma unroll
-      for (int y = 0; y < PP; ++y) u[y] = codes[y * 32];
-      const uint32_t b = *exps;
-      uint32_t fg = factor_of<F>(b);
-      if (kv && b == 255 && o * 8 + r7 >= info.unseen) {  // zero times NaN is NaN
-        fg = 0;
-        *reinterpret_cast<volatile int *>(&sm.any_bad) = 1;
-      }
-      const uint32_t f = __byte_perm(fg, 0, 0x1010), g = __byte_perm(fg, 0, 0x3232);
-      const bool beyond = __any_sync(0xffffffffu, b > kMost<F>);
-#pragma unroll
-      for (int y = 0; y < PP; ++y) {
-        // Piece lane / 8 + 4 y of 16 columns: chunks 2 (lane / 8) and the next of atom y.
-        uint2 x[4] = {form4<F>(u[y].x, f, g), form4<F>(u[y].y, f, g), form4<F>(u[y].z, f, g),
-                      form4<F>(u[y].w, f, g)};
-        if (beyond) {
-          const uint32_t rest = rest_of<F>(b);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            x[k] = make_uint2(bits(__hmul2(bf2_of(x[k].x), bf2_of(rest))),
-                              bits(__hmul2(bf2_of(x[k].y), bf2_of(rest))));
-        }
-        *reinterpret_cast<uint4 *>(row + y * C::kAtom + c0) =
-            make_uint4(x[0].x, x[0].y, x[1].x, x[1].y);
-        *reinterpret_cast<uint4 *>(row + y * C::kAtom + c1) =
-            make_uint4(x[2].x, x[2].y, x[3].x, x[3].y);
-      }
+      for (int k = 0; k < 4; ++k)
+        x[k] = make_uint2(bits(__hmul2(bf2_of(x[k].x), bf2_of(more))),
+                          bits(__hmul2(bf2_of(x[k].y), bf2_of(more))));
     }
-    fence_async_smem();
+    st_shared128(at, x[0].x, x[0].y, x[1].x, x[1].y);
+    st_shared128(at ^ 16, x[2].x, x[2].y, x[3].x, x[3].y);
   }
 
   __device__ void run() {
-    volatile int *abort = &sm.abort;
-    Ring<2> at, next;  // the tile's place in the rings (all of two stages), the next one's
-    bool ok = warp_wait(&sm.info_full[0], 0, abort, a.dev_err);
-    bool more = ok && sm.info[0].more;
-    if (more) {
-      copy(0, sm.info[0]);
-      copy(1, sm.info[0]);
-    }
-    while (more) {
-      const Info &info = sm.info[at.stage];
-      if (!warp_wait(&sm.k_empty[at.stage], at.phase ^ 1, abort, a.dev_err)) break;
-      cp_async_wait<1>();
-      put(0, sm.k[at.stage], info);
-      warp_arrive(&sm.k_full[at.stage]);
-      next = at;
-      next.step();
-      if (!warp_wait(&sm.info_full[next.stage], next.phase, abort, a.dev_err)) break;
-      more = sm.info[next.stage].more;
-      if (more)
-        copy(0, sm.info[next.stage]);
-      else
-        cp_async_commit();
-      if (!warp_wait(&sm.v_empty[at.stage], at.phase ^ 1, abort, a.dev_err)) break;
-      cp_async_wait<1>();
-      put(1, sm.v[at.stage], info);
-      warp_arrive(&sm.looked[at.stage]);
+    Ring<2> at;  // the tile's place in the rings of two stages
+    Ring<1> codes;
+    const uint32_t infos = smem_u32(&sm.info[0]);
+    const int r7 = lane & 7, p = lane >> 3;
+    const bool last = w + (kOwn - 1) * kFormers < kOctets;  // has as many octets as others
+#pragma unroll 1
+    while (true) {
+      const uint32_t info = infos + at.stage * sizeof(Info);
+      if (!wait(&sm.info_full[at.stage], at.phase)) return;
+      if (ld_shared32(info + offsetof(Info, more)) == 0) return;
+      // (The same code for keys and values: it has to fit in the instruction caches
+      // beside the softmax's.)
+#pragma unroll 1
+      for (int kv = 0; kv < 2; ++kv) {
+        uint32_t fg[kOwn], b[kOwn];
+        bool beyond = false;
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+          const int key = min(o * kFormers + w, kOctets - 1) * 8 + r7;
+          b[o] = ld_shared8(info + offsetof(Info, exps) + kv * BN + key);
+        }
+        // Codes as TMA's swizzle has placed them: of 128 bytes a row's pieces are turned by
+        // the row, of 64 by half of it.
+        if (!wait(&sm.codes_full[kv], codes.phase)) return;
+        uint4 u[kOwn][PP];
+        const uint32_t from = smem_u32(sm.codes[kv]) + (w * 8 + r7) * D;
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o)
+#pragma unroll
+          for (int y = 0; y < PP; ++y)
+            if (o < kOwn - 1 || last)
+              u[o][y] = ld_shared128(from + o * kFormers * 8 * D +
+                                     ((p + 4 * y) ^ (D == 64 ? r7 >> 1 : r7)) * 16);
+#pragma unroll
+        for (int o = 0; o < kOwn; ++o) {
+          fg[o] = factor_of<F>(b[o]);
+          beyond |= b[o] > kMost<F>;
+        }
+        if (kv) {
+          // No row's value must meet a weight of 0 as NaN, nor be what was there before.
+          const int unseen = ld_shared32(info + offsetof(Info, unseen));
+          if (unseen < BN) {
+            const int nk = ld_shared32(info + offsetof(Info, nk));
+#pragma unroll
+            for (int o = 0; o < kOwn; ++o) {
+              const int key = (o * kFormers + w) * 8 + r7;
+              const bool bad = b[o] == 255 && key >= unseen;
+              if (bad) *reinterpret_cast<volatile int *>(&sm.any_bad) = 1;
+              if (bad || key >= nk) fg[o] = 0;
+            }
+          }
+        }
+        if (!wait(kv ? &sm.v_empty[at.stage] : &sm.k_empty[at.stage], at.phase ^ 1)) return;
+        warp_arrive(&sm.codes_empty[kv]);
+        const uint32_t to = smem_u32(kv ? sm.v[0] : sm.k[0]) + at.stage * C::kTile +
+                            (w * 8 + r7) * 128 + ((2 * p ^ r7) << 4);
+        if (!__any_sync(0xffffffffu, beyond)) {
+#pragma unroll
+          for (int o = 0; o < kOwn; ++o)
+#pragma unroll
+            for (int y = 0; y < PP; ++y)
+              if (o < kOwn - 1 || last)
+                form<false>(to + y * C::kAtom + o * (kFormers * 8 * 128), u[o][y], fg[o], 0);
+        } else {
+#pragma unroll
+          for (int o = 0; o < kOwn; ++o)
+#pragma unroll
+            for (int y = 0; y < PP; ++y)
+              if (o < kOwn - 1 || last)
+                form<true>(to + y * C::kAtom + o * (kFormers * 8 * 128), u[o][y], fg[o],
+                           rest_of<F>(b[o]));
+        }
+        fence_async_smem();
+        warp_arrive(kv ? &sm.looked[at.stage] : &sm.k_full[at.stage]);
+      }
       warp_arrive(&sm.info_empty[at.stage]);
-      if (more)
-        copy(1, sm.info[next.stage]);
-      else
-        cp_async_commit();
-      at = next;
+      at.step();
+      codes.step();
     }
-    cp_async_wait<0>();  // nothing is on its way into shared memory when the CTA ends
   }
 };
 
 template <int D, int F>
-__global__ void __launch_bounds__(kThreadsQ8, 1) attend_q8_many_kernel(Args a) {
+__global__ void __launch_bounds__(kThreadsQ8, 1) attend_q8_many_kernel(Args a, const __grid_constant__ Maps maps) {
   extern __shared__ uint8_t raw[];
   SmemQ8<D> &sm = *reinterpret_cast<SmemQ8<D> *>(tck::align1k(raw));
   const int tid = threadIdx.x, warp = tid >> 5;
@@ -302,6 +379,8 @@ __global__ void __launch_bounds__(kThreadsQ8, 1) attend_q8_many_kernel(Args a) {
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sm.info_full[x], 1);
       mbar_init(&sm.info_empty[x], kFormers);
+      mbar_init(&sm.codes_full[x], 1);
+      mbar_init(&sm.codes_empty[x], kFormers);
     }
     mbar_init(&sm.done, 1);
     for (int w = 0; w < 2; ++w) {
@@ -314,23 +393,26 @@ __global__ void __launch_bounds__(kThreadsQ8, 1) attend_q8_many_kernel(Args a) {
     sm.abort = 0;
     sm.any_bad = 0;
     fence_mbar_init();
+    prefetch_tmap(&maps.k);
+    prefetch_tmap(&maps.v);
   }
   __syncwarp();
   if (warp == 9) tmem_alloc(&sm.tmem, 512);
   const Walk<M, BN> walk{find_share<kThreadsQ8>(a, M, cta, ctas, sm.scratch)};
+  if (tid == 0) sm.way[0].walk = sm.way[1].walk = walk;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 9)
-      issue<D>(a, sm, walk);
+      issue<D>(a, sm, SharedWalk{sm.way[1]});
     else if (warp == 8)
-      scout<D>(a, sm, walk);
+      scout<D>(a, maps, sm, SharedWalk{sm.way[0]});
     else
       Former<D, F>{a, sm, warp - 10, tid & 31}.run();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     softmax<D, F>(a, sm, walk, cta);
   }
   __syncwarp();
@@ -346,7 +428,7 @@ __global__ void __launch_bounds__(kThreadsQ8, 1) attend_q8_many_kernel(Args a) {
 }
 
 template <int D, int F>
-pair_status run_many(Launch *l, cudaStream_t s) {
+pair_status run_many(Launch *l, const Maps &maps, cudaStream_t s) {
   Args &a = l->a;
   a.unit_cost = kManyCost;
   constexpr int smem = sizeof(SmemQ8<D>) + 1024;
@@ -365,7 +447,7 @@ pair_status run_many(Launch *l, cudaStream_t s) {
   cfg.attrs = &attr;
   cfg.numAttrs = a.rows_over >= 0 ? 1 : 0;  // behind the launch for few rows
   PAIR_BEGIN("attend_q8_many", s);
-  if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, kernel, a, maps) != cudaSuccess) {
     cudaGetLastError();
     return PAIR_ERR_CUDA;
   }
@@ -377,11 +459,16 @@ pair_status run_many(Launch *l, cudaStream_t s) {
 
 }  // namespace
 
-bool many_applies_q8(const Args &a, int D) { return D <= 128 && a.page % 8 == 0; }
+bool many_applies_q8(const Args &a, int D) {
+  Maps maps;
+  return many_maps(a, D, 1, &maps);
+}
 
 pair_status launch_many_q8(Launch *l, int D, int fmt, cudaStream_t s) {
-  if (fmt == kI8) return D == 64 ? run_many<64, kI8>(l, s) : run_many<128, kI8>(l, s);
-  return D == 64 ? run_many<64, kE4M3>(l, s) : run_many<128, kE4M3>(l, s);
+  Maps maps;
+  if (!many_maps(l->a, D, 1, &maps)) return PAIR_ERR_CUDA;
+  if (fmt == kI8) return D == 64 ? run_many<64, kI8>(l, maps, s) : run_many<128, kI8>(l, maps, s);
+  return D == 64 ? run_many<64, kE4M3>(l, maps, s) : run_many<128, kE4M3>(l, maps, s);
 }
 
 }  // namespace attend

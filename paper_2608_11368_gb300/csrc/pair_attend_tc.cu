@@ -9,6 +9,7 @@ namespace {
 
 template <int D>
 struct Smem {
+  static constexpr bool kLean = false;
   static constexpr int kKeyStages = D == 64 ? 4 : 2;    // ring of key tiles
   static constexpr int kValueStages = D == 64 ? 4 : 3;  // ring of value tiles
   uint8_t q[2][Tc<D>::kTile];
@@ -22,21 +23,6 @@ struct Smem {
   uint32_t tmem;
   int abort, any_bad;
 };
-
-struct Maps {
-  CUtensorMap k, v;
-  int8_t k_at[3], v_at[3];  // dimension (1 to 3) of page, token, head
-  int box;                  // tokens of a box
-};
-
-__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x,
-                                            int y, int z, int w) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
-      : "memory");
-}
 
 // Keys (kv = 0) or values (1) of every tile, a box per lane. A warp each: the
 // 16 boxes of a tile of pages of 16 take some 1300 cycles to issue, and one warp
@@ -240,38 +226,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (a.rows_over >= 0) wait_for_previous();
 }
 
-// 4-D map of a cache, dimensions in the order of their strides: boxes of `box`
-// tokens x 64 columns of one page and head. False where no such map exists.
-bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args &a, int D, int box,
-               const pair_cache_strides &st) {
-  const auto fn = tck::encode_fn();
-  if (!fn) return false;
-  const int64_t stride[3] = {st.for_page * 2, st.for_token * 2, st.for_head * 2};
-  const cuuint64_t size[3] = {(cuuint64_t)a.num_pages, (cuuint64_t)a.page, (cuuint64_t)a.Hkv};
-  const cuuint32_t want[3] = {1, (cuuint32_t)box, 1};
-  int order[3] = {0, 1, 2};
-  for (int x = 0; x < 3; ++x)
-    for (int y = 0; y < 2; ++y)
-      if (stride[order[y + 1]] < stride[order[y]]) {
-        const int z = order[y];
-        order[y] = order[y + 1];
-        order[y + 1] = z;
-      }
-  cuuint64_t dims[4] = {(cuuint64_t)D}, strides[3];
-  cuuint32_t boxes[4] = {64}, ones[4] = {1, 1, 1, 1};
-  for (int x = 0; x < 3; ++x) {
-    const int64_t b = stride[order[x]];
-    if (b < 16 || b >= ((int64_t)1 << 40)) return false;
-    strides[x] = (cuuint64_t)b;
-    dims[x + 1] = size[order[x]];
-    boxes[x + 1] = want[order[x]];
-    at[order[x]] = (int8_t)(x + 1);
-  }
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(p), dims, strides, boxes,
-            ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int D>
 pair_status run_many(Launch *l, const Maps &maps, cudaStream_t s) {
   Args &a = l->a;
@@ -302,27 +256,16 @@ pair_status run_many(Launch *l, const Maps &maps, cudaStream_t s) {
   return PAIR_OK;
 }
 
-bool many_maps(const Args &a, int D, Maps *maps) {
-  // A box is the largest power of two of tokens, up to a tile, that divides
-  // the page; the swizzle's period is 8 rows.
-  int box = BN;
-  while (a.page % box != 0) box /= 2;
-  if (D > 128 || box < 8) return false;
-  maps->box = box;
-  return cache_map(&maps->k, maps->k_at, a.kc, a, D, box, a.ks) &&
-         cache_map(&maps->v, maps->v_at, a.vc, a, D, box, a.vs);
-}
-
 }  // namespace
 
 bool many_applies(const Args &a, int D) {
   Maps maps;
-  return many_maps(a, D, &maps);
+  return many_maps(a, D, 2, &maps);
 }
 
 pair_status launch_many(Launch *l, int D, cudaStream_t s) {
   Maps maps;
-  if (!many_maps(l->a, D, &maps)) return PAIR_ERR_CUDA;
+  if (!many_maps(l->a, D, 2, &maps)) return PAIR_ERR_CUDA;
   return D == 64 ? run_many<64>(l, maps, s) : run_many<128>(l, maps, s);
 }
 

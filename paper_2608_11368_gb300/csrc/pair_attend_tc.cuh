@@ -30,12 +30,55 @@ struct Tc {
   static constexpr uint32_t kIdescO = idesc_bf16(128, D, 0, 1);
 };
 
+struct Maps {
+  CUtensorMap k, v;
+  int8_t k_at[3], v_at[3];  // dimension (1 to 3) of page, token, head
+  int box;                  // tokens of a box
+};
+
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, uint64_t *bar, int x,
+                                            int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+
 // wait() by all lanes of a warp, which leave it together: a lane's poll can succeed
 // before another's, and the TMEM instructions (.aligned) want whole warps.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t phase, volatile int *abort,
                                           int32_t *dev_err) {
   const bool ok = wait(bar, phase, abort, dev_err);
   return __all_sync(0xffffffffu, ok);
+}
+
+// wait() with fewer registers: by the low word of the clock, on a barrier's and the abort
+// flag's addresses in shared memory.
+__device__ __forceinline__ bool wait_lean(uint32_t bar, uint32_t phase, uint32_t abort,
+                                          int32_t *dev_err) {
+  static_assert(kWaitCycles < (1ll << 32), "the limit in a word");
+  uint32_t t0 = 0, first = 1;
+  while (true) {
+    uint32_t ok, gone;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(phase)
+        : "memory");
+    if (ok) return true;
+    const uint32_t now = (uint32_t)clock();
+    if (first) t0 = now, first = 0;
+    asm volatile("ld.volatile.shared.b32 %0, [%1];" : "=r"(gone) : "r"(abort) : "memory");
+    if (gone) return false;
+    if (now - t0 > (uint32_t)kWaitCycles) {
+      asm volatile("st.volatile.shared.b32 [%0], %1;" ::"r"(abort), "r"(1) : "memory");
+      flag_error(dev_err, PAIR_DEV_ERR_TIMEOUT);
+      return false;
+    }
+  }
 }
 
 // A warp's arrival, for what its lanes have done (and fenced) before.
@@ -141,19 +184,24 @@ __device__ __forceinline__ bool edge_tile(const Segment &s, int t) {
 // Waits, each lane of the first `n` for a barrier and phase of its own: one poll
 // of several costs a warp as much as one. `ok`: what the lane's waits since the
 // last vote came to.
-__device__ __forceinline__ bool wait_lanes(int n, bool ok, uint64_t *bar, uint32_t phase,
-                                           volatile int *abort, int32_t *dev_err) {
-  if ((int)(threadIdx.x & 31) < n) ok &= wait(bar, phase, abort, dev_err);
+template <typename W>
+__device__ __forceinline__ bool wait_lanes(W wait, int n, bool ok, uint64_t *bar, uint32_t phase) {
+  if ((int)(threadIdx.x & 31) < n) ok &= wait(bar, phase);
   return __all_sync(0xffffffffu, ok);
 }
 
 // The warp votes on its waits once per step, in the first (a vote behind each of
 // them: 20 us of 374 for the four chunks); until then all lanes go the same way, and
 // products issued after a wait that gave up are of a call that has failed.
-template <int D, typename S>
-__device__ void issue(const Args &a, S &sm, Walk<M, BN> walk) {
+template <int D, typename S, typename W>
+__device__ void issue(const Args &a, S &sm, W walk) {
   using C = Tc<D>;
-  volatile int *abort = &sm.abort;
+  const auto wait = [&](uint64_t *bar, uint32_t phase) {
+    if constexpr (S::kLean)
+      return wait_lean(smem_u32(bar), phase, smem_u32(&sm.abort), a.dev_err);
+    else
+      return tc::wait(bar, phase, &sm.abort, a.dev_err);
+  };
   const uint64_t dq = sdesc_sw128(smem_u32(sm.q[0]), 16, 1024);
   const uint64_t dk = sdesc_sw128(smem_u32(sm.k[0]), 16, 1024);
   const uint64_t dv = sdesc_sw128(smem_u32(sm.v[0]), C::kAtom, 1024);
@@ -195,9 +243,9 @@ __device__ void issue(const Args &a, S &sm, Walk<M, BN> walk) {
   while (ok && walk.next(a, &s)) {
     if (s.t0 == s.t1) continue;
     const int top = s.rows > 128;  // the last active tile
-    ok &= wait(&sm.k_full[kr.stage], kr.phase, abort, a.dev_err);
+    ok &= wait(&sm.k_full[kr.stage], kr.phase);
     for (int w = 0; w <= top; ++w) {
-      ok &= wait(&sm.q_full[w], q_ph[w], abort, a.dev_err);
+      ok &= wait(&sm.q_full[w], q_ph[w]);
       q_ph[w] ^= 1;
       tc_fence_after();
       scores(w, kr.stage, w == top);
@@ -211,14 +259,14 @@ __device__ void issue(const Args &a, S &sm, Walk<M, BN> walk) {
                       : lane == 1 ? &sm.looked[vr.stage]
                                   : &sm.k_full[kr.stage];
       const uint32_t phase = lane == 0 ? p_ph[0] : lane == 1 ? vr.phase : kr.phase;
-      if (!(ok = wait_lanes(more ? 3 : 2, ok, bar, phase, abort, a.dev_err))) break;
-#pragma unroll
+      if (!(ok = wait_lanes(wait, more ? 3 : 2, ok, bar, phase))) break;
+#pragma unroll(S::kLean ? 1 : 2)
       for (int w = 0; w < 2; ++w) {
         if (w > top) break;
-        if (w) ok &= wait(&sm.p_ready[w][0], p_ph[w], abort, a.dev_err);
+        if (w) ok &= wait(&sm.p_ready[w][0], p_ph[w]);
         tc_fence_after();
         sums(w, vr.stage, 0, t == s.t0, false);
-        ok &= wait(&sm.p_ready[w][1], p_ph[w], abort, a.dev_err);
+        ok &= wait(&sm.p_ready[w][1], p_ph[w]);
         p_ph[w] ^= 1;
         tc_fence_after();
         sums(w, vr.stage, 1, false, w == top);
@@ -234,7 +282,7 @@ __device__ void issue(const Args &a, S &sm, Walk<M, BN> walk) {
   if (elect_one()) mma_commit(&sm.done);
   __syncwarp();
   volatile int never = 0;
-  wait(&sm.done, 0, &never, a.dev_err);
+  tc::wait(&sm.done, 0, &never, a.dev_err);
   __syncwarp();
 }
 
@@ -460,6 +508,51 @@ __device__ void softmax(const Args &a, S &sm, Walk<M, BN> walk, int cta) {
       a.lse[at.token * a.Hq + at.head] = l == 0.f ? -INFINITY : (m2 + log2f(l)) * kLn2;
     }
   }
+}
+
+// 4-D map of a cache of entries of `size` bytes (2: bf16, 1: codes), dimensions in the
+// order of their strides: boxes of `box` tokens x 64 columns (codes: all of them) of one
+// page and head. False where no such map exists.
+inline bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args &a, int D,
+                      int size, int box, const pair_cache_strides &st) {
+  const auto fn = tck::encode_fn();
+  if (!fn) return false;
+  const int64_t stride[3] = {st.for_page * size, st.for_token * size, st.for_head * size};
+  const cuuint64_t sizes[3] = {(cuuint64_t)a.num_pages, (cuuint64_t)a.page, (cuuint64_t)a.Hkv};
+  const cuuint32_t want[3] = {1, (cuuint32_t)box, 1};
+  int order[3] = {0, 1, 2};
+  for (int x = 0; x < 3; ++x)
+    for (int y = 0; y < 2; ++y)
+      if (stride[order[y + 1]] < stride[order[y]]) {
+        const int z = order[y];
+        order[y] = order[y + 1];
+        order[y + 1] = z;
+      }
+  cuuint64_t dims[4] = {(cuuint64_t)D}, strides[3];
+  cuuint32_t boxes[4] = {size == 2 ? 64u : (cuuint32_t)D}, ones[4] = {1, 1, 1, 1};
+  for (int x = 0; x < 3; ++x) {
+    const int64_t b = stride[order[x]];
+    if (b < 16 || b >= ((int64_t)1 << 40)) return false;
+    strides[x] = (cuuint64_t)b;
+    dims[x + 1] = sizes[order[x]];
+    boxes[x + 1] = want[order[x]];
+    at[order[x]] = (int8_t)(x + 1);
+  }
+  return fn(m, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(p), dims, strides, boxes,
+            ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            size * D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+inline bool many_maps(const Args &a, int D, int size, Maps *maps) {
+  // A box is the largest power of two of tokens, up to a tile, that divides
+  // the page; the swizzle's period is 8 rows.
+  int box = BN;
+  while (a.page % box != 0) box /= 2;
+  if (D > 128 || box < 8) return false;
+  maps->box = box;
+  return cache_map(&maps->k, maps->k_at, a.kc, a, D, size, box, a.ks) &&
+         cache_map(&maps->v, maps->v_at, a.vc, a, D, size, box, a.vs);
 }
 
 }  // namespace
