@@ -208,7 +208,7 @@ __device__ void issue(const Args &a, S &sm, W walk) {
   const uint32_t tmem = sm.tmem;
   Ring<S::kKeyStages> kr;
   Ring<S::kValueStages> vr;
-  uint32_t q_ph[2] = {0, 0}, p_ph[2] = {0, 0};
+  uint32_t q_ph = 0, p_ph = 0;  // a bit per tile
   bool ok = true;
   auto scores = [&](int w, int stage, bool last) {  // S_w = Q_w K^T
     if (elect_one()) {
@@ -245,8 +245,8 @@ __device__ void issue(const Args &a, S &sm, W walk) {
     const int top = s.rows > 128;  // the last active tile
     ok &= wait(&sm.k_full[kr.stage], kr.phase);
     for (int w = 0; w <= top; ++w) {
-      ok &= wait(&sm.q_full[w], q_ph[w]);
-      q_ph[w] ^= 1;
+      ok &= wait(&sm.q_full[w], q_ph >> w & 1);
+      q_ph ^= 1 << w;
       tc_fence_after();
       scores(w, kr.stage, w == top);
     }
@@ -258,16 +258,16 @@ __device__ void issue(const Args &a, S &sm, W walk) {
       uint64_t *bar = lane == 0   ? &sm.p_ready[0][0]
                       : lane == 1 ? &sm.looked[vr.stage]
                                   : &sm.k_full[kr.stage];
-      const uint32_t phase = lane == 0 ? p_ph[0] : lane == 1 ? vr.phase : kr.phase;
+      const uint32_t phase = lane == 0 ? p_ph & 1 : lane == 1 ? vr.phase : kr.phase;
       if (!(ok = wait_lanes(wait, more ? 3 : 2, ok, bar, phase))) break;
 #pragma unroll(S::kLean ? 1 : 2)
       for (int w = 0; w < 2; ++w) {
         if (w > top) break;
-        if (w) ok &= wait(&sm.p_ready[w][0], p_ph[w]);
+        if (w) ok &= wait(&sm.p_ready[w][0], p_ph >> w & 1);
         tc_fence_after();
         sums(w, vr.stage, 0, t == s.t0, false);
-        ok &= wait(&sm.p_ready[w][1], p_ph[w]);
-        p_ph[w] ^= 1;
+        ok &= wait(&sm.p_ready[w][1], p_ph >> w & 1);
+        p_ph ^= 1 << w;
         tc_fence_after();
         sums(w, vr.stage, 1, false, w == top);
         // In the tensor pipe's order behind the sums, which read the weights in
