@@ -166,13 +166,28 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
   }
 }
 
-// Where a warp's copies are: its lane's key of the next slice, and that key's way in the
-// block table.
+// The copies of a slice's rows, whose addresses are at `ptrs`.
+template <int D, int M, bool value>
+__device__ __forceinline__ void bring(uint32_t to, uint32_t ptrs) {
+  constexpr int P = Few<D, M>::kPieces, RP = 32 / P;  // rows of one round of copies
+  const int lane = threadIdx.x & 31, c = lane % P;
+#pragma unroll
+  for (int x = 0; x < kSlice / RP; ++x) {
+    const int r = x * RP + lane / P;
+    const uint8_t *p;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(ptrs + r * 8) : "memory");
+    cp_async16(to + place<D, value>(r, c), wide(p, c, 16), true);
+  }
+}
+
+// Where a warp's copies are: this lane's key of the next slice to be brought, and that
+// key's way in the block table.
 struct Stream {
   const int32_t *row;
   int32_t key, end, at, off, id;
-  int32_t slices, stage;
-  uint32_t kb, vb;  // exponent bytes of the lane's key in the slice on its way
+  int32_t slices;    // of the segment
+  uint32_t kb, vb;   // exponent bytes of the lane's key: of the slice at hand,
+  uint32_t kb1, vb1;  // of the one behind it
 };
 
 // The slices of a segment, and the page of this lane's first key.
@@ -186,7 +201,8 @@ __device__ __forceinline__ void begin_stream(const Args &a, const Segment &s, St
   m.off = m.key - m.at * a.page;
   m.id = m.key < m.end ? m.row[m.at] : 0;
 }
-__device__ __forceinline__ void look_ahead(const Args &a, Stream &m, int by, int by_off) {
+__device__ __forceinline__ void look_ahead(const Args &a, Stream &m) {
+  const int by = kSlice / a.page, by_off = kSlice - by * a.page;
   m.key += kSlice;
   m.at += by;
   m.off += by_off;
@@ -196,54 +212,68 @@ __device__ __forceinline__ void look_ahead(const Args &a, Stream &m, int by, int
   }
   m.id = m.key < m.end ? m.row[m.at] : 0;
 }
-// Starts the copies of the slice that was looked up, and reads its exponents. Keys that do
-// not exist are the cache's first: they are masked.
+// Starts the copies of the keys that were looked up, into half `stage` of the ring, reads
+// their exponents and keeps where their values lie. Keys that do not exist are the cache's
+// first: they are masked.
 template <int D, int M>
-__device__ __forceinline__ void fetch(const Args &a, const Segment &s, Stream &m, uint32_t base) {
+__device__ __forceinline__ void bring_keys(const Args &a, const Segment &s, Stream &m, int stage,
+                                           uint32_t base) {
   using L = Few<D, M>;
   const int lane = threadIdx.x & 31;
-  const uint8_t *kc0 = static_cast<const uint8_t *>(a.kc) + s.h * a.ks.for_head;
-  const uint8_t *vc0 = static_cast<const uint8_t *>(a.vc) + s.h * a.vs.for_head;
-  const uint8_t *ke0 = a.ke + s.h * a.kes.for_head, *ve0 = a.ve + s.h * a.ves.for_head;
   int pg = m.id, o = m.off;
   if (m.key >= m.end) pg = 0, o = 0;
   if ((unsigned)pg >= (unsigned)a.num_pages) {
     flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
     pg = 0;
   }
-  const uint8_t *kp, *vp;
+  const uint8_t *kp = static_cast<const uint8_t *>(a.kc) + s.h * a.ks.for_head;
+  const uint8_t *vp = static_cast<const uint8_t *>(a.vc) + s.h * a.vs.for_head;
+  const uint8_t *ke = a.ke + s.h * a.kes.for_head, *ve = a.ve + s.h * a.ves.for_head;
   if (a.narrow) {
-    m.kb = __ldg(wide(wide(ke0, pg, a.kes.for_page), o, a.kes.for_token));
-    m.vb = __ldg(wide(wide(ve0, pg, a.ves.for_page), o, a.ves.for_token));
-    kp = wide(wide(kc0, pg, a.ks.for_page), o, a.ks.for_token);
-    vp = wide(wide(vc0, pg, a.vs.for_page), o, a.vs.for_token);
+    ke = wide(wide(ke, pg, a.kes.for_page), o, a.kes.for_token);
+    ve = wide(wide(ve, pg, a.ves.for_page), o, a.ves.for_token);
+    kp = wide(wide(kp, pg, a.ks.for_page), o, a.ks.for_token);
+    vp = wide(wide(vp, pg, a.vs.for_page), o, a.vs.for_token);
   } else {
-    m.kb = __ldg(ke0 + cache_row(a, a.kes, pg, o, 0));
-    m.vb = __ldg(ve0 + cache_row(a, a.ves, pg, o, 0));
-    kp = kc0 + cache_row(a, a.ks, pg, o, 0);
-    vp = vc0 + cache_row(a, a.vs, pg, o, 0);
+    ke += cache_row(a, a.kes, pg, o, 0);
+    ve += cache_row(a, a.ves, pg, o, 0);
+    kp += cache_row(a, a.ks, pg, o, 0);
+    vp += cache_row(a, a.vs, pg, o, 0);
   }
+  m.kb1 = __ldg(ke);
+  m.vb1 = __ldg(ve);
   const uint32_t ptrs = base + L::kPtr;
-  asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(ptrs + lane * 16), "l"(kp), "l"(vp)
-               : "memory");
+  asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + lane * 8), "l"(kp) : "memory");
+  asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + (kSlice + lane) * 8), "l"(vp) : "memory");
   __syncwarp();
-  constexpr int P = L::kPieces, RP = 32 / P;  // rows of one round of copies
-  const int c = lane % P;
-  const uint32_t kd = base + L::kRing + m.stage * 2 * L::kPart, vd = kd + L::kPart;
-#pragma unroll
-  for (int x = 0; x < kSlice / RP; ++x) {
-    const int r = x * RP + lane / P;
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];"
-                 : "=l"(kp), "=l"(vp)
-                 : "r"(ptrs + r * 16)
-                 : "memory");
-    cp_async16(kd + place<D, false>(r, c), wide(kp, c, 16), true);
-    cp_async16(vd + place<D, true>(r, c), wide(vp, c, 16), true);
-  }
+  bring<D, M, false>(base + L::kRing + stage * 2 * L::kPart, ptrs);
 }
 
-// A warp's segment of up to 8 NT rows. Its first slice is on its way; when it ends, the
-// first slice of the segment `next` is (if there is one).
+// The first two slices of a segment, on their way. Copies are in groups of their own, of
+// keys and of values in turn: a slice's keys have been used when its values have not, and
+// are followed by those of the next slice but one.
+template <int D, int M>
+__device__ __forceinline__ void begin_copies(const Args &a, const Segment &s, Stream &m,
+                                             uint32_t base) {
+  using L = Few<D, M>;
+  Stream n = m;  // of the second slice: both slices' pages are on their way
+  if (m.slices > 1) look_ahead(a, n);
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    if (x < m.slices) bring_keys<D, M>(a, s, x ? n : m, x, base);
+    cp_async_commit();
+    if (x < m.slices)
+      bring<D, M, true>(base + L::kRing + (x * 2 + 1) * L::kPart, base + L::kPtr + kSlice * 8);
+    cp_async_commit();
+    __syncwarp();
+  }
+  n.kb = m.kb1, n.vb = m.vb1;
+  m = n;
+  if (m.slices > 2) look_ahead(a, m);
+}
+
+// A warp's segment of up to 8 NT rows. Its first slices are on their way; when it ends,
+// those of the segment after it are (if there is one).
 template <int D, int F, int M, int NT>
 __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Stream &m,
                                             const Place<M> &place_of, uint8_t *smem, float *part) {
@@ -254,14 +284,12 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
   const int g = lane >> 2, t = lane & 3;
   const uint32_t base = smem_u32(smem);
   float *factor = reinterpret_cast<float *>(smem + L::kFactor);
-  const int by = kSlice / a.page, by_off = kSlice - by * a.page;
   const int slices = m.slices, first = s.t0 * BN;
   __syncwarp();
 
   // Queries in fp16, in the order in which the products take them: step k of 16 columns
   // takes of lane (g, t) the columns 16 (t + 4 (k / 4)) + 4 (k % 4) + {0, 1, 2, 3} of
   // row g, the places of the four codes of a word.
-  if (slices > 1) look_ahead(a, m, by, by_off);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q);
@@ -321,16 +349,10 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 #pragma unroll 1
   for (int x = 0; x < slices; ++x) {
     const float ke = q8::scale_of(m.kb), ve = q8::scale_of(m.vb);  // of this lane's key
-    cp_async_wait<0>();
+    cp_async_wait<3>();  // this slice's keys are there
     __syncwarp();
-    const uint32_t ks = base + L::kRing + m.stage * 2 * L::kPart, vs = ks + L::kPart;
+    const uint32_t ks = base + L::kRing + (x & 1) * 2 * L::kPart, vs = ks + L::kPart;
     const int key0 = first + x * kSlice;
-    m.stage ^= 1;
-    if (x + 1 < slices) {
-      fetch<D, M>(a, s, m, base);
-      if (x + 2 < slices) look_ahead(a, m, by, by_off);
-    }
-    cp_async_commit();
     // Scores of 32 keys with 8 NT rows.
     float sc[MT][NT][4];
 #pragma unroll
@@ -426,6 +448,13 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
           }
         }
     }
+    __syncwarp();  // nobody reads these keys any more
+    m.kb = m.kb1, m.vb = m.vb1;
+    if (x + 2 < slices) bring_keys<D, M>(a, s, m, x & 1, base);
+    cp_async_commit();
+    if (x + 3 < slices) look_ahead(a, m);
+    cp_async_wait<3>();  // this slice's values are there
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const float v0 = __shfl_sync(0xffffffffu, ve, i * 16 + g);
@@ -483,13 +512,15 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
           }
       }
     }
+    __syncwarp();  // nor these values
+    if (x + 2 < slices) bring<D, M, true>(vs, base + L::kPtr + kSlice * 8);
+    cp_async_commit();
   }
-  // The next segment's first slice, then this one's sums: lane (g, t) has 16 columns (8
+  // The next segment's first slices, then this one's sums: lane (g, t) has 16 columns (8
   // for heads of 64) of the rows 8 j + 2 t and the one behind.
   if (place_of.more) {
     begin_stream(a, place_of.next, m);
-    if (m.slices > 0) fetch<D, M>(a, place_of.next, m, base);
-    cp_async_commit();
+    begin_copies<D, M>(a, place_of.next, m, base);
   }
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -558,11 +589,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(A
   if (lane == 0) p.walk = Walk<M, BN>(share);
   p.step(a);
   Stream m;
-  m.stage = 0;
+  m.kb = m.vb = m.kb1 = m.vb1 = 0;
   if (p.more) {
     begin_stream(a, p.next, m);
-    if (m.slices > 0) fetch<D, M>(a, p.next, m, smem_u32(mine));
-    cp_async_commit();
+    begin_copies<D, M>(a, p.next, m, smem_u32(mine));
   }
   for (int seg = 0; p.more; ++seg) {
     const Segment s = p.next;
