@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 import torch
 
@@ -551,24 +552,32 @@ def _cache_q8(k_codes, k_exps, v_codes, v_exps, like, at):
     if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
         raise ValueError("k_codes must be [num_pages, page_size, Hkv, D]")
     shape, dtype = k_codes.shape, k_codes.dtype
-    if dtype not in _FORMATS:
+    fmt = _FORMATS.get(dtype)
+    if fmt is None:
         raise TypeError("k_codes must be int8 or float8_e4m3fn, got %s" % dtype)
-    both = []
-    for name, codes, exps in (("k", k_codes, k_exps), ("v", v_codes, v_exps)):
-        p = _strided(codes, name + "_codes", dtype, shape, like, at)
-        if not (type(exps) is torch.Tensor and exps.dtype is torch.uint8
-                and exps.shape == shape[:3] and exps.get_device() == at):
-            if not isinstance(exps, torch.Tensor) or not exps.is_cuda:
-                raise TypeError("%s_exps must be a CUDA tensor" % name)
-            if exps.dtype is not torch.uint8:
-                raise TypeError("%s_exps must be torch.uint8, got %s" % (name, exps.dtype))
-            if exps.shape != shape[:3]:
-                raise ValueError("%s_exps must have shape %s, got %s"
-                                 % (name, tuple(shape[:3]), tuple(exps.shape)))
-            _same_device(like, name + "_exps", exps)
-        both.append(CacheQ8(p, CacheStrides(*codes.stride()[:3]), exps.data_ptr(),
-                            CacheStrides(*exps.stride())))
-    return (_FORMATS[dtype], *both, shape)
+    rows = shape[:3]
+    return (fmt, _held("k", k_codes, k_exps, dtype, shape, rows, like, at),
+            _held("v", v_codes, v_exps, dtype, shape, rows, like, at), shape)
+
+
+_pack_q8 = struct.Struct("=8q").pack  # of the fields: a fourth of the time
+
+
+def _held(name, codes, exps, dtype, shape, rows, like, at):
+    """One cache in 8 bits as the library takes it."""
+    p = _strided(codes, name + "_codes", dtype, shape, like, at)
+    if not (type(exps) is torch.Tensor and exps.dtype is torch.uint8 and exps.shape == rows
+            and exps.get_device() == at):
+        if not isinstance(exps, torch.Tensor) or not exps.is_cuda:
+            raise TypeError("%s_exps must be a CUDA tensor" % name)
+        if exps.dtype is not torch.uint8:
+            raise TypeError("%s_exps must be torch.uint8, got %s" % (name, exps.dtype))
+        if exps.shape != rows:
+            raise ValueError("%s_exps must have shape %s, got %s"
+                             % (name, tuple(rows), tuple(exps.shape)))
+        _same_device(like, name + "_exps", exps)
+    s0, s1, s2, _ = codes.stride()
+    return CacheQ8.from_buffer_copy(_pack_q8(p, s0, s1, s2, exps.data_ptr(), *exps.stride()))
 
 
 def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, page_size, T,

@@ -109,11 +109,8 @@ constexpr float kValueUnit = F == kI8 ? 64.f : 1.f;
 template <int F, int hi>
 __device__ __forceinline__ uint32_t to_bf16(uint32_t x) {
   if constexpr (F == kI8) {
-    // A byte u = code + 128 is as a bf16 number u 2^-133: below 128 a subnormal one, from
-    // there on one of the least exponent, in the same steps. Times 2^127, less 2.
     const uint32_t y = hi ? x >> 8 : x;
-    return bits(__hfma2(bf2_of((y & 0x00ff00ffu) ^ 0x00800080u), bf2_of(0x7f007f00u),
-                        bf2_of(0xc000c000u)));
+    return bits(q8::whole_to_bf16((y & 0x00ff00ffu) ^ 0x00800080u));
   } else {
     // Exponent and significand at bf16's places are the number times 2^-120 (numbers
     // below e4m3's normal ones too: bf16's multiply takes them as they are). The two

@@ -41,167 +41,229 @@ __device__ __forceinline__ bool find_slot(const Rows &a, int64_t t, int64_t *pg,
   return true;
 }
 
-// 16 bytes of a row: four fp32 entries or eight bf16 ones.
+// 32 bytes of a row: eight fp32 entries or sixteen bf16 ones.
 template <typename T>
 struct Piece {
-  static constexpr int n = 16 / sizeof(T);
-  uint4 u;
+  static constexpr int n = 32 / sizeof(T);
+  uint4 u[2];
+  __device__ __forceinline__ void words(uint32_t (&w)[8]) const {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      w[4 * k] = u[k].x, w[4 * k + 1] = u[k].y, w[4 * k + 2] = u[k].z, w[4 * k + 3] = u[k].w;
+  }
   // The bits of the largest |x|, as those of an fp32 number: infinities and NaN come
   // out above all others.
   __device__ __forceinline__ uint32_t top() const {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    uint32_t m = 0;
+    uint32_t w[8], m = 0;
+    words(w);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (sizeof(T) == 4) {
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (sizeof(T) == 4)
         m = max(m, w[k] & 0x7fffffffu);
-      } else {
+      else
         m = max(m, max(w[k] & 0x7fff0000u, (w[k] & 0x7fffu) << 16));
-      }
     }
     return m;
   }
-  __device__ __forceinline__ void get(int from, float (&x)[4]) const {
-    if constexpr (sizeof(T) == 4) {
-      x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y);
-      x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
-    } else {
-      const uint32_t a = from ? u.z : u.x, b = from ? u.w : u.y;
-      x[0] = __uint_as_float(a << 16), x[1] = __uint_as_float(a & 0xffff0000u);
-      x[2] = __uint_as_float(b << 16), x[3] = __uint_as_float(b & 0xffff0000u);
+  // Its codes, four to a word.
+  template <int F>
+  __device__ __forceinline__ void codes(float inv, uint32_t (&c)[n / 4]) const {
+    uint32_t w[8];
+    words(w);
+#pragma unroll
+    for (int k = 0; k < n / 4; ++k) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4)
+          x[e] = __uint_as_float(w[4 * k + e]);
+        else
+          x[e] = __uint_as_float(e & 1 ? w[2 * k + (e >> 1)] & 0xffff0000u
+                                       : w[2 * k + (e >> 1)] << 16);
+      }
+      c[k] = encode4<F>(x, inv);
     }
   }
 };
 
-// A warp stores a token: L lanes a head, 32 / L heads at once, NP pieces of 16 bytes a
-// lane, kAhead rounds of heads in flight. A row is read once; its largest entry is
-// found among its lanes (log2 L exchanges), its codes are formed from registers.
-// Bound by HBM: every entry is read once, every code written once.
-template <typename T, int F, int NP>
+// Lanes of a row of D entries, a piece each: a power of two.
+template <typename T>
+int lanes_of(int D) {
+  int L = 1;
+  while (L * Piece<T>::n < D) L *= 2;
+  return L;
+}
+
+// A warp stores a token: L lanes a head, 32 / L heads at once, two such rounds of keys and
+// of values in flight. A row is read once; its largest entry is found among its lanes
+// (log2 L exchanges), its codes are formed from registers.
+template <typename T, int F>
 __global__ void __launch_bounds__(kThreads) append_kernel(Rows a, int L) {
-  constexpr int n = Piece<T>::n, kAhead = 4 / NP;
+  constexpr int n = Piece<T>::n, kAhead = 2;
   const int lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   if (t >= a.T) return;
   int64_t pg, off;
   if (!find_slot(a, t, &pg, &off)) return;
-  const int sub = lane & (L - 1), per = 32 / L, pieces = a.D / n;
-  const T *src[2] = {static_cast<const T *>(a.k) + t * a.k_row,
-                     static_cast<const T *>(a.v) + t * a.v_row};
-  const int64_t head[2] = {a.k_head, a.v_head};
-  for (int h0 = lane / L; h0 - lane / L < a.H; h0 += per * kAhead) {  // alike in all lanes
-    Piece<T> x[kAhead][2][NP];
+  const int sub = lane & (L - 1), per = 32 / L, h_lane = lane / L;
+  const bool there = sub * n < a.D;
+  const T *src[2] = {static_cast<const T *>(a.k) + t * a.k_row + h_lane * a.k_head + sub * n,
+                     static_cast<const T *>(a.v) + t * a.v_row + h_lane * a.v_head + sub * n};
+  uint8_t *to[2], *exps[2];
 #pragma unroll
-    for (int y = 0; y < kAhead; ++y)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int h = h0 + y * per, at = sub + p * L;
-          x[y][c][p].u = make_uint4(0, 0, 0, 0);
-          if (h < a.H && at < pieces)
-            x[y][c][p].u =
-                __ldg(reinterpret_cast<const uint4 *>(src[c] + h * head[c] + at * n));
-        }
+  for (int c = 0; c < 2; ++c) {
+    const Held &held = c ? a.vc : a.kc;
+    to[c] = held.codes + pg * held.at.for_page + off * held.at.for_token +
+            h_lane * held.at.for_head + sub * n;
+    exps[c] = held.exps + pg * held.exps_at.for_page + off * held.exps_at.for_token +
+              h_lane * held.exps_at.for_head;
+  }
+  for (int h0 = 0; h0 < a.H; h0 += per * kAhead) {  // alike in all lanes
+    Piece<T> x[kAhead][2];
 #pragma unroll
     for (int y = 0; y < kAhead; ++y)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int h = h0 + y * per;
-        uint32_t top = 0;
+        x[y][c].u[0] = x[y][c].u[1] = make_uint4(0, 0, 0, 0);
+        if (there && h0 + y * per + h_lane < a.H) {
+          const uint4 *p = reinterpret_cast<const uint4 *>(src[c]);
+          x[y][c].u[0] = __ldg(p);
+          x[y][c].u[1] = __ldg(p + 1);
+        }
+        src[c] += per * (c ? a.v_head : a.k_head);
+      }
 #pragma unroll
-        for (int p = 0; p < NP; ++p) top = max(top, x[y][c][p].top());
+    for (int y = 0; y < kAhead; ++y)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t top = x[y][c].top();
         for (int w = L >> 1; w > 0; w >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, w));
         const uint32_t b = exponent_of<F>(top);
-        const float inv = __uint_as_float(b == 255 ? 0u : (254u - b) << 23);
-        if (h >= a.H) continue;
-        const Held &held = c ? a.vc : a.kc;
-        uint8_t *to = held.codes + pg * held.at.for_page + off * held.at.for_token +
-                      h * held.at.for_head;
-#pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          const int at = sub + p * L;
-          if (at >= pieces) continue;
-          uint32_t w[2] = {0, 0};  // a row that is not finite has no codes
-#pragma unroll
-          for (int e = 0; e < n / 4; ++e) {
-            float v[4];
-            x[y][c][p].get(e, v);
-            if (b != 255) w[e] = encode4<F>(v, inv);
+        if (h0 + y * per + h_lane < a.H) {
+          uint32_t w[n / 4] = {};  // a row that is not finite has no codes
+          if (b != 255) x[y][c].template codes<F>(__uint_as_float((254u - b) << 23), w);
+          if (there) {
+            if constexpr (n == 8)
+              *reinterpret_cast<uint2 *>(to[c]) = make_uint2(w[0], w[1]);
+            else
+              *reinterpret_cast<uint4 *>(to[c]) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-          if constexpr (n == 4) {
-            *reinterpret_cast<uint32_t *>(to + at * n) = w[0];
-          } else {
-            *reinterpret_cast<uint2 *>(to + at * n) = make_uint2(w[0], w[1]);
-          }
+          if (sub == 0) *exps[c] = (uint8_t)b;
         }
-        if (sub == 0)
-          held.exps[pg * held.exps_at.for_page + off * held.exps_at.for_token +
-                    h * held.exps_at.for_head] = (uint8_t)b;
+        to[c] += per * (c ? a.vc : a.kc).at.for_head;
+        exps[c] += per * (c ? a.vc : a.kc).exps_at.for_head;
       }
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void put8(T *to, const float (&x)[4], const float (&y)[4]) {
-  if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<float4 *>(to)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4 *>(to)[1] = make_float4(y[0], y[1], y[2], y[3]);
+// The values of a piece's codes.
+template <typename T, int F>
+__device__ __forceinline__ void values(const uint32_t (&w)[8 / sizeof(T)], uint32_t b,
+                                       uint32_t (&u)[8]) {
+  if constexpr (F == kI8 && sizeof(T) == 2) {
+    // Codes over 64 by one multiply-add for two (to_bf16 in pair_cache_q8.cuh), times 2^(b
+    // - 121): in two factors where that is beyond bf16.
+    const bool beyond = b > 248 && b != 255;
+    const uint32_t f = b == 255 ? 0x7fc0u : (beyond ? b - 64 + 6 : b + 6) << 7;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t x = w[k >> 1] ^ 0x80808080u;
+      __nv_bfloat162 y = whole_to_bf16(__byte_perm(x, 0, k & 1 ? 0x4342 : 0x4140));
+      if (beyond) y = __hmul2(y, as_bf16x2(0x5f805f80u));  // 2^64
+      y = __hmul2(y, as_bf16x2(f * 0x10001u));
+      u[k] = *reinterpret_cast<const uint32_t *>(&y);
+    }
   } else {
-    const __nv_bfloat162 u[4] = {__floats2bfloat162_rn(x[0], x[1]), __floats2bfloat162_rn(x[2], x[3]),
-                                 __floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
-    *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(u);
+    const float s = scale_of(b);
+    float x[32 / sizeof(T)];
+#pragma unroll
+    for (int k = 0; k < 8 / (int)sizeof(T); ++k) {
+      float z[4];
+      decode4<F>(w[k], z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * k + e] = z[e] * s;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        u[k] = __float_as_uint(x[k]);
+      } else {
+        const __nv_bfloat162 y = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+        u[k] = *reinterpret_cast<const uint32_t *>(&y);
+      }
+    }
   }
 }
 
-// A warp reads a token back, eight codes per lane and step, kAhead steps of keys and of
-// values in flight. bf16 holds every value exactly, unless it is below its normal
-// numbers.
-template <typename T, int F>
-__global__ void __launch_bounds__(kThreads) read_kernel(Rows a) {
-  constexpr int kAhead = 4;
+// 32 bytes of a row.
+template <typename T, bool whole>
+__device__ __forceinline__ void put32(T *to, const uint32_t (&u)[8]) {
+  if constexpr (whole) {  // a sector in one piece
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(u[0]),
+                 "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4 *>(to)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    reinterpret_cast<uint4 *>(to)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
+}
+
+// A warp reads a token back, laid out as in append_kernel. bf16 holds every value
+// exactly, unless it is below its normal numbers. whole: every row of the outputs begins
+// at a multiple of 32 bytes.
+template <typename T, int F, bool whole>
+__global__ void __launch_bounds__(kThreads) read_kernel(Rows a, int L) {
+  constexpr int n = Piece<T>::n, kAhead = 2;
   const int lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
   if (t >= a.T) return;
   int64_t pg = 0, off = 0;
   const bool there = find_slot(a, t, &pg, &off);
-  const int per = a.D / 8, pieces = a.H * per;
-  T *out[2] = {static_cast<T *>(a.k) + t * a.k_row, static_cast<T *>(a.v) + t * a.v_row};
-  const int64_t head[2] = {a.k_head, a.v_head};
-  for (int x0 = lane; x0 < pieces; x0 += 32 * kAhead) {
-    uint2 u[kAhead][2];
-    uint32_t b[kAhead][2];
+  const int sub = lane & (L - 1), per = 32 / L, h_lane = lane / L;
+  if (sub * n >= a.D) return;
+  T *out[2] = {static_cast<T *>(a.k) + t * a.k_row + h_lane * a.k_head + sub * n,
+               static_cast<T *>(a.v) + t * a.v_row + h_lane * a.v_head + sub * n};
+  const uint8_t *from[2], *exps[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const Held &held = c ? a.vc : a.kc;
+    from[c] = held.codes + pg * held.at.for_page + off * held.at.for_token +
+              h_lane * held.at.for_head + sub * n;
+    exps[c] = held.exps + pg * held.exps_at.for_page + off * held.exps_at.for_token +
+              h_lane * held.exps_at.for_head;
+  }
+  for (int h0 = h_lane; h0 < a.H; h0 += per * kAhead) {
+    uint32_t u[kAhead][2][n / 4], b[kAhead][2];
 #pragma unroll
     for (int y = 0; y < kAhead; ++y)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int x = x0 + 32 * y, h = x / per, at = (x - h * per) * 8;
-        const Held &held = c ? a.vc : a.kc;
-        u[y][c] = make_uint2(0, 0);
         b[y][c] = 127;
-        if (there && x < pieces) {
-          u[y][c] = __ldg(reinterpret_cast<const uint2 *>(held.codes + pg * held.at.for_page +
-                                                          off * held.at.for_token +
-                                                          h * held.at.for_head + at));
-          b[y][c] = __ldg(held.exps + pg * held.exps_at.for_page + off * held.exps_at.for_token +
-                          h * held.exps_at.for_head);
+#pragma unroll
+        for (int k = 0; k < n / 4; ++k) u[y][c][k] = 0;
+        if (there && h0 + y * per < a.H) {
+          b[y][c] = __ldg(exps[c]);
+          if constexpr (n == 8) {
+            const uint2 z = __ldg(reinterpret_cast<const uint2 *>(from[c]));
+            u[y][c][0] = z.x, u[y][c][1] = z.y;
+          } else {
+            const uint4 z = __ldg(reinterpret_cast<const uint4 *>(from[c]));
+            u[y][c][0] = z.x, u[y][c][1] = z.y, u[y][c][2] = z.z, u[y][c][3] = z.w;
+          }
         }
+        from[c] += per * (c ? a.vc : a.kc).at.for_head;
+        exps[c] += per * (c ? a.vc : a.kc).exps_at.for_head;
       }
 #pragma unroll
     for (int y = 0; y < kAhead; ++y)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        const int x = x0 + 32 * y, h = x / per, at = (x - h * per) * 8;
-        if (x >= pieces) continue;
-        float lo[4] = {}, hi[4] = {};
-        if (there) {
-          const float s = scale_of(b[y][c]);
-          decode4<F>(u[y][c].x, lo);
-          decode4<F>(u[y][c].y, hi);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) lo[k] *= s, hi[k] *= s;
+        if (h0 + y * per < a.H) {
+          uint32_t x[8];
+          values<T, F>(u[y][c], b[y][c], x);
+          put32<T, whole>(out[c], x);
         }
-        put8(out[c] + h * head[c] + at, lo, hi);
+        out[c] += per * (c ? a.v_head : a.k_head);
       }
   }
 }
@@ -244,25 +306,24 @@ pair_status rows_of(int64_t T, int32_t H, int32_t D, pair_dtype dt, const void *
 
 template <typename T, int F>
 pair_status append(const Rows &a, cudaStream_t s) {
-  const unsigned blocks = (unsigned)ceil_div(a.T, kThreads / 32);
-  const int pieces = a.D / Piece<T>::n;
-  int L = 1;
-  while (L < 32 && L < pieces) L *= 2;
   PAIR_BEGIN("cache_append_q8", s);
-  if (pieces <= 32) {
-    append_kernel<T, F, 1><<<blocks, kThreads, 0, s>>>(a, L);
-  } else {
-    if constexpr (sizeof(T) == 4)  // 256 fp32 entries are two pieces a lane
-      append_kernel<T, F, 2><<<blocks, kThreads, 0, s>>>(a, L);
-  }
+  append_kernel<T, F><<<(unsigned)ceil_div(a.T, kThreads / 32), kThreads, 0, s>>>(
+      a, lanes_of<T>(a.D));
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
 }
 
 template <typename T, int F>
 pair_status read(const Rows &a, cudaStream_t s) {
+  bool whole = ((reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v)) & 31) == 0;
+  const int64_t strides[][2] = {{a.k_row, a.T}, {a.v_row, a.T}, {a.k_head, a.H}, {a.v_head, a.H}};
+  for (const auto &x : strides) whole &= x[1] == 1 || x[0] * sizeof(T) % 32 == 0;
   PAIR_BEGIN("cache_read_q8", s);
-  read_kernel<T, F><<<(unsigned)ceil_div(a.T, kThreads / 32), kThreads, 0, s>>>(a);
+  const unsigned blocks = (unsigned)ceil_div(a.T, kThreads / 32);
+  if (whole)
+    read_kernel<T, F, true><<<blocks, kThreads, 0, s>>>(a, lanes_of<T>(a.D));
+  else
+    read_kernel<T, F, false><<<blocks, kThreads, 0, s>>>(a, lanes_of<T>(a.D));
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
 }

@@ -47,6 +47,16 @@ __device__ __forceinline__ float decode1(uint32_t byte) {
   return x[0];
 }
 
+__device__ __forceinline__ __nv_bfloat162 as_bf16x2(uint32_t x) {
+  return *reinterpret_cast<const __nv_bfloat162 *>(&x);
+}
+// Whole numbers c over 64 out of the bytes u = c + 128 in the low halves of x's halves: a
+// byte u is as a bf16 number u 2^-133 (below 128 a subnormal one, from there on one of
+// the least exponent, in the same steps). Times 2^127, less 2.
+__device__ __forceinline__ __nv_bfloat162 whole_to_bf16(uint32_t x) {
+  return __hfma2(as_bf16x2(x), as_bf16x2(0x7f007f00u), as_bf16x2(0xc000c000u));
+}
+
 // The exponent byte of a row whose largest |x| has these bits: the least one with
 // which it does not round beyond the largest code. A significand of 1 + m with E - 6
 // gives 64 (1 + m), at most 127 if it is below 127.5; with E - 8 e4m3 gets 256 (1 + m),
