@@ -544,6 +544,8 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                k.exps_at,
                v.exps_at,
                false,
+               0,
+               0,
                0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   Launch few{a, 0, 0}, many{a, 0, 0};
@@ -565,7 +567,9 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   } else if (held && (only_few || R > 1)) {
     const float *end = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need);
     const int64_t room = (only_few ? end : many.a.part) - few.a.part;
-    st = launch_few_q8(&few, D, fmt, most_rows, (int)(room / part_floats(kFewTile, D)), s);
+    const int slots = (int)(room / part_floats(kFewTile, D));
+    st = fmt == q8::kI8 ? launch_few_i8(&few, D, most_rows, slots, s)
+                        : launch_few_e4m3(&few, D, most_rows, slots, s);
   } else if (only_few || R > 1) {
     st = launch_few(&few, D, s);
   }

@@ -71,6 +71,7 @@ struct Args {
   const uint8_t *ke, *ve;
   pair_cache_strides kes, ves;
   bool narrow;        // strides of pages and tokens fit in 32 bits
+  int32_t slice_pages, slice_rest;  // 32 keys further in the block table: pages, places
   int32_t unit_cost;  // fixed cost of a unit of this launch, in keys
 };
 
@@ -378,6 +379,30 @@ __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// x s + r, x + y and x y, two lanes per instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 r) {
+  float2 o;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t &>(o))
+      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(s)),
+        "l"(reinterpret_cast<uint64_t &>(r)));
+  return o;
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  float2 o;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t &>(o))
+      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+  return o;
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  float2 o;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<uint64_t &>(o))
+      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
+  return o;
+}
+
 // Programmatic dependent launch. The kernel for many rows starts beside the one
 // for few, on whose results it does not depend (it waits for its end only before
 // its own, so that what comes after it comes after both); the pass that joins the
@@ -399,8 +424,8 @@ pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s);
 pair_status launch_few(Launch *l, int D, cudaStream_t s);
 // Caches in 8 bits; most_rows: of a chunk, as far as the host knows.
 // slots: partial sums of kFewTile rows that the workspace has room for.
-pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, int slots,
-                          cudaStream_t s);
+pair_status launch_few_i8(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s);
+pair_status launch_few_e4m3(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s);
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);
 bool many_applies_q8(const Args &a, int D);

@@ -14,6 +14,8 @@
 // V: codes become bf16 (exact), against weights exp(s - max) 2^(b - 127) in bf16: they
 // carry the value's scale and want the exponent range. Each weight is off by up to 2^-8
 // of itself, independently, while their sum takes them unrounded in fp32.
+#pragma once
+
 #include <cuda_fp16.h>
 
 #include "pair_attend.cuh"
@@ -199,10 +201,9 @@ __device__ __forceinline__ void begin_stream(const Args &a, const Segment &s, St
   m.id = m.key < m.end ? m.row[m.at] : 0;
 }
 __device__ __forceinline__ void look_ahead(const Args &a, Stream &m) {
-  const int by = kSlice / a.page, by_off = kSlice - by * a.page;
   m.key += kSlice;
-  m.at += by;
-  m.off += by_off;
+  m.at += a.slice_pages;
+  m.off += a.slice_rest;
   if (m.off >= a.page) {
     m.off -= a.page;
     ++m.at;
@@ -396,8 +397,12 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          sc[i][j][c] = fmaf(sc[i][j][c] * (c < 2 ? k0 : k1), cs[j][c & 1], -mx[j][c & 1]);
+        for (int c = 0; c < 4; c += 2) {  // two rows at once
+          const float k = c ? k1 : k0;
+          const float2 y = fma2(mul2({sc[i][j][c], sc[i][j][c + 1]}, {k, k}), {cs[j][0], cs[j][1]},
+                                {-mx[j][0], -mx[j][1]});
+          sc[i][j][c] = y.x, sc[i][j][c + 1] = y.y;
+        }
     }
     const bool edge = key0 + kSlice > least;
     if (edge) {
@@ -460,10 +465,12 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float e = ex2_approx(sc[i][j][c]);
-          l[j][c & 1] += e;
-          w[j][c] = e * (c < 2 ? v0 : v1);
+        for (int c = 0; c < 4; c += 2) {
+          const float2 e = {ex2_approx(sc[i][j][c]), ex2_approx(sc[i][j][c + 1])};
+          const float v = c ? v1 : v0;
+          const float2 sum = add2({l[j][0], l[j][1]}, e), y = mul2(e, {v, v});
+          l[j][0] = sum.x, l[j][1] = sum.y;
+          w[j][c] = y.x, w[j][c + 1] = y.y;
         }
       if (edge) {  // the scale of a value that a row does not see may be NaN
 #pragma unroll
@@ -603,9 +610,9 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(A
     }
     if (M == 8 || s.rows <= 8)
       few_segment<D, F, M, 1>(a, s, m, p, mine, part);
-    else if (M == 16 || s.rows <= 16)
+    else if (M == 16 || (M == 32 && s.rows <= 16))
       few_segment<D, F, M, M < 16 ? 1 : 2>(a, s, m, p, mine, part);
-    else if (s.rows <= 24)
+    else if (M == 24 || s.rows <= 24)
       few_segment<D, F, M, M < 24 ? 1 : 3>(a, s, m, p, mine, part);
     else
       few_segment<D, F, M, M < 32 ? 1 : 4>(a, s, m, p, mine, part);
@@ -622,6 +629,8 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   const auto kernel = attend_q8_few_kernel<D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   a.unit_cost = 96;
+  a.slice_pages = kSlice / a.page;
+  a.slice_rest = kSlice % a.page;
   a.narrow = true;
   for (const pair_cache_strides *x : {&a.ks, &a.vs, &a.kes, &a.ves})
     a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
@@ -637,22 +646,21 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   return PAIR_OK;
 }
 
+template <int D, int F>
+pair_status run_few(Launch *l, int64_t most_rows, int slots, cudaStream_t s) {
+  if (most_rows <= 8) return run_few<D, F, 8>(l, slots, s);
+  if (most_rows <= 16) return run_few<D, F, 16>(l, slots, s);
+  if (most_rows <= 24) return run_few<D, F, 24>(l, slots, s);
+  return run_few<D, F, 32>(l, slots, s);
+}
+
 template <int F>
 pair_status run_few(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s) {
-  if (D == 64)
-    return most_rows <= 8 ? run_few<64, F, 8>(l, slots, s) : run_few<64, F, 32>(l, slots, s);
-  if (D == 128)
-    return most_rows <= 8 ? run_few<128, F, 8>(l, slots, s) : run_few<128, F, 32>(l, slots, s);
+  if (D == 64) return run_few<64, F>(l, most_rows, slots, s);
+  if (D == 128) return run_few<128, F>(l, most_rows, slots, s);
   return run_few<256, F, 16>(l, slots, s);
 }
 
 }  // namespace
-
-pair_status launch_few_q8(Launch *l, int D, int fmt, int64_t most_rows, int slots,
-                          cudaStream_t s) {
-  return fmt == kI8 ? run_few<kI8>(l, D, most_rows, slots, s)
-                    : run_few<kE4M3>(l, D, most_rows, slots, s);
-}
-
 }  // namespace attend
 }  // namespace pairk

@@ -134,22 +134,6 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
                :
                : "memory");
 }
-// (x0, x1) * (s, s) + (r, r) and (a0, a1) + (x0, x1), two lanes per instruction.
-__device__ __forceinline__ float2 fma2(float2 x, float2 s, float2 r) {
-  float2 o;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<uint64_t &>(o))
-      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(s)),
-        "l"(reinterpret_cast<uint64_t &>(r)));
-  return o;
-}
-__device__ __forceinline__ float2 add2(float2 x, float2 y) {
-  float2 o;
-  asm("add.rn.f32x2 %0, %1, %2;"
-      : "=l"(reinterpret_cast<uint64_t &>(o))
-      : "l"(reinterpret_cast<uint64_t &>(x)), "l"(reinterpret_cast<uint64_t &>(y)));
-  return o;
-}
 __device__ __forceinline__ void tmem_st_wait() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
