@@ -446,7 +446,7 @@ bool aligned(const void *p, uintptr_t to) {
 // worth at most: the host knows the table's width, not the lengths.
 int useful_ctas(const Args &a, int M, int fit, int least) {
   const double units = (double)ceil_div(a.T * a.g, M) + (double)(a.R < a.T ? a.R : a.T);
-  const double keys = units * a.Hkv * (a.unit_cost + (double)a.width * a.page + (double)M / a.g);
+  const double keys = units * a.heads * (a.unit_cost + (double)a.width * a.page + (double)M / a.g);
   return keys < (double)fit * least ? 1 + (int)(keys / least) : fit;
 }
 
@@ -546,6 +546,7 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
                false,
                0,
                0,
+               Hkv,
                0};
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   Launch few{a, 0, 0}, many{a, 0, 0};

@@ -72,6 +72,7 @@ struct Args {
   pair_cache_strides kes, ves;
   bool narrow;        // strides of pages and tokens fit in 32 bits
   int32_t slice_pages, slice_rest;  // 32 keys further in the block table: pages, places
+  int32_t heads;      // key heads on the line of units (a fourth where warps share a CTA's)
   int32_t unit_cost;  // fixed cost of a unit of this launch, in keys
 };
 
@@ -128,7 +129,7 @@ struct Line {
 __device__ __forceinline__ int64_t request_cost(const Args &a, int i, int M) {
   const Request r = request(a, i);
   const Line l(r, M, a);
-  return (int64_t)a.Hkv * l.upto(l.units);
+  return (int64_t)a.heads * l.upto(l.units);
 }
 
 // Where on the line a CTA begins and ends.
@@ -142,7 +143,8 @@ struct Share {
 // shares of a block, from that of its first warp on: warp w's is the w-th of them, and
 // `cta` that share's number (the block's, where N is 1).
 template <int NT, int N = 1>
-__device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *scratch) {
+__device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *scratch,
+                            int least = kMinKeys) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int W = NT / 32;
   const int per = (a.R + NT - 1) / NT;
@@ -162,9 +164,9 @@ __device__ Share find_share(const Args &a, int M, int cta, int ctas, int64_t *sc
     total += scratch[w];
   }
   x += before - sum;  // exclusive
-  int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * (N > 1 ? kMinWarp : kMinKeys))));
+  int64_t n = max((int64_t)1, min((int64_t)ctas, total / (2 * a.g * least)));
   if (a.R == 1) {  // units of one length, nearly: no CTA across two of them
-    const int64_t units = (int64_t)a.Hkv * Line(request(a, 0), M, a).units;
+    const int64_t units = (int64_t)a.heads * Line(request(a, 0), M, a).units;
     if (n > units && units > 0) n -= n % units;
   }
   const int k0 = N > 1 ? warp : 0;  // the share that is returned
@@ -248,7 +250,7 @@ struct Walk {
       } else {
         if (++k == units) {
           k = 0;
-          if (++h == a.Hkv) {
+          if (++h == a.heads) {
             h = 0;
             do {
               if (++s.i >= a.R) return false;

@@ -131,7 +131,10 @@ struct Place {
   Segment next;
   bool more;
   __device__ __forceinline__ void step(const Args &a) {
-    if ((threadIdx.x & 31) == 0) more = walk.next(a, &next);
+    if ((threadIdx.x & 31) == 0) {
+      more = walk.next(a, &next);
+      if (a.heads < a.Hkv) next.h = next.h * kWarps + (threadIdx.x >> 5);
+    }
     __syncwarp();
   }
 };
@@ -572,21 +575,25 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 template <int D, int M>
 constexpr int kPerSm = D == 256 ? 1 : M == 8 ? 3 : 2;
 
-// Every warp has a share of the work of its own (a CTA is no more than its four warps):
-// a unit is worked on by one warp from end to end, in 32 keys at a time, but where shares
-// meet. Nothing waits for another warp.
+// A unit is worked on by one warp from end to end, 32 keys at a time, but where shares
+// meet. Nothing waits for another warp. Every warp has a share of the work of its own, or,
+// where key heads come in fours, a CTA has one of four heads at once: its warps then read
+// the same tokens, whose heads lie side by side in a cache by token.
 template <int D, int F, int M>
 __global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(Args a) {
   using L = Few<D, M>;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int worker = blockIdx.x * kWarps + warp, workers = gridDim.x * kWarps;
+  const int worker = blockIdx.x * kWarps + warp;
   if (a.rows_upto < INT32_MAX) let_next_start();  // the kernel for many rows
   if (lane < 2) a.desc[worker * 2 + lane] = {0, 0, 0, 0, 0, 0, 0, 0};
   clear_spare_rows<__nv_bfloat16, D, kThreads>(a, blockIdx.x, gridDim.x);
   if (blockIdx.x == gridDim.x - 1) report_requests(a);
-  const Share share = find_share<kThreads, kWarps>(a, M, worker, workers,
-                                                   reinterpret_cast<int64_t *>(smem));
+  int64_t *scratch = reinterpret_cast<int64_t *>(smem);
+  const Share share =
+      a.heads < a.Hkv
+          ? find_share<kThreads>(a, M, blockIdx.x, gridDim.x, scratch, kMinWarp)
+          : find_share<kThreads, kWarps>(a, M, worker, gridDim.x * kWarps, scratch, kMinWarp);
   __syncthreads();  // the scratch is the rings' place
   uint8_t *mine = smem + warp * L::kWarpBytes;
   Place<M> &p = *reinterpret_cast<Place<M> *>(mine + L::kPlace);
@@ -636,8 +643,12 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
     a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
   const int fit = min(slots * (kFewTile / M) / 2,  // two partial sums each
                       min(kMaxWorkers, kPerSm<D, M> * kWarps * sm_count()));
-  const int ctas =
-      (int)ceil_div(useful_ctas(a, M, fit / kWarps * kWarps, kMinWarp), kWarps);
+  // Where key heads come in fours a CTA's warps take four of them over the same keys.
+  const bool together = a.Hkv % kWarps == 0;
+  if (together) a.heads = a.Hkv / kWarps;
+  const int ctas = together
+                       ? useful_ctas(a, M, fit / kWarps, kMinWarp)
+                       : (int)ceil_div(useful_ctas(a, M, fit / kWarps * kWarps, kMinWarp), kWarps);
   PAIR_BEGIN("attend_q8_few", s);
   kernel<<<ctas, kThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
