@@ -162,15 +162,19 @@ __device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk
     const int32_t *table = a.table + (int64_t)s.i * a.width;
     int key = s.t0 * BN + lane * box, at = key / a.page, off = key - at * a.page;
     int id = mine && key < s.keys ? table[at] : 0;
-    for (int t = s.t0; t < s.t1; ++t) {
-      const bool load = mine && key < s.keys;
-      int pg = id;
-      const int o = off;
+    // Pages, places and exponents of the tile at hand; those of the next one are on
+    // their way while it is brought in.
+    int pg, o, nk;
+    bool load;
+    uint32_t exps[2][4];
+    auto look = [&](int t) {
+      load = mine && key < s.keys;
+      pg = id;
+      o = off;
       if (load && (unsigned)pg >= (unsigned)a.num_pages) {
         flag_error(a.dev_err, PAIR_DEV_ERR_PAGES);
         pg = 0;
       }
-      // The next tile's pages are on their way meanwhile.
       key += BN;
       at += by;
       off += by_off;
@@ -179,6 +183,20 @@ __device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk
         ++at;
       }
       if (t + 1 < s.t1) id = mine && key < s.keys ? table[at] : 0;
+      nk = min(BN, s.keys - t * BN);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {  // keys lane + 32 x
+        const int k = lane + 32 * x, from = k >> box_bits, in = k & (box - 1);
+        const int p = __shfl_sync(0xffffffffu, pg, from), q = __shfl_sync(0xffffffffu, o, from);
+        exps[0][x] = exps[1][x] = 127;
+        if (k < nk) {
+          exps[0][x] = __ldg(a.ke + cache_row(a, a.kes, p, q + in, s.h));
+          exps[1][x] = __ldg(a.ve + cache_row(a, a.ves, p, q + in, s.h));
+        }
+      }
+    };
+    look(s.t0);
+    for (int t = s.t0; t < s.t1; ++t) {
       const int boxes = __popc(__ballot_sync(0xffffffffu, load));
       auto bring = [&](int kv) {
         if (!wait(&sm.codes_empty[kv], codes.phase ^ 1)) return false;
@@ -195,26 +213,12 @@ __device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk
         return true;
       };
       if (!(ok = bring(0))) break;
-      const int nk = min(BN, s.keys - t * BN);
-      uint32_t e[2] = {0, 0};
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {  // keys lane + 32 x
-        const int k = lane + 32 * x, from = k >> box_bits, in = k & (box - 1);
-        const int p = __shfl_sync(0xffffffffu, pg, from), q = __shfl_sync(0xffffffffu, o, from);
-        uint32_t eb = 127, vb = 127;
-        if (k < nk) {
-          eb = __ldg(a.ke + cache_row(a, a.kes, p, q + in, s.h));
-          vb = __ldg(a.ve + cache_row(a, a.ves, p, q + in, s.h));
-        }
-        e[0] |= eb << 8 * x;
-        e[1] |= vb << 8 * x;
-      }
       if (!(ok = wait(&sm.info_empty[ring.stage], ring.phase ^ 1))) break;
       Info &info = sm.info[ring.stage];
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) info.exps[kv][lane + 32 * x] = (uint8_t)(e[kv] >> 8 * x);
+        for (int x = 0; x < 4; ++x) info.exps[kv][lane + 32 * x] = (uint8_t)exps[kv][x];
       if (lane == 0) {
         info.unseen = edge_tile(s, t) ? max(0, s.least - t * BN) : BN;
         info.nk = nk;
@@ -224,6 +228,7 @@ __device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk
       ring.step();
       if (!(ok = bring(1))) break;
       codes.step();
+      if (t + 1 < s.t1) look(t + 1);
     }
   }
   if (ok && wait(&sm.info_empty[ring.stage], ring.phase ^ 1)) {

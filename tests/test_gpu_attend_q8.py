@@ -120,6 +120,24 @@ def test_attend(what, heads, dtype, fmt):
     check(build(SHAPES[what], Hq, Hkv, D, 16, dtype, fmt, seed=len(what)))
 
 
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("heads", [(8, 4, 64), (8, 8, 128), (16, 4, 128), (32, 8, 64), (8, 4, 256)])
+@pytest.mark.parametrize("what", ["tokens", "drafts", "chunk", "none"])
+def test_attend_key_heads_in_fours(what, heads, fmt):
+    """Four key heads are worked on side by side."""
+    Hq, Hkv, D = heads
+    check(build(SHAPES[what], Hq, Hkv, D, 16, torch.bfloat16, fmt, seed=len(what)))
+
+
+@pytest.mark.parametrize("rows", [1, 8, 9, 16, 17, 24, 25, 32, 33])
+@pytest.mark.parametrize("hint", [True, False])
+def test_attend_every_number_of_rows(rows, hint):
+    """Rows of a key head from 1 to more than the kernels for few rows take, known to
+    the host or not."""
+    check(build([(rows, 200 + rows), (rows, rows), (0, 9), (rows, 70 + rows)], 4, 4, 128, 16,
+                torch.bfloat16, "i8", seed=rows), max_new=rows if hint else 0)
+
+
 @pytest.mark.parametrize("page", [1, 5, 8, 24, 32, 64, 128, 256])
 @pytest.mark.parametrize("layout", ["token", "head"])
 @pytest.mark.parametrize("dtype,fmt", [(torch.bfloat16, "i8"), (torch.bfloat16, "e4m3"),
@@ -254,3 +272,82 @@ def test_same_results_every_time_on_any_stream_and_captured(n):
         torch.cuda.synchronize()
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
     assert torch.equal(other[0], first[0]) and torch.equal(other[1], first[1])
+
+
+def test_many_requests_and_idle_ones():
+    """More requests than a block has threads, most of them with nothing to do."""
+    reqs = [(1 if i % 3 == 0 else 0, 1 + i % 40) for i in range(700)]
+    check(build(reqs, 4, 4, 64, 8, torch.bfloat16, "e4m3", seed=1), max_new=1)
+    check(build(reqs, 4, 2, 64, 8, torch.bfloat16, "i8", seed=2))
+
+
+def test_exponents_with_strides_of_their_own():
+    """Exponent bytes out of a wider array, codes in pages of a larger one."""
+    from paper_2608_11368_gb300 import binding as B
+    t = build([(1, 100), (6, 77), (90, 190)], 8, 4, 128, 16, torch.bfloat16, "i8", seed=8)
+    ref = reference(t, 128 ** -0.5)
+    k, ke, v, ve = t["held"]
+    wide = torch.full((*ke.shape, 3), 255, dtype=torch.uint8, device="cuda")
+    wide[..., 1], wide[..., 2] = ke, ve
+    both = torch.zeros((k.shape[0], 2, *k.shape[1:]), dtype=k.dtype, device="cuda")
+    both[:, 0], both[:, 1] = k, v
+    t["held"] = [both[:, 0], wide[..., 1], both[:, 1], wide[..., 2]]
+    assert wide[..., 1].stride(-1) == 3
+    check(t, ref=ref)
+    assert B.PAIR_CACHE_I8 == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq", [1, 4, 48])
+def test_views_with_one_entry(Hq, dtype):
+    """Strides over a single page, head or row are not looked at."""
+    t = build([(1, 9)], Hq, 1, 64, 16, dtype, "i8", seed=Hq)
+    t["q"] = t["q"].as_strided((1, Hq, 64), (Hq * 64 + 1, 64, 1))
+    at = int(t["table"][0, 0])
+    k, ke, v, ve = (x[at:at + 1] for x in t["held"])
+    t["held"] = [k.as_strided((1, 16, 1, 64), (3, 64, 5, 1), k.storage_offset()), ke,
+                 v.as_strided((1, 16, 1, 64), (7, 64, 9, 1), v.storage_offset()), ve]
+    t["table"].zero_()
+    check(t)
+
+
+def test_a_step_as_it_is_used():
+    """Pages, keys and values into the cache in 8 bits, attention over it: the same as
+    attention over the values that are read back, to the bounds of both."""
+    from paper_2608_11368_gb300 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(0)
+    R, H, D, page, pages = 5, 4, 128, 16, 200
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for fmt, dt in CODES.items():
+        held = [torch.zeros((pages, page, H, D), dtype=dt, device="cuda"),
+                torch.zeros((pages, page, H), dtype=torch.uint8, device="cuda")] + [
+                    torch.zeros((pages, page, H, D), dtype=dt, device="cuda"),
+                    torch.zeros((pages, page, H), dtype=torch.uint8, device="cuda")]
+        table = torch.zeros((R, 40), dtype=torch.int32, device="cuda")
+        lens, pgs, free, count = i32([0] * R), i32([0] * R), i32(list(range(pages))), i32([pages])
+        plain = [torch.zeros((pages, page, H, D), dtype=torch.bfloat16, device="cuda")
+                 for _ in "kv"]
+        for n in ([200, 3, 0, 17, 64], [1, 1, 0, 1, 1], [4, 4, 1, 0, 40]):
+            T = sum(n) + 3
+            kv, pgs, cu, slots, taken = B.pair_pages_extend(lens, pgs, i32(n), free, count, table,
+                                                            page, T, dev_err=err)
+            free, count = torch.roll(free, -int(taken)), count - taken
+            q, k, v = (torch.randn((T, h, D), generator=g, device="cuda").bfloat16()
+                       for h in (2 * H, H, H))
+            B.pair_cache_append_q8(k, v, slots, *held, dev_err=err)
+            out, lse = B.pair_attend_paged_q8(q, *held, table, kv, cu, max_new=max(n), dev_err=err)
+            back = B.pair_cache_read_q8(slots, *held, dev_err=err)
+            B.pair_cache_append(*back, slots, *plain, dev_err=err)
+            want, wlse = B.pair_attend_paged(q, *plain, table, kv, cu, max_new=max(n), dev_err=err)
+            mag, _ = B.pair_attend_paged(q, plain[0], plain[1].abs(), table, kv, cu, max_new=max(n))
+            assert B.pair_status_sync(err) == 0
+            # Both sides: weights and output rounded to bf16 (2^-8 of sum p |v| each), and
+            # |mag| is itself off by as much.
+            bound = 4 * 2.0 ** -8 * 1.02 * mag.float() * (1 + 2.0 ** -6)
+            assert ((out.float() - want.float()).abs() <= bound + 1e-30).all()
+            same = torch.isinf(wlse)
+            assert torch.equal(torch.isinf(lse), same)
+            # 2 sides x 2 2^-24 (D size + keys + 16), sizes (scale sum |q_d k_d|) below 16.
+            assert ((lse - wlse).abs()[~same] <= 6e-4).all()
+            lens = kv
