@@ -547,37 +547,36 @@ def _cache(k_cache, v_cache, like, at):
 _FORMATS = {torch.int8: PAIR_CACHE_I8, torch.float8_e4m3fn: PAIR_CACHE_E4M3}
 
 
+_pack_q8 = struct.Struct("=8q").pack  # a CacheQ8's fields: a fourth of the time
+
+
 def _cache_q8(k_codes, k_exps, v_codes, v_exps, like, at):
-    """Format, both caches in 8 bits, their shape."""
+    """Format, both caches in 8 bits, their sizes."""
     if not isinstance(k_codes, torch.Tensor) or k_codes.dim() != 4:
         raise ValueError("k_codes must be [num_pages, page_size, Hkv, D]")
     shape, dtype = k_codes.shape, k_codes.dtype
     fmt = _FORMATS.get(dtype)
     if fmt is None:
         raise TypeError("k_codes must be int8 or float8_e4m3fn, got %s" % dtype)
-    rows = shape[:3]
-    return (fmt, _held("k", k_codes, k_exps, dtype, shape, rows, like, at),
-            _held("v", v_codes, v_exps, dtype, shape, rows, like, at), shape)
-
-
-_pack_q8 = struct.Struct("=8q").pack  # of the fields: a fourth of the time
-
-
-def _held(name, codes, exps, dtype, shape, rows, like, at):
-    """One cache in 8 bits as the library takes it."""
-    p = _strided(codes, name + "_codes", dtype, shape, like, at)
-    if not (type(exps) is torch.Tensor and exps.dtype is torch.uint8 and exps.shape == rows
-            and exps.get_device() == at):
-        if not isinstance(exps, torch.Tensor) or not exps.is_cuda:
-            raise TypeError("%s_exps must be a CUDA tensor" % name)
-        if exps.dtype is not torch.uint8:
-            raise TypeError("%s_exps must be torch.uint8, got %s" % (name, exps.dtype))
-        if exps.shape != rows:
-            raise ValueError("%s_exps must have shape %s, got %s"
-                             % (name, tuple(rows), tuple(exps.shape)))
-        _same_device(like, name + "_exps", exps)
-    s0, s1, s2, _ = codes.stride()
-    return CacheQ8.from_buffer_copy(_pack_q8(p, s0, s1, s2, exps.data_ptr(), *exps.stride()))
+    pages, page, heads, _ = shape
+    rows, u8 = (pages, page, heads), torch.uint8
+    for name, t in (("k_exps", k_exps), ("v_exps", v_exps)):
+        if not (type(t) is torch.Tensor and t.dtype is u8 and t.shape == rows
+                and t.get_device() == at):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda:
+                raise TypeError("%s must be a CUDA tensor" % name)
+            if t.dtype is not u8:
+                raise TypeError("%s must be torch.uint8, got %s" % (name, t.dtype))
+            if t.shape != rows:
+                raise ValueError("%s must have shape %s, got %s" % (name, rows, tuple(t.shape)))
+            _same_device(like, name, t)
+    kp = _strided(k_codes, "k_codes", dtype, shape, like, at)
+    vp = _strided(v_codes, "v_codes", dtype, shape, like, at)
+    k0, k1, k2, _ = k_codes.stride()
+    v0, v1, v2, _ = v_codes.stride()
+    new = CacheQ8.from_buffer_copy
+    return (fmt, new(_pack_q8(kp, k0, k1, k2, k_exps.data_ptr(), *k_exps.stride())),
+            new(_pack_q8(vp, v0, v1, v2, v_exps.data_ptr(), *v_exps.stride())), shape)
 
 
 def pair_pages_extend(lens, held, n_new, free_pages, free_count, block_table, page_size, T,
@@ -634,11 +633,13 @@ def pair_cache_append_q8(k, v, slots, k_codes, k_exps, v_codes, v_exps, dev_err=
               _strided(v, "v", k.dtype, (T, H, D), k, at))
     slots_p = _ptr(slots, "slots", torch.int64, (T,), k, at)
     fmt, kc, vc, shape = _cache_q8(k_codes, k_exps, v_codes, v_exps, k, at)
-    if shape[2] != H or shape[3] != D:
+    pages, page, heads, size = shape
+    if heads != H or size != D:
         raise ValueError("k_codes must have %d heads of %d, got %s" % (H, D, tuple(shape)))
-    _call("pair_cache_append_q8", k, stream, T, H, D, dt, kp, k.stride(0), k.stride(1), vp,
-          v.stride(0), v.stride(1), slots_p, shape[0], shape[1], fmt, kc, vc,
-          _err_ptr(dev_err, k, at))
+    k_row, k_head, _ = k.stride()
+    v_row, v_head, _ = v.stride()
+    _call("pair_cache_append_q8", k, stream, T, H, D, dt, kp, k_row, k_head, vp, v_row, v_head,
+          slots_p, pages, page, fmt, kc, vc, _err_ptr(dev_err, k, at))
     return k_codes, k_exps, v_codes, v_exps
 
 
@@ -650,17 +651,16 @@ def pair_cache_read_q8(slots, k_codes, k_exps, v_codes, v_exps, dtype=torch.bflo
     at, T = _index(slots, "slots"), slots.numel()
     slots_p = _ptr(slots, "slots", torch.int64, (T,), slots, at)
     fmt, kc, vc, (pages, page, H, D) = _cache_q8(k_codes, k_exps, v_codes, v_exps, slots, at)
-    given = k if k is not None else v
-    dtype = dtype if given is None else given.dtype
-    outs = []
-    for name, t in (("k", k), ("v", v)):
-        if t is None:
-            t = _fresh((T, H, D), dtype, slots, stream)
-        outs += [t, _strided(t, name, dtype, (T, H, D), slots, at)]
-    k, kp, v, vp = outs
+    dtype, shape = dtype if k is None and v is None else (v if k is None else k).dtype, (T, H, D)
+    if k is None:
+        k = _fresh(shape, dtype, slots, stream)
+    if v is None:
+        v = _fresh(shape, dtype, slots, stream)
+    kp, vp = _strided(k, "k", dtype, shape, slots, at), _strided(v, "v", dtype, shape, slots, at)
+    k_row, k_head, _ = k.stride()
+    v_row, v_head, _ = v.stride()
     _call("pair_cache_read_q8", slots, stream, T, H, D, slots_p, pages, page, fmt, kc, vc,
-          _pair_dtype(k, "k"), kp, k.stride(0), k.stride(1), vp, v.stride(0), v.stride(1),
-          _err_ptr(dev_err, slots, at))
+          _pair_dtype(k, "k"), kp, k_row, k_head, vp, v_row, v_head, _err_ptr(dev_err, slots, at))
     return k, v
 
 
@@ -709,7 +709,8 @@ def pair_attend_paged_q8(q, k_codes, k_exps, v_codes, v_exps, block_table, kv_le
     dt, at, i32 = _pair_dtype(q, "q"), _index(q, "q"), torch.int32
     qp = _strided(q, "q", q.dtype, (T, Hq, D), q, at)
     fmt, kc, vc, shape = _cache_q8(k_codes, k_exps, v_codes, v_exps, q, at)
-    if shape[3] != D:
+    pages, page, heads, size = shape
+    if size != D:
         raise ValueError("k_codes must have heads of %d, got %s" % (D, tuple(shape)))
     R, width = block_table.shape
     table = _ptr(block_table, "block_table", i32, (R, width), q, at)
@@ -718,11 +719,12 @@ def pair_attend_paged_q8(q, k_codes, k_exps, v_codes, v_exps, block_table, kv_le
     out, out_p = _out_ptr(out, "out", q.dtype, (T, Hq, D), q, at, stream)
     lse, lse_p = _out_ptr(lse, "lse", torch.float32, (T, Hq), q, at, stream)
     if ws is None:
-        need = pair_attend_workspace_size(R, Hq, shape[2], D, dt)
+        need = pair_attend_workspace_size(R, Hq, heads, D, dt)
         ws = _fresh((max(need, 256),), torch.uint8, q, stream)
     n = ws.numel()
-    _call("pair_attend_paged_q8", q, stream, T, R, Hq, shape[2], D, dt, qp, q.stride(0),
-          q.stride(1), fmt, kc, vc, shape[0], shape[1], table, width, lens, cu,
+    q_row, q_head, _ = q.stride()
+    _call("pair_attend_paged_q8", q, stream, T, R, Hq, heads, D, dt, qp, q_row, q_head, fmt, kc, vc,
+          pages, page, table, width, lens, cu,
           D ** -0.5 if scale is None else float(scale), int(max_new), out_p, lse_p,
           _ptr(ws, "ws", torch.uint8, (n,), q, at), n, _err_ptr(dev_err, q, at))
     return out, lse
