@@ -17,23 +17,18 @@ __device__ __forceinline__ void from_float(__nv_bfloat16 *o, float x) {
   *o = __float2bfloat16_rn(x);
 }
 
-// F: the cache's codes, or q8::kPlain for one in fp32.
-template <int D, int F>
+template <int D>
 struct SimtSmem {
-  static constexpr bool kHeld = F != q8::kPlain;
   static constexpr int kKeys = D == 64 ? 64 : 32;
   static constexpr int kStages = 3;
-  using E = std::conditional_t<kHeld, uint8_t, float>;  // an entry of the cache
-  static constexpr int kPer = 16 / sizeof(E);           // of them in 16 bytes
-  E k[kStages][kKeys][D + kPer];
-  E v[kStages][kKeys][D];
+  float k[kStages][kKeys][D + 4];
+  float v[kStages][kKeys][D];
   float q[kSimtRows][D];
   float p[kSimtRows][kKeys];
   float m[kSimtRows], l[kSimtRows], fix[kSimtRows];
   int64_t row[2][2][kKeys];  // offsets of a tile's keys and values
   int seen[kSimtRows];
   int64_t scratch[kSimtThreads / 32 + 2];
-  float e[kHeld ? kStages : 1][2][kHeld ? kKeys : 1];  // scales of a tile's rows
 };
 
 // fp32 products on the CUDA cores, 16 rows against tiles of keys and values
@@ -44,17 +39,12 @@ struct SimtSmem {
 // latency at small sizes (three barriers and two exchanges per tile; 32 requests
 // of up to 640 keys, heads of 64: 22 us with the joining pass), else by
 // shared-memory reads.
-//
-// Over a cache in 8 bits the tiles hold the codes, which become fp32 where they are
-// read; a key's scale multiplies its scores, a value's its weights.
-template <int D, int F>
+template <int D>
 __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   extern __shared__ __align__(16) uint8_t raw[];
-  using S = SimtSmem<D, F>;
-  using E = typename S::E;
+  using S = SimtSmem<D>;
   S &sm = *reinterpret_cast<S *>(raw);
   constexpr int M = kSimtRows, BN = S::kKeys, NST = S::kStages, V4 = D / 4;
-  constexpr int PER = S::kPer, VE = D / PER;  // entries of 16 bytes; such pieces of a row
   constexpr int QR = M * BN / kSimtThreads;                      // rows of a thread's scores
   constexpr int QG = M / QR;                                     // groups of them
   constexpr int CPT = D >= kSimtThreads ? D / kSimtThreads : 1;  // columns per thread
@@ -67,7 +57,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   if (cta == ctas - 1) report_requests(a);
   Walk<M, BN> walk{find_share<kSimtThreads>(a, M, cta, ctas, sm.scratch)};
   const float *q = static_cast<const float *>(a.q);
-  const E *kc = static_cast<const E *>(a.kc), *vc = static_cast<const E *>(a.vc);
+  const float *kc = static_cast<const float *>(a.kc), *vc = static_cast<const float *>(a.vc);
   const float scale = a.scale * kLog2e;
   const int col = tid % (kSimtThreads / RG), rg = tid / (kSimtThreads / RG);
   Segment s;
@@ -82,19 +72,14 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         const int id = key < s.keys ? page_of(a, s.i, key, &off) : -1;
         sm.row[t & 1][0][tid] = id < 0 ? -1 : cache_row(a, a.ks, id, off, s.h);
         sm.row[t & 1][1][tid] = id < 0 ? -1 : cache_row(a, a.vs, id, off, s.h);
-        if constexpr (S::kHeld) {
-          float *e = sm.e[(t - s.t0) % NST][0] + tid;
-          e[0] = id < 0 ? 0.f : q8::scale_of(a.ke[cache_row(a, a.kes, id, off, s.h)]);
-          e[BN] = id < 0 ? 0.f : q8::scale_of(a.ve[cache_row(a, a.ves, id, off, s.h)]);
-        }
       }
     };
     auto fetch = [&](int t) {
       if (t < s.t1) {
         const int st = (t - s.t0) % NST;
 #pragma unroll 4
-        for (int x = tid; x < BN * VE; x += kSimtThreads) {
-          const int k = x / VE, c = x % VE * PER;
+        for (int x = tid; x < BN * V4; x += kSimtThreads) {
+          const int k = x / V4, c = x % V4 * 4;
           const int64_t ko = sm.row[t & 1][0][k], vo = sm.row[t & 1][1][k];
           cp_async16(tc::smem_u32(&sm.k[st][k][c]), kc + (ko < 0 ? 0 : ko + c), ko >= 0);
           cp_async16(tc::smem_u32(&sm.v[st][k][c]), vc + (vo < 0 ? 0 : vo + c), vo >= 0);
@@ -137,32 +122,15 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
       {
         const int k = tid % BN, g0 = tid / BN;  // rows g0, g0 + QG, ..
         float acc[QR] = {};
-        auto add = [&](const float4 &x, int d) {
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+          const float4 x = *reinterpret_cast<const float4 *>(&sm.k[st][k][d]);
 #pragma unroll
           for (int r = 0; r < QR; ++r) {
             if (r * QG >= s.rows) break;
             const float4 y = *reinterpret_cast<const float4 *>(&sm.q[r * QG + g0][d]);
             acc[r] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, acc[r]))));
           }
-        };
-        if constexpr (S::kHeld) {
-#pragma unroll 1
-          for (int d = 0; d < D; d += 16) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(&sm.k[st][k][d]);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              float x[4];
-              q8::decode4<F>(w[c], x);
-              add(make_float4(x[0], x[1], x[2], x[3]), d + c * 4);
-            }
-          }
-          const float e = sm.e[st][0][k];
-#pragma unroll
-          for (int r = 0; r < QR; ++r) acc[r] *= e;
-        } else {
-#pragma unroll 4
-          for (int d = 0; d < D; d += 4) add(*reinterpret_cast<const float4 *>(&sm.k[st][k][d]), d);
         }
 #pragma unroll
         for (int r = 0; r < QR; ++r)
@@ -195,7 +163,6 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
         for (int x = 0; x < BN / 32; ++x) {
           sc[r][x] = exp2f(sc[r][x] - ref);
           sum[r] += sc[r][x];
-          if constexpr (S::kHeld) sc[r][x] *= sm.e[st][1][lane + 32 * x];
           sm.p[warp * (M / 4) + r][lane + 32 * x] = sc[r][x];
         }
       }
@@ -227,10 +194,7 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
 #pragma unroll
         for (int y = 0; y < 4; ++y)
 #pragma unroll
-          for (int c = 0; c < CPT; ++c) {
-            const E x = sm.v[st][k + y][col + c * kSimtThreads];
-            if constexpr (S::kHeld) v[y][c] = q8::decode1<F>(x); else v[y][c] = x;
-          }
+          for (int c = 0; c < CPT; ++c) v[y][c] = sm.v[st][k + y][col + c * kSimtThreads];
 #pragma unroll
         for (int r = 0; r < RPT; ++r) {
           if (r * RG >= s.rows) break;
@@ -382,18 +346,17 @@ __global__ void __launch_bounds__(kJoinThreads)
   }
 }
 
-template <int D, int F>
+template <int D>
 pair_status run_simt(Launch *l, cudaStream_t s) {
   Args &a = l->a;
   a.unit_cost = kSimtCost;
-  constexpr int smem = sizeof(SimtSmem<D, F>);
+  constexpr int smem = sizeof(SimtSmem<D>);
   static_assert(smem <= 232448, "shared memory of a CTA");
-  const auto kernel = attend_simt_kernel<D, F>;
-  PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel,
+  PAIR_CUDA_TRY(cudaFuncSetAttribute(attend_simt_kernel<D>,
                                      cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   const int ctas = useful_ctas(a, kSimtRows, min(kMaxCtas, (D <= 128 ? 2 : 1) * sm_count()));
-  PAIR_BEGIN(F == q8::kPlain ? "attend_simt" : "attend_simt_q8", s);
-  kernel<<<ctas, kSimtThreads, smem, s>>>(a);
+  PAIR_BEGIN("attend_simt", s);
+  attend_simt_kernel<D><<<ctas, kSimtThreads, smem, s>>>(a);
   PAIR_LAUNCH_CHECK(s);
   l->M = kSimtRows;
   l->ctas = ctas;
@@ -460,13 +423,8 @@ int sm_count() {
   return n;
 }
 
-pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s) {
-  return by_size(D, [&](auto d) {
-    constexpr int n = decltype(d)::value;
-    return fmt == q8::kPlain ? run_simt<n, q8::kPlain>(l, s)
-           : fmt == q8::kI8  ? run_simt<n, q8::kI8>(l, s)
-                             : run_simt<n, q8::kE4M3>(l, s);
-  });
+pair_status launch_simt(Launch *l, int D, cudaStream_t s) {
+  return by_size(D, [&](auto d) { return run_simt<decltype(d)::value>(l, s); });
 }
 
 static pair_status launch_join(const Launch &l0, const Launch &l1, int D, pair_dtype dt,
@@ -512,7 +470,7 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   if (!ws || ws_bytes < need || !aligned(ws, 256)) return PAIR_ERR_WORKSPACE;
   const pair_status dv = check_device();
   if (dv != PAIR_OK) return dv;
-  const size_t notes = held && dt == PAIR_BF16 ? kHeldNotes : kNotes;
+  const size_t notes = held ? kHeldNotes : kNotes;
   const Args a{T,
                R,
                Hq,
@@ -555,22 +513,22 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   // Which kernel a chunk goes to is decided by its rows, on the device; a
   // launch is left out where the host knows that no chunk can be its.
   const int64_t most_rows = (int64_t)(max_new > 0 && max_new < T ? max_new : T) * a.g;
-  const bool simt = dt == PAIR_F32;
-  const bool only_few = simt || most_rows <= kFewRows ||
+  const bool only_few = dt == PAIR_F32 || most_rows <= kFewRows ||
                         !(held ? many_applies_q8(a, D) : many_applies(a, D));
   if (!only_few && R > 1) {
     few.a.rows_upto = kFewRows;
     many.a.rows_over = kFewRows;
   }
   pair_status st = PAIR_OK;
-  if (simt) {
-    st = launch_simt(&few, D, fmt, s);
-  } else if (held && (only_few || R > 1)) {
+  if (held && (only_few || R > 1)) {
     const float *end = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + need);
     const int64_t room = (only_few ? end : many.a.part) - few.a.part;
-    const int slots = (int)(room / part_floats(kFewTile, D));
-    st = fmt == q8::kI8 ? launch_few_i8(&few, D, most_rows, slots, s)
-                        : launch_few_e4m3(&few, D, most_rows, slots, s);
+    FewLauncher *const launch = dt == PAIR_BF16
+                                    ? (fmt == q8::kI8 ? launch_few_i8 : launch_few_e4m3)
+                                    : (fmt == q8::kI8 ? launch_few_i8_f32 : launch_few_e4m3_f32);
+    st = launch(&few, D, most_rows, (int)(room / part_floats(kFewTile, D)), s);
+  } else if (dt == PAIR_F32) {
+    st = launch_simt(&few, D, s);
   } else if (only_few || R > 1) {
     st = launch_few(&few, D, s);
   }

@@ -422,12 +422,12 @@ struct Launch {
   Args a;
   int M, ctas;  // rows of its units; 0 CTAs: there is no such launch
 };
-pair_status launch_simt(Launch *l, int D, int fmt, cudaStream_t s);
+pair_status launch_simt(Launch *l, int D, cudaStream_t s);
 pair_status launch_few(Launch *l, int D, cudaStream_t s);
 // Caches in 8 bits; most_rows: of a chunk, as far as the host knows.
 // slots: partial sums of kFewTile rows that the workspace has room for.
-pair_status launch_few_i8(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s);
-pair_status launch_few_e4m3(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s);
+using FewLauncher = pair_status(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s);
+FewLauncher launch_few_i8, launch_few_e4m3, launch_few_i8_f32, launch_few_e4m3_f32;
 bool many_applies(const Args &a, int D);
 pair_status launch_many(Launch *l, int D, cudaStream_t s);
 bool many_applies_q8(const Args &a, int D);

@@ -1,5 +1,5 @@
-// pair_attend_paged_q8 for chunks with few rows (single tokens, drafts), bf16 queries:
-// one pass over the cached codes, bound by HBM.
+// pair_attend_paged_q8 for chunks with few rows (single tokens, drafts), and in fp32 for
+// all: one pass over the cached codes.
 //
 // The products are formed the other way round, S^T = K Q^T and O^T += V^T P^T, with
 // mma.sync: the keys (then the head's columns) are the 16 rows of a product and the
@@ -14,6 +14,12 @@
 // V: codes become bf16 (exact), against weights exp(s - max) 2^(b - 127) in bf16: they
 // carry the value's scale and want the exponent range. Each weight is off by up to 2^-8
 // of itself, independently, while their sum takes them unrounded in fp32.
+//
+// fp32 queries: the stored numbers are exact in either type all the same, so only the other
+// operand is split. A query entry is two fp16 numbers (22 bits, down to 2^-39 of the
+// row's largest), a weight three bf16 ones (24 bits): two products for one, and three. The
+// tensor cores need not round to nearest; four products at most are summed there, and
+// those sums by rounded additions.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -139,17 +145,43 @@ struct Place {
   }
 };
 
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, bool there, float (&v)[8]) {
+  const uint4 u = there ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0);
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] = __uint_as_float(w[k] << 16);
+    v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load8(const float *p, bool there, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 4) {
+    const float4 u = there ? *reinterpret_cast<const float4 *>(p + k) : make_float4(0, 0, 0, 0);
+    v[k] = u.x, v[k + 1] = u.y, v[k + 2] = u.z, v[k + 3] = u.w;
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8]) {
+  *reinterpret_cast<uint4 *>(p) = make_uint4(
+      bits(__floats2bfloat162_rn(v[0], v[1])), bits(__floats2bfloat162_rn(v[2], v[3])),
+      bits(__floats2bfloat162_rn(v[4], v[5])), bits(__floats2bfloat162_rn(v[6], v[7])));
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+  reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+
 // Shared memory of a warp whose units have up to M rows.
-template <int D, int M>
+template <typename T, int D, int M>
 struct Few {
   static constexpr int kStages = 2;
   static constexpr int kPart = kSlice * D;     // bytes of a slice of keys or values
-  static constexpr int kPieces = D / 16;       // 16-byte pieces of a row
   static constexpr int kSteps = D / 16;        // steps of 16 columns in K Q^T
   static constexpr int kRing = 0;              // [kStages][keys, values]
   static constexpr int kPtr = kRing + kStages * 2 * kPart;  // [kSlice] addresses of both
   static constexpr int kQ = kPtr + kSlice * 16;  // [M / 8][kSteps / 2][32 lanes] 16 bytes
-  static constexpr int kFactor = kQ + M * D * 2;  // [M] scales of the queries
+  static constexpr int kRest = M * D * 2;  // from there to what fp32 queries have beyond fp16
+  static constexpr int kFactor = kQ + M * D * (int)sizeof(T);  // [M] scales of the queries
   static constexpr int kPlace = kFactor + M * 4;  // a Place
   static constexpr int kWarpBytes = (kPlace + (int)sizeof(Place<M>) + 127) / 128 * 128;
   static constexpr int kBytes = kWarps * kWarpBytes;
@@ -169,9 +201,9 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
 }
 
 // The copies of a slice's rows, whose addresses are at `ptrs`.
-template <int D, int M, bool value>
+template <int D, bool value>
 __device__ __forceinline__ void bring(uint32_t to, uint32_t ptrs) {
-  constexpr int P = Few<D, M>::kPieces, RP = 32 / P;  // rows of one round of copies
+  constexpr int P = D / 16, RP = 32 / P;  // pieces of a row, rows of one round of copies
   const int lane = threadIdx.x & 31, c = lane % P;
 #pragma unroll
   for (int x = 0; x < kSlice / RP; ++x) {
@@ -216,10 +248,10 @@ __device__ __forceinline__ void look_ahead(const Args &a, Stream &m) {
 // Starts the copies of the keys that were looked up, into half `stage` of the ring, reads
 // their exponents and keeps where their values lie. Keys that do not exist are the cache's
 // first: they are masked.
-template <int D, int M>
+template <typename T, int D, int M>
 __device__ __forceinline__ void bring_keys(const Args &a, const Segment &s, Stream &m, int stage,
                                            uint32_t base) {
-  using L = Few<D, M>;
+  using L = Few<T, D, M>;
   const int lane = threadIdx.x & 31;
   int pg = m.id, o = m.off;
   if (m.key >= m.end) pg = 0, o = 0;
@@ -247,24 +279,24 @@ __device__ __forceinline__ void bring_keys(const Args &a, const Segment &s, Stre
   asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + lane * 8), "l"(kp) : "memory");
   asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + (kSlice + lane) * 8), "l"(vp) : "memory");
   __syncwarp();
-  bring<D, M, false>(base + L::kRing + stage * 2 * L::kPart, ptrs);
+  bring<D, false>(base + L::kRing + stage * 2 * L::kPart, ptrs);
 }
 
 // The first two slices of a segment, on their way. Copies are in groups of their own, of
 // keys and of values in turn: a slice's keys have been used when its values have not, and
 // are followed by those of the next slice but one.
-template <int D, int M>
+template <typename T, int D, int M>
 __device__ __forceinline__ void begin_copies(const Args &a, const Segment &s, Stream &m,
                                              uint32_t base) {
-  using L = Few<D, M>;
+  using L = Few<T, D, M>;
   Stream n = m;  // of the second slice: both slices' pages are on their way
   if (m.slices > 1) look_ahead(a, n);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
-    if (x < m.slices) bring_keys<D, M>(a, s, x ? n : m, x, base);
+    if (x < m.slices) bring_keys<T, D, M>(a, s, x ? n : m, x, base);
     cp_async_commit();
     if (x < m.slices)
-      bring<D, M, true>(base + L::kRing + (x * 2 + 1) * L::kPart, base + L::kPtr + kSlice * 8);
+      bring<D, true>(base + L::kRing + (x * 2 + 1) * L::kPart, base + L::kPtr + kSlice * 8);
     cp_async_commit();
     __syncwarp();
   }
@@ -275,12 +307,14 @@ __device__ __forceinline__ void begin_copies(const Args &a, const Segment &s, St
 
 // A warp's segment of up to 8 NT rows. Its first slices are on their way; when it ends,
 // those of the segment after it are (if there is one).
-template <int D, int F, int M, int NT>
+template <typename T, int D, int F, int M, int NT>
 __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Stream &m,
                                             const Place<M> &place_of, uint8_t *smem, float *part) {
-  using L = Few<D, M>;
+  using L = Few<T, D, M>;
   constexpr int MT = kSlice / 16;
   constexpr int DT = D / 16;  // tiles of 16 columns in O^T
+  constexpr bool f32 = sizeof(T) == 4;
+  constexpr int NP = f32 ? 3 : 1;  // bf16 numbers to a weight
   const int lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
   const uint32_t base = smem_u32(smem);
@@ -293,19 +327,16 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
   // row g, the places of the four codes of a word.
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
-    const __nv_bfloat16 *q = static_cast<const __nv_bfloat16 *>(a.q);
     const int r = j * 8 + g;
-    uint4 u[D / 32];
+    float v[D / 32][8];
     uint32_t top = 0;
     const RowAt w = row_at(a, s.row0, s.r0, s.h, r < s.rows ? r : 0);
-    const __nv_bfloat16 *src = q + w.token * a.q_row + w.head * a.q_head + 16 * t;
+    const T *src = static_cast<const T *>(a.q) + w.token * a.q_row + w.head * a.q_head + 16 * t;
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) {
-      u[x] = r < s.rows ? *reinterpret_cast<const uint4 *>(src + 64 * (x >> 1) + 8 * (x & 1))
-                        : make_uint4(0, 0, 0, 0);
-      const uint32_t y[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
+      load8(src + 64 * (x >> 1) + 8 * (x & 1), r < s.rows, v[x]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) top = max(top, max(y[k] & 0x7fff0000u, (y[k] & 0x7fffu) << 16));
+      for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[x][k]) & 0x7fffffffu);
     }
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
@@ -313,16 +344,21 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
     const uint32_t e = min(max((int)(top >> 23) - 14, 1), 253);
     const float up = __uint_as_float((254 - e) << 23);
     if (t == 0) factor[r] = __uint_as_float(e << 23);
-    uint4 *dst = reinterpret_cast<uint4 *>(smem + L::kQ) + j * (L::kSteps / 2) * 32 + lane;
+    uint8_t *dst = smem + L::kQ + (j * (L::kSteps / 2) * 32 + lane) * 16;
 #pragma unroll
     for (int x = 0; x < D / 32; ++x) {
-      const uint32_t y[4] = {u[x].x, u[x].y, u[x].z, u[x].w};
-      uint32_t h[4];
+      uint32_t h[4], rest[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        h[k] = bits(__floats2half2_rn(__uint_as_float(y[k] << 16) * up,
-                                      __uint_as_float(y[k] & 0xffff0000u) * up));
-      dst[x * 32] = make_uint4(h[0], h[1], h[2], h[3]);
+      for (int k = 0; k < 4; ++k) {
+        const float y0 = v[x][2 * k] * up, y1 = v[x][2 * k + 1] * up;
+        const __half2 z = __floats2half2_rn(y0, y1);
+        h[k] = bits(z);
+        if (f32) rest[k] = bits(__floats2half2_rn(y0 - __low2float(z), y1 - __high2float(z)));
+      }
+      *reinterpret_cast<uint4 *>(dst + x * 512) = make_uint4(h[0], h[1], h[2], h[3]);
+      if (f32)
+        *reinterpret_cast<uint4 *>(dst + L::kRest + x * 512) =
+            make_uint4(rest[0], rest[1], rest[2], rest[3]);
     }
   }
   __syncwarp();
@@ -382,11 +418,26 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
           }
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          const uint4 b = lds128(q_at + (j * (L::kSteps / 2) + 2 * y + p) * 512);
+          const uint32_t b_at = q_at + (j * (L::kSteps / 2) + 2 * y + p) * 512;
+          const uint4 b = lds128(b_at);
+          if constexpr (f32) {
+            const uint4 b1 = lds128(b_at + L::kRest);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            mma_f16(sc[i][j], f[0][i], b.x, b.y);
-            mma_f16(sc[i][j], f[1][i], b.z, b.w);
+            for (int i = 0; i < MT; ++i) {
+              float part_of[4] = {};  // sums of 32 columns, joined by rounded additions
+              mma_f16(part_of, f[0][i], b1.x, b1.y);
+              mma_f16(part_of, f[1][i], b1.z, b1.w);
+              mma_f16(part_of, f[0][i], b.x, b.y);
+              mma_f16(part_of, f[1][i], b.z, b.w);
+#pragma unroll
+              for (int c = 0; c < 4; ++c) sc[i][j][c] += part_of[c];
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              mma_f16(sc[i][j], f[0][i], b.x, b.y);
+              mma_f16(sc[i][j], f[1][i], b.z, b.w);
+            }
           }
         }
       }
@@ -455,7 +506,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
     }
     __syncwarp();  // nobody reads these keys any more
     m.kb = m.kb1, m.vb = m.vb1;
-    if (x + 2 < slices) bring_keys<D, M>(a, s, m, x & 1, base);
+    if (x + 2 < slices) bring_keys<T, D, M>(a, s, m, x & 1, base);
     cp_async_commit();
     if (x + 3 < slices) look_ahead(a, m);
     cp_async_wait<3>();  // this slice's values are there
@@ -482,12 +533,17 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
           for (int c = 0; c < 4; ++c)
             if (key0 + i * 16 + g + 8 * (c >> 1) >= seen[j][c & 1]) w[j][c] = 0.f;
       }
-      uint32_t p[NT][2];
+      uint32_t p[NT][NP][2];
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        p[j][0] = transposed(bits(__floats2bfloat162_rn(w[j][0], w[j][1])));
-        p[j][1] = transposed(bits(__floats2bfloat162_rn(w[j][2], w[j][3])));
-      }
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int y = 0; y < NP; ++y)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(w[j][2 * h], w[j][2 * h + 1]);
+            p[j][y][h] = transposed(bits(z));
+            if (f32) w[j][2 * h] -= __low2float(z), w[j][2 * h + 1] -= __high2float(z);
+          }
       // Values of the lane's keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9: 16 columns (8 for heads
       // of 64), two of a product's 16 at a time.
       constexpr int W = D == 64 ? 2 : 4;  // words
@@ -515,19 +571,30 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
             const uint32_t f[4] = {to_bf16<F, 0>(z0), to_bf16<F, 1>(z0), to_bf16<F, 0>(z1),
                                    to_bf16<F, 1>(z1)};
 #pragma unroll
-            for (int j = 0; j < NT; ++j) mma_bf(o[(y * W + w) * 2 + h][j], f, p[j][0], p[j][1]);
+            for (int j = 0; j < NT; ++j) {
+              float(&to)[4] = o[(y * W + w) * 2 + h][j];
+              if constexpr (f32) {
+                float part_of[4] = {};
+#pragma unroll
+                for (int z = NP - 1; z >= 0; --z) mma_bf(part_of, f, p[j][z][0], p[j][z][1]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) to[c] += part_of[c];
+              } else {
+                mma_bf(to, f, p[j][0][0], p[j][0][1]);
+              }
+            }
           }
       }
     }
     __syncwarp();  // nor these values
-    if (x + 2 < slices) bring<D, M, true>(vs, base + L::kPtr + kSlice * 8);
+    if (x + 2 < slices) bring<D, true>(vs, base + L::kPtr + kSlice * 8);
     cp_async_commit();
   }
   // The next segment's first slices, then this one's sums: lane (g, t) has 16 columns (8
   // for heads of 64) of the rows 8 j + 2 t and the one behind.
   if (place_of.more) {
     begin_stream(a, place_of.next, m);
-    begin_copies<D, M>(a, place_of.next, m, base);
+    begin_copies<T, D, M>(a, place_of.next, m, base);
   }
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -542,17 +609,16 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
       if (!part) {
         const RowAt w = row_at(a, s.row0, s.r0, s.h, r);
         const float inv = sum == 0.f ? 0.f : kValueUnit<F> / sum;
-        __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(a.out) +
-                            (w.token * a.Hq + w.head) * D + C * g;
+        T *to = static_cast<T *>(a.out) + (w.token * a.Hq + w.head) * D + C * g;
 #pragma unroll
-        for (int y = 0; y < DT * 2 / 8; ++y) {
-          uint32_t u[4];
+        for (int y = 0; y < DT / 4; ++y) {
+          float v[8];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            u[k] = bits(__floats2bfloat162_rn(o[y * 4 + k][j][c] * inv,
-                                              o[y * 4 + k][j][c + 2] * inv));
-          *reinterpret_cast<uint4 *>(to + (y >> 1) * 128 + (y & 1) * 8) =
-              make_uint4(u[0], u[1], u[2], u[3]);
+          for (int k = 0; k < 4; ++k) {
+            v[2 * k] = o[y * 4 + k][j][c] * inv;
+            v[2 * k + 1] = o[y * 4 + k][j][c + 2] * inv;
+          }
+          store8(to + (y >> 1) * 128 + (y & 1) * 8, v);
         }
         if (g == 0 && a.lse)
           a.lse[w.token * a.Hq + w.head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -572,22 +638,22 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 }
 
 // CTAs of an SM.
-template <int D, int M>
-constexpr int kPerSm = D == 256 ? 1 : M == 8 ? 3 : 2;
+template <typename T, int D, int M>
+constexpr int kPerSm = D == 256 ? 1 : M == 8 && D * sizeof(T) <= 256 ? 3 : 2;
 
 // A unit is worked on by one warp from end to end, 32 keys at a time, but where shares
 // meet. Nothing waits for another warp. Every warp has a share of the work of its own, or,
 // where key heads come in fours, a CTA has one of four heads at once: its warps then read
 // the same tokens, whose heads lie side by side in a cache by token.
-template <int D, int F, int M>
-__global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(Args a) {
-  using L = Few<D, M>;
+template <typename T, int D, int F, int M>
+__global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kernel(Args a) {
+  using L = Few<T, D, M>;
   extern __shared__ __align__(128) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int worker = blockIdx.x * kWarps + warp;
   if (a.rows_upto < INT32_MAX) let_next_start();  // the kernel for many rows
   if (lane < 2) a.desc[worker * 2 + lane] = {0, 0, 0, 0, 0, 0, 0, 0};
-  clear_spare_rows<__nv_bfloat16, D, kThreads>(a, blockIdx.x, gridDim.x);
+  clear_spare_rows<T, D, kThreads>(a, blockIdx.x, gridDim.x);
   if (blockIdx.x == gridDim.x - 1) report_requests(a);
   int64_t *scratch = reinterpret_cast<int64_t *>(smem);
   const Share share =
@@ -603,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(A
   m.kb = m.vb = m.kb1 = m.vb1 = 0;
   if (p.more) {
     begin_stream(a, p.next, m);
-    begin_copies<D, M>(a, p.next, m, smem_u32(mine));
+    begin_copies<T, D, M>(a, p.next, m, smem_u32(mine));
   }
   for (int seg = 0; p.more; ++seg) {
     const Segment s = p.next;
@@ -616,24 +682,24 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, M>) attend_q8_few_kernel(A
       part = a.part + slot * part_floats(M, D);
     }
     if (M == 8 || s.rows <= 8)
-      few_segment<D, F, M, 1>(a, s, m, p, mine, part);
+      few_segment<T, D, F, M, 1>(a, s, m, p, mine, part);
     else if (M == 16 || (M == 32 && s.rows <= 16))
-      few_segment<D, F, M, M < 16 ? 1 : 2>(a, s, m, p, mine, part);
+      few_segment<T, D, F, M, M < 16 ? 1 : 2>(a, s, m, p, mine, part);
     else if (M == 24 || s.rows <= 24)
-      few_segment<D, F, M, M < 24 ? 1 : 3>(a, s, m, p, mine, part);
+      few_segment<T, D, F, M, M < 24 ? 1 : 3>(a, s, m, p, mine, part);
     else
-      few_segment<D, F, M, M < 32 ? 1 : 4>(a, s, m, p, mine, part);
+      few_segment<T, D, F, M, M < 32 ? 1 : 4>(a, s, m, p, mine, part);
     __syncwarp();  // all lanes have seen `more`
   }
   let_next_start();
 }
 
-template <int D, int F, int M>
+template <typename T, int D, int F, int M>
 pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   Args &a = l->a;
-  constexpr int smem = Few<D, M>::kBytes;
-  static_assert(kPerSm<D, M> * (smem + 1024) <= 233472, "shared memory of an SM");
-  const auto kernel = attend_q8_few_kernel<D, F, M>;
+  constexpr int smem = Few<T, D, M>::kBytes;
+  static_assert(kPerSm<T, D, M> * (smem + 1024) <= 233472, "shared memory of an SM");
+  const auto kernel = attend_q8_few_kernel<T, D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   a.unit_cost = 96;
   a.slice_pages = kSlice / a.page;
@@ -642,7 +708,7 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   for (const pair_cache_strides *x : {&a.ks, &a.vs, &a.kes, &a.ves})
     a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
   const int fit = min(slots * (kFewTile / M) / 2,  // two partial sums each
-                      min(kMaxWorkers, kPerSm<D, M> * kWarps * sm_count()));
+                      min(kMaxWorkers, kPerSm<T, D, M> * kWarps * sm_count()));
   // Where key heads come in fours a CTA's warps take four of them over the same keys.
   const bool together = a.Hkv % kWarps == 0;
   if (together) a.heads = a.Hkv / kWarps;
@@ -657,19 +723,22 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   return PAIR_OK;
 }
 
-template <int D, int F>
+template <typename T, int D, int F>
 pair_status run_few(Launch *l, int64_t most_rows, int slots, cudaStream_t s) {
-  if (most_rows <= 8) return run_few<D, F, 8>(l, slots, s);
-  if (most_rows <= 16) return run_few<D, F, 16>(l, slots, s);
-  if (most_rows <= 24) return run_few<D, F, 24>(l, slots, s);
-  return run_few<D, F, 32>(l, slots, s);
+  if constexpr (D < 256 || sizeof(T) == 4)
+    if (most_rows <= 8) return run_few<T, D, F, 8>(l, slots, s);
+  if constexpr (D < 256 && sizeof(T) == 2) {
+    if (most_rows > 24) return run_few<T, D, F, 32>(l, slots, s);
+    if (most_rows > 16) return run_few<T, D, F, 24>(l, slots, s);
+  }
+  return run_few<T, D, F, 16>(l, slots, s);
 }
 
-template <int F>
+template <typename T, int F>
 pair_status run_few(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s) {
-  if (D == 64) return run_few<64, F>(l, most_rows, slots, s);
-  if (D == 128) return run_few<128, F>(l, most_rows, slots, s);
-  return run_few<256, F, 16>(l, slots, s);
+  if (D == 64) return run_few<T, 64, F>(l, most_rows, slots, s);
+  if (D == 128) return run_few<T, 128, F>(l, most_rows, slots, s);
+  return run_few<T, 256, F>(l, most_rows, slots, s);
 }
 
 }  // namespace

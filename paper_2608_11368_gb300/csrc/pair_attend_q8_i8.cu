@@ -1,11 +1,11 @@
-// pair_attend_paged_q8 for chunks with few rows: codes that are whole numbers.
+// pair_attend_paged_q8 for chunks with few rows: bf16 queries over codes that are whole numbers.
 #include "pair_attend_q8_few.cuh"
 
 namespace pairk {
 namespace attend {
 
 pair_status launch_few_i8(Launch *l, int D, int64_t most_rows, int slots, cudaStream_t s) {
-  return run_few<kI8>(l, D, most_rows, slots, s);
+  return run_few<__nv_bfloat16, kI8>(l, D, most_rows, slots, s);
 }
 
 }  // namespace attend
