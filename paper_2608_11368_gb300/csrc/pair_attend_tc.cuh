@@ -307,21 +307,28 @@ __device__ void softmax(const Args &a, S &sm, Walk<M, BN> walk, int cta) {
   uint32_t s_ph = 0, pv_ph = 0;
   bool ok = true;
   const int r = w * 128 + row;
-  // This row's query, in the K-major swizzled layout of the A operand.
+  // The warp's queries, in the K-major swizzled layout of the A operand: whole rows at a
+  // time, D / 8 lanes to each.
   auto put_query = [&](const Segment &g) {
     if (g.t0 == g.t1 || (w == 1 && g.rows <= 128)) return;
     const bool there = r < g.rows && a.scale != 0.f;
     const RowAt at = row_at(a, g.row0, g.r0, g.h, r < g.rows ? r : 0);
-    const __nv_bfloat16 *src = q + at.token * a.q_row + at.head * a.q_head;
-    uint4 u[D / 8];
+    const uint64_t mine =
+        there ? reinterpret_cast<uint64_t>(q + at.token * a.q_row + at.head * a.q_head) : 0;
+    constexpr int per = D / 8, RP = 32 / per;  // lanes of a row, rows at once
+    const int lane = tid & 31, c = lane % per;
+    uint4 u[per];
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c)
-      u[c] = there ? *reinterpret_cast<const uint4 *>(src + c * 8) : make_uint4(0, 0, 0, 0);
+    for (int x = 0; x < per; ++x) {
+      const uint64_t src = __shfl_sync(0xffffffffu, mine, x * RP + lane / per);
+      u[x] = src ? *(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
+    }
 #pragma unroll
-    for (int c = 0; c < D / 8; ++c) {
-      u[c].x ^= flip, u[c].y ^= flip, u[c].z ^= flip, u[c].w ^= flip;
-      *reinterpret_cast<uint4 *>(sm.q[w] + (c >> 3) * C::kAtom + row * 128 +
-                                 (((c & 7) ^ (row & 7)) << 4)) = u[c];
+    for (int x = 0; x < per; ++x) {
+      const int to = (row & ~31) + x * RP + lane / per;
+      u[x].x ^= flip, u[x].y ^= flip, u[x].z ^= flip, u[x].w ^= flip;
+      *reinterpret_cast<uint4 *>(sm.q[w] + (c >> 3) * C::kAtom + to * 128 +
+                                 (((c & 7) ^ (to & 7)) << 4)) = u[x];
     }
     fence_async_smem();
     warp_arrive(&sm.q_full[w]);
@@ -351,6 +358,7 @@ __device__ void softmax(const Args &a, S &sm, Walk<M, BN> walk, int cta) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int upto = seen - key0 - c * 32;  // by selects: rows end at different keys
+            if (__all_sync(0xffffffffu, upto >= 32)) continue;
 #pragma unroll
             for (int k = 0; k < 32; ++k) x[c][k] = k >= upto ? 0xff800000u : x[c][k];  // -inf
           }
