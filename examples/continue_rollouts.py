@@ -13,7 +13,9 @@ generated in between, on one GPU:
 
 The policy is a random single attention layer with an output head; the drafter
 is the head applied to the embedding of the last token. Run it with
-    python examples/continue_rollouts.py
+    python examples/continue_rollouts.py [bf16 | int8 | e4m3]
+by what the cache is to hold (pair_cache_append_q8 and pair_attend_paged_q8 for
+the latter two).
 """
 import os
 import sys
@@ -48,11 +50,17 @@ class Policy:
 
 
 class Cache:
-    """Pages of all requests and the list of free ones, on the device."""
+    """Pages of all requests and the list of free ones, on the device; keys and values
+    in bf16, or as codes of 8 bits (torch.int8, torch.float8_e4m3fn) with exponents."""
 
-    def __init__(self, policy, R, pages, page, width):
+    def __init__(self, policy, R, pages, page, width, dtype=torch.bfloat16):
         shape = (pages, page, policy.Hkv, policy.D)
-        self.k, self.v = (torch.zeros(shape, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        self.codes = dtype != torch.bfloat16
+        self.parts = []
+        for _ in "kv":
+            self.parts.append(torch.zeros(shape, dtype=dtype, device="cuda"))
+            if self.codes:
+                self.parts.append(torch.zeros(shape[:3], dtype=torch.uint8, device="cuda"))
         self.page = page
         self.table = torch.zeros((R, width), dtype=torch.int32, device="cuda")
         self.lens = torch.zeros(R, dtype=torch.int32, device="cuda")
@@ -71,25 +79,32 @@ class Cache:
         self.count = self.count - taken
         return kv_len, cu, slots
 
+    def append(self, k, v, slots, err):
+        call = B.pair_cache_append_q8 if self.codes else B.pair_cache_append
+        call(k, v, slots, *self.parts, dev_err=err)
+
+    def attend(self, q, kv_len, cu, max_new, err):
+        call = B.pair_attend_paged_q8 if self.codes else B.pair_attend_paged
+        return call(q, *self.parts, self.table, kv_len, cu, max_new=max_new, dev_err=err)[0]
+
 
 def chunk(policy, cache, ids, n_new, T, err, max_new=0):
     """Hidden states [T, d] of a chunk of tokens per request, which go into the
     cache; and the chunks' offsets."""
     kv_len, cu, slots = cache.extend(n_new, T, err)
     q, k, v = policy.qkv(ids)
-    B.pair_cache_append(k, v, slots, cache.k, cache.v, dev_err=err)
-    out, _ = B.pair_attend_paged(q, cache.k, cache.v, cache.table, kv_len, cu, max_new=max_new,
-                                 dev_err=err)
-    return out.view(T, policy.d), cu
+    cache.append(k, v, slots, err)
+    return cache.attend(q, kv_len, cu, max_new, err).view(T, policy.d), cu
 
 
-def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, seed=0):
+def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, seed=0,
+         cache_dtype=torch.bfloat16):
     g = torch.Generator(device="cuda").manual_seed(seed)
     policy = Policy(V, 4, 2, 128, g)
     R, n = prompts * G, drafts + 1
     err = torch.zeros(1, dtype=torch.int32, device="cuda")
     longest = prompt_len + steps * n
-    cache = Cache(policy, R, R * (longest // page + 2), page, longest // page + 2)
+    cache = Cache(policy, R, R * (longest // page + 2), page, longest // page + 2, cache_dtype)
 
     # Which rollouts go on: the design's probabilities, and the draw.
     p_hat = 0.05 + 0.9 * torch.rand((prompts, G), generator=g, device="cuda")
@@ -168,8 +183,7 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
     logp_tokens = torch.cat([logp_all[i, 1:len(s)] for i, s in enumerate(seq)])
     logp_old = logp_all.sum(1)
     q, _, _ = policy.qkv(ids)
-    hidden, _ = B.pair_attend_paged(q, cache.k, cache.v, cache.table, cache.lens, cu_seq,
-                                    max_new=int(made.max()), dev_err=err)
+    hidden = cache.attend(q, cache.lens, cu_seq, int(made.max()), err)
     hidden = (8.0 * hidden.view(T, policy.d)).contiguous()  # the policy's sharpness
     Jobj, dH, dW, logp_seq, coef = B.pair_grad_clipped(
         hidden, policy.head, y, torch.ones(T, dtype=torch.uint8, device="cuda"), cu_seq,
@@ -181,8 +195,10 @@ def main(prompts=4, G=8, prompt_len=100, steps=24, drafts=3, V=4096, page=16, se
                 drafts=drafts)
 
 
+CACHES = {"bf16": torch.bfloat16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
 if __name__ == "__main__":
-    o = main()
+    o = main(cache_dtype=CACHES[sys.argv[1] if len(sys.argv) > 1 else "bf16"])
     going = o["J"].view(-1).bool()
     print("status %d, %d of %d rollouts continued, %d tokens, %.2f per step and rollout"
           % (o["status"], int(going.sum()), going.numel(), int(o["made"].sum()),

@@ -515,6 +515,7 @@ PAIR_API pair_status pair_grad_noalloc(int64_t T, int32_t d, int32_t V,
  *     pair_cache_append   the chunk's keys and values into those slots,
  *     pair_attend_paged   the chunk's queries over the request's cache,
  *     pair_verify_drafts  the drafts against the target's probabilities.
+ * (The cache may be held in 8 bits: pair_cache_append_q8, pair_attend_paged_q8.)
  * Requests are packed: request i owns the rows [cu_new[i], cu_new[i+1]) of
  * the step's arrays (none for a request that the design stopped). All lengths
  * stay on the device, so a step needs no host synchronisation and can be
@@ -654,7 +655,9 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  * b is the least byte with which the row's largest entry does not round beyond
  * the largest code, and every code is its entry's nearest (halves to even), so
  * codes do not depend on the device. b = 255: the row had a NaN or an infinity;
- * it holds NaN. The scales are powers of two: a stored value is a bf16 number.
+ * it holds NaN. (No other row has codes that are not numbers; what e4m3's two
+ * such codes count as in a row that a caller made is not defined.) The scales
+ * are powers of two: a stored value is a bf16 number.
  */
 typedef struct {
   void *codes;                 /* int8 or e4m3, strides in elements (bytes) */
@@ -701,11 +704,17 @@ PAIR_API pair_status pair_cache_read_q8(int64_t T, int32_t Hkv, int32_t D, const
 
 /*
  * pair_attend_paged_q8 -- pair_attend_paged over caches in 8 bits: the same
- * sums over the stored values, in the same arithmetic (the values are exact in
- * it), with the same conventions, workspace (pair_attend_workspace_size for dt)
- * and errors. dt is the type of q and out; no stride is asked of the exponent
- * bytes. A row that holds NaN counts like a NaN: with a row that sees it, and
- * with no other.
+ * sums over the stored values, which are exact in the arithmetic, with the same
+ * conventions, workspace (pair_attend_workspace_size for dt) and errors. dt is
+ * the type of q and out; nothing is asked of the exponent bytes' strides. A key
+ * or value that holds NaN makes the rows that see it NaN, and no others.
+ * Arithmetic: PAIR_BF16 as for pair_attend_paged. PAIR_F32: on the tensor cores
+ * too, queries as sums of two fp16 numbers (22 bits, down to 2^-39 of a row's
+ * largest entry) and weights of three bf16 ones (24 bits), sums in fp32.
+ * max_new is of more use here than there: chunks of few rows have kernels for 8,
+ * 16, 24 and 32 of them per key head, by what it says. Chunks of more go to the
+ * tensor cores' kernel for many rows where D is 64 or 128 and pages are a
+ * multiple of 8 tokens.
  */
 PAIR_API pair_status pair_attend_paged_q8(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
                                           pair_dtype dt, const void *q, int64_t q_row,

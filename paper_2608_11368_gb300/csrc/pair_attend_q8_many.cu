@@ -159,6 +159,14 @@ __device__ void scout(const Args &a, const Maps &maps, SmemQ8<D> &sm, SharedWalk
   const bool mine = lane * box < BN;
   bool ok = true;
   while (ok && walk.next(a, &s)) {
+    // Of a unit that comes next, the queries too are fetched from afar beforehand.
+    for (int r = lane; r < s.rows; r += 32) {
+      const RowAt w = row_at(a, s.row0, s.r0, s.h, r);
+      const uint8_t *p = static_cast<const uint8_t *>(a.q) +
+                         (w.token * a.q_row + w.head * a.q_head) * sizeof(__nv_bfloat16);
+      for (int x = 0; x < D * 2; x += 128)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p + x));
+    }
     const int32_t *table = a.table + (int64_t)s.i * a.width;
     int key = s.t0 * BN + lane * box, at = key / a.page, off = key - at * a.page;
     int id = mine && key < s.keys ? table[at] : 0;

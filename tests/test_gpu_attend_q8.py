@@ -351,3 +351,45 @@ def test_a_step_as_it_is_used():
             # 2 sides x 2 2^-24 (D size + keys + 16), sizes (scale sum |q_d k_d|) below 16.
             assert ((lse - wlse).abs()[~same] <= 6e-4).all()
             lens = kv
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_offsets_beyond_32_bits(wide):
+    """Pages more than 4 GiB into the cache, by a page's number or by its stride."""
+    from paper_2608_11368_gb300 import binding as B
+    H, D, page = 4, 128, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    raw = torch.zeros((1 << 32) + (1 << 26), dtype=torch.int8, device="cuda")
+    size = page * H * D
+    if wide:  # two pages, 2^32 + 2^15 bytes apart; keys and values side by side
+        pages, stride = 2, (1 << 32) + (1 << 15)
+        k, v = (raw.as_strided((2, page, H, D), (stride, H * D, D, 1), x * size * 2) for x in (0, 1))
+        own = [0, 1]
+    else:
+        pages = (1 << 32) // size + 100
+        k = v = raw[:pages * size].view(pages, page, H, D)
+        own = [3, pages - 1]
+    ke = torch.full((pages, page, H), 255, dtype=torch.uint8, device="cuda")
+    ve = ke if not wide else ke.clone()
+    n = 100  # the first page and some of the second
+    x = torch.randn((n, H, D), generator=g, device="cuda")
+    pos = torch.arange(n, device="cuda")
+    slots = torch.tensor(own, device="cuda")[pos // page] * page + pos % page
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.pair_cache_append_q8(x, x, slots, k, ke, v, ve, dev_err=err)
+    back, _ = B.pair_cache_read_q8(slots, k, ke, v, ve, dtype=torch.float32, dev_err=err)
+    want = rollout.values_q8(*rollout.store_q8(x.double().cpu().numpy(), "i8"))
+    assert np.array_equal(back.double().cpu().numpy(), want)
+    table = torch.tensor([own], dtype=torch.int32, device="cuda")
+    for dtype, rows in ((torch.bfloat16, 1), (torch.bfloat16, 60), (torch.float32, 5)):
+        q = torch.randn((rows, 2 * H, D), generator=g, device="cuda").to(dtype)
+        out, _ = B.pair_attend_paged_q8(
+            q, k, ke, v, ve, table, torch.tensor([n], dtype=torch.int32, device="cuda"),
+            torch.tensor([0, rows], dtype=torch.int32, device="cuda"), dev_err=err)
+        two = [want.reshape(1, n, H, D)] * 2
+        ro, _, mag, _ = rollout.attend_paged(q.double().cpu().numpy(), *two, np.zeros((1, 1), int),
+                                             [n], [0, rows], D ** -0.5)
+        # Two roundings to bf16 of 2^-8 at most, or sums in fp32.
+        rel = 2 * 2.0 ** -8 * 1.02 if dtype == torch.bfloat16 else 2.0 ** -12
+        assert (np.abs(out.double().cpu().numpy() - ro) <= rel * mag).all()
+    assert B.pair_status_sync(err) == 0
