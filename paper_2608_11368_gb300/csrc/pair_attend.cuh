@@ -71,7 +71,7 @@ struct Args {
   const uint8_t *ke, *ve;
   pair_cache_strides kes, ves;
   bool narrow;        // strides of pages and tokens fit in 32 bits
-  int32_t slice_pages, slice_rest;  // 32 keys further in the block table: pages, places
+  int32_t slice_pages, slice_rest;  // a slice further in the block table: pages, places
   int32_t heads;      // key heads on the line of units (a fourth where warps share a CTA's)
   int32_t unit_cost;  // fixed cost of a unit of this launch, in keys
 };

@@ -38,7 +38,9 @@ using q8::kI8;
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int BN = 128;           // keys of a tile: 32 for each warp
-constexpr int kSlice = 32;        // keys that a warp works on at once
+// Keys that a warp works on at once: 16 where slices of 32 would leave an SM four warps.
+template <int D>
+constexpr int kSlice = D == 256 ? 16 : 32;
 
 __device__ __forceinline__ uint32_t bits(__nv_bfloat162 x) {
   return *reinterpret_cast<const uint32_t *>(&x);
@@ -175,11 +177,11 @@ __device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
 template <typename T, int D, int M>
 struct Few {
   static constexpr int kStages = 2;
-  static constexpr int kPart = kSlice * D;     // bytes of a slice of keys or values
+  static constexpr int kPart = kSlice<D> * D;     // bytes of a slice of keys or values
   static constexpr int kSteps = D / 16;        // steps of 16 columns in K Q^T
   static constexpr int kRing = 0;              // [kStages][keys, values]
   static constexpr int kPtr = kRing + kStages * 2 * kPart;  // [kSlice] addresses of both
-  static constexpr int kQ = kPtr + kSlice * 16;  // [M / 8][kSteps / 2][32 lanes] 16 bytes
+  static constexpr int kQ = kPtr + kSlice<D> * 16;  // [M / 8][kSteps / 2][32 lanes] 16 bytes
   static constexpr int kRest = M * D * 2;  // from there to what fp32 queries have beyond fp16
   static constexpr int kFactor = kQ + M * D * (int)sizeof(T);  // [M] scales of the queries
   static constexpr int kPlace = kFactor + M * 4;  // a Place
@@ -206,7 +208,7 @@ __device__ __forceinline__ void bring(uint32_t to, uint32_t ptrs) {
   constexpr int P = D / 16, RP = 32 / P;  // pieces of a row, rows of one round of copies
   const int lane = threadIdx.x & 31, c = lane % P;
 #pragma unroll
-  for (int x = 0; x < kSlice / RP; ++x) {
+  for (int x = 0; x < kSlice<D> / RP; ++x) {
     const int r = x * RP + lane / P;
     const uint8_t *p;
     asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(ptrs + r * 8) : "memory");
@@ -225,18 +227,20 @@ struct Stream {
 };
 
 // The slices of a segment, and the page of this lane's first key.
+template <int D>
 __device__ __forceinline__ void begin_stream(const Args &a, const Segment &s, Stream &m) {
   const int first = s.t0 * BN;
   m.row = a.table + (int64_t)s.i * a.width;
   m.end = min(s.keys, s.t1 * BN);
-  m.slices = first < m.end ? (m.end - first + kSlice - 1) / kSlice : 0;
+  m.slices = first < m.end ? (m.end - first + kSlice<D> - 1) / kSlice<D> : 0;
   m.key = first + (threadIdx.x & 31);
   m.at = m.key / a.page;
   m.off = m.key - m.at * a.page;
   m.id = m.key < m.end ? m.row[m.at] : 0;
 }
+template <int D>
 __device__ __forceinline__ void look_ahead(const Args &a, Stream &m) {
-  m.key += kSlice;
+  m.key += kSlice<D>;
   m.at += a.slice_pages;
   m.off += a.slice_rest;
   if (m.off >= a.page) {
@@ -276,8 +280,11 @@ __device__ __forceinline__ void bring_keys(const Args &a, const Segment &s, Stre
   m.kb1 = __ldg(ke);
   m.vb1 = __ldg(ve);
   const uint32_t ptrs = base + L::kPtr;
-  asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + lane * 8), "l"(kp) : "memory");
-  asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + (kSlice + lane) * 8), "l"(vp) : "memory");
+  if (lane < kSlice<D>) {
+    asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + lane * 8), "l"(kp) : "memory");
+    asm volatile("st.shared.b64 [%0], %1;" ::"r"(ptrs + (kSlice<D> + lane) * 8), "l"(vp)
+                 : "memory");
+  }
   __syncwarp();
   bring<D, false>(base + L::kRing + stage * 2 * L::kPart, ptrs);
 }
@@ -290,19 +297,19 @@ __device__ __forceinline__ void begin_copies(const Args &a, const Segment &s, St
                                              uint32_t base) {
   using L = Few<T, D, M>;
   Stream n = m;  // of the second slice: both slices' pages are on their way
-  if (m.slices > 1) look_ahead(a, n);
+  if (m.slices > 1) look_ahead<D>(a, n);
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     if (x < m.slices) bring_keys<T, D, M>(a, s, x ? n : m, x, base);
     cp_async_commit();
     if (x < m.slices)
-      bring<D, true>(base + L::kRing + (x * 2 + 1) * L::kPart, base + L::kPtr + kSlice * 8);
+      bring<D, true>(base + L::kRing + (x * 2 + 1) * L::kPart, base + L::kPtr + kSlice<D> * 8);
     cp_async_commit();
     __syncwarp();
   }
   n.kb = m.kb1, n.vb = m.vb1;
   m = n;
-  if (m.slices > 2) look_ahead(a, m);
+  if (m.slices > 2) look_ahead<D>(a, m);
 }
 
 // A warp's segment of up to 8 NT rows. Its first slices are on their way; when it ends,
@@ -311,7 +318,7 @@ template <typename T, int D, int F, int M, int NT>
 __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Stream &m,
                                             const Place<M> &place_of, uint8_t *smem, float *part) {
   using L = Few<T, D, M>;
-  constexpr int MT = kSlice / 16;
+  constexpr int MT = kSlice<D> / 16;
   constexpr int DT = D / 16;  // tiles of 16 columns in O^T
   constexpr bool f32 = sizeof(T) == 4;
   constexpr int NP = f32 ? 3 : 1;  // bf16 numbers to a weight
@@ -389,7 +396,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
     cp_async_wait<3>();  // this slice's keys are there
     __syncwarp();
     const uint32_t ks = base + L::kRing + (x & 1) * 2 * L::kPart, vs = ks + L::kPart;
-    const int key0 = first + x * kSlice;
+    const int key0 = first + x * kSlice<D>;
     // Scores of 32 keys with 8 NT rows.
     float sc[MT][NT][4];
 #pragma unroll
@@ -458,7 +465,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
           sc[i][j][c] = y.x, sc[i][j][c + 1] = y.y;
         }
     }
-    const bool edge = key0 + kSlice > least;
+    const bool edge = key0 + kSlice<D> > least;
     if (edge) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -508,7 +515,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
     m.kb = m.kb1, m.vb = m.vb1;
     if (x + 2 < slices) bring_keys<T, D, M>(a, s, m, x & 1, base);
     cp_async_commit();
-    if (x + 3 < slices) look_ahead(a, m);
+    if (x + 3 < slices) look_ahead<D>(a, m);
     cp_async_wait<3>();  // this slice's values are there
     __syncwarp();
 #pragma unroll
@@ -587,13 +594,13 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
       }
     }
     __syncwarp();  // nor these values
-    if (x + 2 < slices) bring<D, true>(vs, base + L::kPtr + kSlice * 8);
+    if (x + 2 < slices) bring<D, true>(vs, base + L::kPtr + kSlice<D> * 8);
     cp_async_commit();
   }
   // The next segment's first slices, then this one's sums: lane (g, t) has 16 columns (8
   // for heads of 64) of the rows 8 j + 2 t and the one behind.
   if (place_of.more) {
-    begin_stream(a, place_of.next, m);
+    begin_stream<D>(a, place_of.next, m);
     begin_copies<T, D, M>(a, place_of.next, m, base);
   }
 #pragma unroll
@@ -639,7 +646,9 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 
 // CTAs of an SM.
 template <typename T, int D, int M>
-constexpr int kPerSm = D == 256 ? 1 : M == 8 && D * sizeof(T) <= 256 ? 3 : 2;
+constexpr int kPerSm = 2 * (Few<T, D, M>::kBytes + 1024) > 233472 ? 1
+                       : M == 8 && D * sizeof(T) <= 256           ? 3
+                                                                  : 2;
 
 // A unit is worked on by one warp from end to end, 32 keys at a time, but where shares
 // meet. Nothing waits for another warp. Every warp has a share of the work of its own, or,
@@ -668,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kerne
   Stream m;
   m.kb = m.vb = m.kb1 = m.vb1 = 0;
   if (p.more) {
-    begin_stream(a, p.next, m);
+    begin_stream<D>(a, p.next, m);
     begin_copies<T, D, M>(a, p.next, m, smem_u32(mine));
   }
   for (int seg = 0; p.more; ++seg) {
@@ -702,8 +711,8 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   const auto kernel = attend_q8_few_kernel<T, D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   a.unit_cost = 96;
-  a.slice_pages = kSlice / a.page;
-  a.slice_rest = kSlice % a.page;
+  a.slice_pages = kSlice<D> / a.page;
+  a.slice_rest = kSlice<D> % a.page;
   a.narrow = true;
   for (const pair_cache_strides *x : {&a.ks, &a.vs, &a.kes, &a.ves})
     a.narrow &= (uint64_t)x->for_page <= UINT32_MAX && (uint64_t)x->for_token <= UINT32_MAX;
