@@ -446,9 +446,10 @@ static pair_status attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, i
   reset_launches();
   const bool held = fmt != q8::kPlain;
   if (T < 1 || T > INT32_MAX || R < 1 || R > kMaxRequests || Hkv < 1 || Hq < Hkv ||
-      Hq % Hkv != 0 || !q || !k.codes || !v.codes || (held && (!k.exps || !v.exps)) || num_pages < 1 || page_size < 1 ||
-      !block_table || table_width < 1 || !kv_len || !cu_new || !out || !(fabsf(scale) <= 3.0e38f) ||
-      max_new < 0 || (dt != PAIR_F32 && dt != PAIR_BF16) || T * (Hq / Hkv) > INT32_MAX)
+      Hq % Hkv != 0 || !q || !k.codes || !v.codes || (held && (!k.exps || !v.exps)) ||
+      num_pages < 1 || page_size < 1 || !block_table || table_width < 1 || !kv_len || !cu_new ||
+      !out || !(fabsf(scale) <= 3.0e38f) || max_new < 0 || (dt != PAIR_F32 && dt != PAIR_BF16) ||
+      T * (Hq / Hkv) > INT32_MAX)
     return PAIR_ERR_INVALID_ARG;
   const int per = dt == PAIR_BF16 ? 8 : 4;  // elements of 16 bytes
   // A stride over a single entry says nothing; a tensor map wants one all the same.

@@ -5,7 +5,16 @@
 // mma.sync: the keys (then the head's columns) are the 16 rows of a product and the
 // query rows its 8 columns, so four rows of a single token leave half of a product
 // empty and not three quarters, and every code is made a number once for all rows of
-// a warp. With numbers of 8 bits that conversion is what the issue slots go to.
+// a warp. mma.sync rather than tcgen05: so few rows cannot fill a tile of 128.
+//
+// 32 x 16 requests of 1500 tokens as the median (2.1 GB of codes, prompts of 256 tokens
+// shared by 16 of them counted once): 352 us by token, 332 by head in e4m3. The copies
+// alone, without the products, take 340 by head: the shared prompts come from memory again
+// for nearly every request, 2.36 GB, so that is HBM's rate. Whole numbers leave no room
+// beside the copies: of 715 instructions for 32 keys and 8 rows 350 make codes into
+// numbers. With five rows of four heads (16 x 16 requests of 512 to 4096 tokens, 1.0 GB)
+// 316 us: 1050 instructions for 32 keys and 24 rows, 0.43 of them issued per cycle by two
+// warps a scheduler; registers (254) admit no more.
 //
 // K: codes become fp16 (exact, five instructions for four whole numbers), against
 // queries in fp16 that are scaled by a power of two per row: the row's largest entry is
@@ -113,7 +122,8 @@ __device__ __forceinline__ void to_half(uint32_t w, uint32_t &lo, uint32_t &hi) 
 }
 
 // The codes in the low (hi = 0) or the high bytes of both halves of x in bf16, over
-// kValueUnit.
+// kValueUnit. (Whole numbers by two masks and a subtraction instead of a mask and a
+// multiply-add: 416 us instead of 366 for five rows of four heads.)
 template <int F>
 constexpr float kValueUnit = F == kI8 ? 64.f : 1.f;
 template <int F, int hi>
@@ -291,7 +301,8 @@ __device__ __forceinline__ void bring_keys(const Args &a, const Segment &s, Stre
 
 // The first two slices of a segment, on their way. Copies are in groups of their own, of
 // keys and of values in turn: a slice's keys have been used when its values have not, and
-// are followed by those of the next slice but one.
+// are followed by those of the next slice but one (whole slices, one ahead: 382 us instead
+// of 358 for five rows of four heads).
 template <typename T, int D, int M>
 __device__ __forceinline__ void begin_copies(const Args &a, const Segment &s, Stream &m,
                                              uint32_t base) {
@@ -650,10 +661,12 @@ constexpr int kPerSm = 2 * (Few<T, D, M>::kBytes + 1024) > 233472 ? 1
                        : M == 8 && D * sizeof(T) <= 256           ? 3
                                                                   : 2;
 
-// A unit is worked on by one warp from end to end, 32 keys at a time, but where shares
-// meet. Nothing waits for another warp. Every warp has a share of the work of its own, or,
-// where key heads come in fours, a CTA has one of four heads at once: its warps then read
-// the same tokens, whose heads lie side by side in a cache by token.
+// A unit is worked on by one warp from end to end, a slice of keys at a time, but where
+// shares meet. Nothing waits for another warp (four warps over one unit's keys, their sums
+// joined at its end: 442 us instead of 391 for the skewed requests). Every warp has a share
+// of the work of its own, or, where key heads come in fours, a CTA has one of four heads at
+// once: its warps then read the same tokens, whose heads lie side by side in a cache by
+// token (405 us -> 351). Three CTAs an SM for up to 8 rows (two: 419), two for more.
 template <typename T, int D, int F, int M>
 __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kernel(Args a) {
   using L = Few<T, D, M>;
@@ -710,7 +723,7 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   static_assert(kPerSm<T, D, M> * (smem + 1024) <= 233472, "shared memory of an SM");
   const auto kernel = attend_q8_few_kernel<T, D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  a.unit_cost = 96;
+  a.unit_cost = 96;  // 192: 360 us instead of 350 for the skewed requests by head
   a.slice_pages = kSlice<D> / a.page;
   a.slice_rest = kSlice<D> % a.page;
   a.narrow = true;

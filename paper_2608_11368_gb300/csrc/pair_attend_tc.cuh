@@ -530,8 +530,8 @@ inline bool cache_map(CUtensorMap *m, int8_t (&at)[3], const void *p, const Args
     boxes[x + 1] = want[order[x]];
     at[order[x]] = (int8_t)(x + 1);
   }
-  return fn(m, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void *>(p), dims, strides, boxes,
-            ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return fn(m, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4,
+            const_cast<void *>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
             size * D == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

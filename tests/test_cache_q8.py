@@ -41,7 +41,7 @@ def test_stored_form_by_hand():
                           ([np.inf, 1.0], [0, 0], 255), ([np.nan, 1.0], [0, 0], 255)):
         c, e = rollout.store_q8(np.array([row]), "i8")
         assert c[0].tolist() == codes and e[0] == b
-    for row, codes, b in (([448.0, 17.0], [448, 16], 127), ([463.9, 0.001], [448, 2.0 ** -9 * 1], 127),
+    for row, codes, b in (([448.0, 17.0], [448, 16], 127), ([463.9, 0.001], [448, 2.0 ** -9], 127),
                           ([464.0, 1.0], [224, 0.5], 128), ([480.0, 1.0], [240, 0.5], 128),
                           ([19.0, 1.0], [320, 16], 123)):
         c, e = rollout.store_q8(np.array([row]), "e4m3")
@@ -81,7 +81,8 @@ def _checks(L):
               (cache(at=S(2048 + 8, 128, 64)), 1), (cache(at=S(2048, 128, 72)), 1),
               (cache(at=S(2048, 136, 64)), 1)]
     p = P(one)
-    good = [8, 2, 64, L.PAIR_BF16, p, 128, 64, p, 128, 64, p, 9, 16, 0, cache(), cache(), None, None]
+    good = [8, 2, 64, L.PAIR_BF16, p, 128, 64, p, 128, 64, p, 9, 16, 0, cache(), cache(), None,
+            None]
     refusals(lib.pair_cache_append_q8, good,
              [(0, 0, 1), (0, big, 1), (1, 0, 1), (2, 0, 1), (2, 8, 1), (2, 72, 1), (2, 272, 1),
               (3, 7, 1), (4, None, 1), (4, P(odd), 1), (5, 129, 1), (6, 63, 1), (7, None, 1),

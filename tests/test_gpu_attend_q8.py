@@ -252,8 +252,11 @@ def test_bad_pages_and_lengths_are_reported():
 def test_same_results_every_time_on_any_stream_and_captured(n):
     from paper_2608_11368_gb300 import binding as B
     t = build([(n, 2000 + 100 * i) for i in range(9)], 8, 2, 128, 16, torch.bfloat16, "i8", seed=n)
-    call = lambda **kw: B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"],  # noqa: E731
-                                               t["cu"], max_new=n, **kw)
+
+    def call(**kw):
+        return B.pair_attend_paged_q8(t["q"], *t["held"], t["table"], t["kv"], t["cu"], max_new=n,
+                                      **kw)
+
     first = [x.clone() for x in call()]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -363,7 +366,8 @@ def test_offsets_beyond_32_bits(wide):
     size = page * H * D
     if wide:  # two pages, 2^32 + 2^15 bytes apart; keys and values side by side
         pages, stride = 2, (1 << 32) + (1 << 15)
-        k, v = (raw.as_strided((2, page, H, D), (stride, H * D, D, 1), x * size * 2) for x in (0, 1))
+        k, v = (raw.as_strided((2, page, H, D), (stride, H * D, D, 1), x * size * 2)
+                for x in range(2))
         own = [0, 1]
     else:
         pages = (1 << 32) // size + 100
