@@ -11,7 +11,9 @@ library ``libpair.so`` (header ``include/pair.h``):
 * ``pair_estimate_dense``: Eq. (pair-ht) for explicit score vectors;
 * ``pair_pages_extend``, ``pair_cache_append``, ``pair_attend_paged``,
   ``pair_verify_drafts``: a step of generating the continued rollouts, from a
-  paged cache and with drafted tokens.
+  paged cache and with drafted tokens;
+* ``pair_cache_append_q8``, ``pair_attend_paged_q8``, ``pair_cache_read_q8``:
+  the same cache in 8 bits.
 
 ``binding`` wraps those entry points for torch tensors (argument marshalling
 only). ``synth`` draws seeded synthetic workloads. Importing this package
