@@ -242,85 +242,100 @@ __global__ void __launch_bounds__(kSimtThreads) attend_simt_kernel(Args a) {
   let_next_start();
 }
 
-constexpr int kJoinThreads = 256;
-
-// Blocks that share the rows of one of a launch's units: 32 rows each.
-__host__ __device__ inline int join_blocks(const Launch &l) {
+// Blocks that share the rows of one of a launch's units: 4 rows a warp.
+template <int NT>
+__host__ __device__ int join_blocks(const Launch &l) {
   int64_t rows = l.a.T * l.a.g;
   if (rows > l.M) rows = l.M;
   if (rows > l.a.rows_upto) rows = l.a.rows_upto;
-  return (int)((rows + 31) / 32);
+  return (int)((rows + NT / 8 - 1) / (NT / 8));
 }
 
 // Joins the partial sums of the units that more than one CTA worked on, of one
 // launch or of two: blocks of the CTA that has a unit's beginning. The other
 // pieces are the first segments of the CTAs behind. Sums go in the order of the
-// keys. Bound by latency (notes, then statistics, then sums) and, after a launch
-// with many rows, by the 40 MB of its partial sums.
-template <typename T, int D>
-__global__ void __launch_bounds__(kJoinThreads)
+// keys. Bound by latency (notes, then sums, whose loads do not wait for the maxima) and,
+// after a launch with many rows, by the 40 MB of its partial sums. NT threads, each with B
+// floats of partial sums on their way.
+template <typename T, int D, int NT, int B>
+__global__ void __launch_bounds__(NT)
     attend_join_kernel(const __grid_constant__ Launch l0, const __grid_constant__ Launch l1) {
-  const int first = l0.ctas * join_blocks(l0);  // blocks of the first launch's sums
+  const int first = l0.ctas * join_blocks<NT>(l0);  // blocks of the first launch's sums
   const bool second = (int)blockIdx.x >= first;
   const Args &a = second ? l1.a : l0.a;
   const int M = second ? l1.M : l0.M, ctas = second ? l1.ctas : l0.ctas;
-  const int per = join_blocks(second ? l1 : l0);
+  const int per = join_blocks<NT>(second ? l1 : l0);
   const int block = blockIdx.x - (second ? first : 0);
   const int cta = block / per, y = block - cta * per;
-  __shared__ int slots[kMaxWorkers];
+  __shared__ uint16_t slots[kMaxWorkers];
   __shared__ int n_slots;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   wait_for_previous();
   // A CTA has the beginning of one unit at most whose end it does not have.
   const Desc d0 = a.desc[cta * 2], d1 = a.desc[cta * 2 + 1];
+  Desc e{};  // notes of the CTAs behind, 32 at a time
+  if (warp == 0 && cta + 1 + lane < ctas) e = a.desc[(cta + 1 + lane) * 2];
   const bool is0 = d0.tiles != 0 && d0.t0 == 0;
   const Desc d = is0 ? d0 : d1;
   if (d.tiles == 0 || d.t0 != 0) return;
   const int mine = cta * 2 + (is0 ? 0 : 1);
-  const Request req = request(a, d.i);
   if (warp == 0) {
     int n = 1;
     if (lane == 0) slots[0] = mine;
     bool more = true;
     for (int c0 = cta + 1; more && c0 < ctas; c0 += 32) {
       const int c = c0 + lane;
-      Desc e{};
-      if (c < ctas) e = a.desc[c * 2];
       const bool in = e.tiles > 0 && e.i == d.i && e.h == d.h && e.rt == d.rt;
       const unsigned ins = __ballot_sync(0xffffffffu, in);
       if (in) slots[n + __popc(ins & ((1u << lane) - 1))] = c * 2;
       n += __popc(ins);
       more = !__any_sync(0xffffffffu, in && e.t1 == e.tiles);
+      if (more) e = c + 32 < ctas ? a.desc[(c + 32) * 2] : Desc{};
     }
     if (lane == 0) n_slots = n;
   }
   __syncthreads();
   const int n = n_slots;
-  const int rows = min(M, req.n * a.g - d.rt * M);
-  constexpr int kWarps = kJoinThreads / 32, C = D / 32;
+  constexpr int kWarps = NT / 32, C = D / 32;
+  constexpr int P = B / C;  // partial sums on their way to a lane
   // With few partial sums a warp takes a row; with many (a long unit over many
   // CTAs) the warps share a row's, in runs, and the first adds up what they have.
   const bool share = n >= 2 * kWarps;
   const int k0 = share ? warp * n / kWarps : 0, k1 = share ? (warp + 1) * n / kWarps : n;
   const int step = share ? per : per * kWarps;
-  for (int r = share ? y : y * kWarps + warp; r < rows; r += step) {
+  for (int r = share ? y : y * kWarps + warp; r < d.rows; r += step) {
+    float2 x[P][C / 2];
+    float m[P], sum[P];
+    const auto bring = [&](int k) {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (k + i < k1) {
+          const float *p = a.part + slots[k + i] * part_floats(M, D);
+          m[i] = p[r], sum[i] = p[M + r];
+          const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * C);
+#pragma unroll
+          for (int c = 0; c < C / 2; ++c) x[i][c] = src[c];
+        }
+    };
     float mx = -INFINITY;
     for (int k = lane; k < n; k += 32) mx = fmaxf(mx, a.part[slots[k] * part_floats(M, D) + r]);
+    bring(k0);  // beside the maxima
     for (int w = 16; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
     const float ref = mx == -INFINITY ? 0.f : mx;
     float l = 0.f, o[C] = {};
-#pragma unroll 4
-    for (int k = k0; k < k1; ++k) {
-      const float *p = a.part + slots[k] * part_floats(M, D);
-      const float f = exp2f(p[r] - ref);
-      l = fmaf(p[M + r], f, l);
-      const float2 *src = reinterpret_cast<const float2 *>(p + 2 * M + r * D + lane * C);
+    for (int k = k0; k < k1; k += P) {
+      if (k > k0) bring(k);
 #pragma unroll
-      for (int c = 0; c < C / 2; ++c) {
-        const float2 x = src[c];
-        o[2 * c] = fmaf(x.x, f, o[2 * c]);
-        o[2 * c + 1] = fmaf(x.y, f, o[2 * c + 1]);
-      }
+      for (int i = 0; i < P; ++i)
+        if (k + i < k1) {
+          const float f = exp2f(m[i] - ref);
+          l = fmaf(sum[i], f, l);
+#pragma unroll
+          for (int c = 0; c < C / 2; ++c) {
+            o[2 * c] = fmaf(x[i][c].x, f, o[2 * c]);
+            o[2 * c + 1] = fmaf(x[i][c].y, f, o[2 * c + 1]);
+          }
+        }
     }
     if (share) {
       __shared__ float sums[kWarps][D + 1];
@@ -336,7 +351,7 @@ __global__ void __launch_bounds__(kJoinThreads)
         for (int c = 0; c < C; ++c) o[c] += sums[w][lane * C + c];
       }
     }
-    const RowAt at = row_at(a, req.row0, d.rt * M, d.h, r);
+    const RowAt at = row_at(a, d.row0, d.rt * M, d.h, r);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T *out = static_cast<T *>(a.out) + (at.token * a.Hq + at.head) * D + lane * C;
 #pragma unroll
@@ -363,11 +378,11 @@ pair_status run_simt(Launch *l, cudaStream_t s) {
   return PAIR_OK;
 }
 
-template <typename T, int D>
+template <typename T, int D, int NT, int B>
 pair_status run_join(const Launch &l0, const Launch &l1, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(l0.ctas * join_blocks(l0) + l1.ctas * join_blocks(l1), 1, 1);
-  cfg.blockDim = dim3(kJoinThreads, 1, 1);
+  cfg.gridDim = dim3(l0.ctas * join_blocks<NT>(l0) + l1.ctas * join_blocks<NT>(l1), 1, 1);
+  cfg.blockDim = dim3(NT, 1, 1);
   cfg.stream = s;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -375,12 +390,26 @@ pair_status run_join(const Launch &l0, const Launch &l1, cudaStream_t s) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   PAIR_BEGIN("attend_join", s);
-  if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, l0, l1) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D, NT, B>, l0, l1) != cudaSuccess) {
     cudaGetLastError();
     return PAIR_ERR_CUDA;
   }
   PAIR_LAUNCH_CHECK(s);
   return PAIR_OK;
+}
+
+// After a launch with many rows blocks are many and their rows have two or three partial
+// sums: few registers (four chunks over bf16 388 us, with 32 floats 398). Else a row has all
+// its sums on their way at once where they are many (a token over 20,000 of codes 38 us,
+// four at a time and behind the maxima 47). Where warps have shares of their own and a
+// unit falls to a few of them, blocks of four warps, all at once on the SMs (8 x 8 requests,
+// a token each: 42.1 us, of eight warps 45.5).
+template <typename T, int D>
+pair_status run_join(const Launch &l0, const Launch &l1, cudaStream_t s) {
+  if (l1.ctas) return run_join<T, D, 256, 8>(l0, l1, s);
+  if (l0.a.ke && l0.ctas < 8 * (int64_t)l0.a.R * l0.a.Hkv)
+    return run_join<T, D, 128, 16>(l0, l1, s);
+  return run_join<T, D, 256, 32>(l0, l1, s);
 }
 
 template <typename F>

@@ -78,7 +78,8 @@ struct Args {
 
 // A segment of a CTA: key tiles [t0, t1) of the unit's `tiles`.
 struct Desc {
-  int32_t i, h, rt, t0, t1, tiles, pad0, pad1;
+  int32_t i, h, rt, t0, t1, tiles;
+  int32_t row0, rows;  // first token of the request's chunk, rows of the unit
 };
 
 // Partial sums of M rows: max (log2 units), sum, output sums.
@@ -338,7 +339,7 @@ __device__ __forceinline__ RowAt row_at(const Args &a, int row0, int r0, int h, 
 // the partial sums; its slot in the workspace.
 __device__ __forceinline__ int64_t note_partial(const Args &a, const Segment &s, int cta, int k) {
   const int slot = cta * 2 + (k ? 1 : 0);
-  if (threadIdx.x == 0) a.desc[slot] = {s.i, s.h, s.rt, s.t0, s.t1, s.tiles, 0, 0};
+  if (threadIdx.x == 0) a.desc[slot] = {s.i, s.h, s.rt, s.t0, s.t1, s.tiles, s.row0, s.rows};
   return slot;
 }
 __device__ __forceinline__ void clear_notes(const Args &a, int cta) {

@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kerne
     float *part = nullptr;
     if (!s.whole()) {
       const int64_t slot = worker * 2 + (seg ? 1 : 0);
-      if (lane == 0) a.desc[slot] = {s.i, s.h, s.rt, s.t0, s.t1, s.tiles, 0, 0};
+      if (lane == 0) a.desc[slot] = {s.i, s.h, s.rt, s.t0, s.t1, s.tiles, s.row0, s.rows};
       part = a.part + slot * part_floats(M, D);
     }
     if (M == 8 || s.rows <= 8)
