@@ -47,7 +47,7 @@ constexpr int kManyCost = 800, kFewCost = 192, kSimtCost = 48;
 // cost, stay within 32 bits.
 constexpr int kMaxKeys = INT32_MAX - 4096;
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
-constexpr int kMinWarp = 64;     // or a warp, where those have shares
+constexpr int kMinWarp = 96;     // or a warp, where those have shares
 
 struct Args {
   int64_t T;

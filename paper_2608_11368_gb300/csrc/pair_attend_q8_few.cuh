@@ -212,18 +212,25 @@ __device__ __forceinline__ uint32_t place(int row, int piece) {
   }
 }
 
-// The copies of a slice's rows, whose addresses are at `ptrs`.
+// The copies of a slice's rows, whose addresses are at `ptrs`: all addresses are read before
+// the first copy (no load passes a copy, which writes shared memory: one after the other, a
+// copy waits for each load, 316 us instead of 288 for five rows of four heads), two at once.
 template <int D, bool value>
 __device__ __forceinline__ void bring(uint32_t to, uint32_t ptrs) {
   constexpr int P = D / 16, RP = 32 / P;  // pieces of a row, rows of one round of copies
+  constexpr int B = kSlice<D> / RP;       // rows of a lane
   const int lane = threadIdx.x & 31, c = lane % P;
+  const auto row = [&](int x) { return x / 2 * 2 * RP + lane / P * 2 + x % 2; };
+  const uint8_t *p[B];
 #pragma unroll
-  for (int x = 0; x < kSlice<D> / RP; ++x) {
-    const int r = x * RP + lane / P;
-    const uint8_t *p;
-    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(p) : "r"(ptrs + r * 8) : "memory");
-    cp_async16(to + place<D, value>(r, c), wide(p, c, 16), true);
-  }
+  for (int x = 0; x < B; x += 2)
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];"
+                 : "=l"(p[x]), "=l"(p[x + 1])
+                 : "r"(ptrs + row(x) * 8)
+                 : "memory");
+#pragma unroll
+  for (int x = 0; x < B; ++x)
+    cp_async16(to + place<D, value>(row(x), c), wide(p[x], c, 16), true);
 }
 
 // Where a warp's copies are: this lane's key of the next slice to be brought, and that
@@ -675,8 +682,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kerne
   const int worker = blockIdx.x * kWarps + warp;
   if (a.rows_upto < INT32_MAX) let_next_start();  // the kernel for many rows
   if (lane < 2) a.desc[worker * 2 + lane] = {0, 0, 0, 0, 0, 0, 0, 0};
-  clear_spare_rows<T, D, kThreads>(a, blockIdx.x, gridDim.x);
-  if (blockIdx.x == gridDim.x - 1) report_requests(a);
   int64_t *scratch = reinterpret_cast<int64_t *>(smem);
   const Share share =
       a.heads < a.Hkv
@@ -693,6 +698,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kerne
     begin_stream<D>(a, p.next, m);
     begin_copies<T, D, M>(a, p.next, m, smem_u32(mine));
   }
+  clear_spare_rows<T, D, kThreads>(a, blockIdx.x, gridDim.x);
+  if (blockIdx.x == gridDim.x - 1) report_requests(a);
   for (int seg = 0; p.more; ++seg) {
     const Segment s = p.next;
     __syncwarp();
