@@ -220,8 +220,9 @@ struct Segment {
   }
 };
 
-// Walks a CTA's share, one segment per call. All arguments are uniform.
-template <int M, int BN>
+// Walks a CTA's share, one segment per call. All arguments are uniform. Units are cut
+// between tiles of BN keys, of many requests between every S of them.
+template <int M, int BN, int S = 1>
 struct Walk {
   Share s;
   Request r;
@@ -275,8 +276,9 @@ struct Walk {
       g->least = min(r.kv, g->seen(0, a.g));
       g->keys = min(r.kv, g->seen(g->rows - 1, a.g));
       g->tiles = (g->keys + BN - 1) / BN;
-      g->t0 = cut(x0, cost, g->tiles);
-      g->t1 = cut(x1, cost, g->tiles);
+      const int every = a.R == 1 ? 1 : S;
+      g->t0 = cut(x0, cost, g->tiles, every);
+      g->t1 = cut(x1, cost, g->tiles, every);
       g->head = x0 == 0;
       s.from += x1 - x0;
       // A unit without keys is worked on (zeros are written) by whoever has
@@ -288,10 +290,12 @@ struct Walk {
 
   // The key tile at which x of a unit's `cost` falls: the same for the CTA that
   // ends there and the one that begins there.
-  static __device__ __forceinline__ int cut(int64_t x, int64_t cost, int tiles) {
+  static __device__ __forceinline__ int cut(int64_t x, int64_t cost, int tiles, int every) {
     if (x == 0) return 0;
     if (x == cost) return tiles;
-    return min(tiles, (int)__float2int_rn(__fdiv_rn((float)x, (float)cost) * (float)tiles));
+    const int n = S == 1 ? tiles : (tiles + every - 1) / every;
+    const int t = (int)__float2int_rn(__fdiv_rn((float)x, (float)cost) * (float)n);
+    return S == 1 ? min(tiles, t) : t >= n ? tiles : t * every;
   }
 };
 
