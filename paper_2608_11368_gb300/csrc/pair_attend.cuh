@@ -47,7 +47,9 @@ constexpr int kManyCost = 800, kFewCost = 192, kSimtCost = 48;
 // cost, stay within 32 bits.
 constexpr int kMaxKeys = INT32_MAX - 4096;
 constexpr int kMinKeys = 128;    // least share of the line worth a CTA of its own
-constexpr int kMinWarp = 96;     // or a warp, where those have shares
+// Or a warp, where those have shares (32 requests in fp32 of up to 640 keys: 16.6 us; 64
+// keys 18.6, 128 keys 20.7).
+constexpr int kMinWarp = 96;
 
 struct Args {
   int64_t T;

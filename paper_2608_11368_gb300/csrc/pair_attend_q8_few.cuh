@@ -8,13 +8,12 @@
 // a warp. mma.sync rather than tcgen05: so few rows cannot fill a tile of 128.
 //
 // 32 x 16 requests of 1500 tokens as the median (2.1 GB of codes, prompts of 256 tokens
-// shared by 16 of them counted once): 352 us by token, 332 by head in e4m3. The copies
-// alone, without the products, take 340 by head: the shared prompts come from memory again
-// for nearly every request, 2.36 GB, so that is HBM's rate. Whole numbers leave no room
-// beside the copies: of 715 instructions for 32 keys and 8 rows 350 make codes into
-// numbers. With five rows of four heads (16 x 16 requests of 512 to 4096 tokens, 1.0 GB)
-// 316 us: 1050 instructions for 32 keys and 24 rows, 0.43 of them issued per cycle by two
-// warps a scheduler; registers (254) admit no more.
+// shared by 16 of them counted once): 329 us by token, 325 by head in e4m3. That is HBM's
+// rate: the shared prompts come from memory again for nearly every request, 2.36 GB. Whole
+// numbers leave little room beside the copies: of 715 instructions for 32 keys and 8 rows
+// 350 make codes into numbers. With five rows of four heads (16 x 16 requests of 512 to
+// 4096 tokens, 1.0 GB) 288 us: 1050 instructions for 32 keys and 24 rows, in two warps a
+// scheduler, which issue in 0.46 of the cycles; registers (254) admit no more.
 //
 // K: codes become fp16 (exact, five instructions for four whole numbers), against
 // queries in fp16 that are scaled by a power of two per row: the row's largest entry is
