@@ -284,6 +284,17 @@ def test_many_requests_and_idle_ones():
     check(build(reqs, 4, 2, 64, 8, torch.bfloat16, "i8", seed=2))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("heads", [(8, 4, 64), (8, 4, 128), (4, 2, 128), (8, 4, 256)])
+@pytest.mark.parametrize("n", [1, 6])
+def test_one_long_request_among_many(n, heads, dtype):
+    """A unit in very many pieces where units are in few on average."""
+    reqs = [(n, n + 16 + i % 50) for i in range(130)]
+    reqs[33] = (n, 20000)
+    Hq, Hkv, D = heads
+    check(build(reqs, Hq, Hkv, D, 16, dtype, "i8", seed=n), max_new=n)
+
+
 def test_exponents_with_strides_of_their_own():
     """Exponent bytes out of a wider array, codes in pages of a larger one."""
     from paper_2608_11368_gb300 import binding as B
