@@ -48,7 +48,7 @@ constexpr int kWarps = kThreads / 32;
 // Work is cut between tiles of BN keys, of many requests between every kCut of them: a
 // token of one request over 700 keys takes 14.6 us, cut between every 128 keys 16.5; 128
 // requests of up to 640 keys in fp32 20.7, cut between all tiles 24.8 (more units fall into
-// pieces, which have to be joined).
+// pieces, which have to be joined), between every eight 25.8 (shares differ by more).
 constexpr int BN = 32, kCut = 4;
 // Keys that a warp works on at once: 16 where slices of 32 would leave an SM four warps.
 template <int D>
@@ -733,7 +733,7 @@ pair_status run_few(Launch *l, int slots, cudaStream_t s) {
   static_assert(kPerSm<T, D, M> * (smem + 1024) <= 233472, "shared memory of an SM");
   const auto kernel = attend_q8_few_kernel<T, D, F, M>;
   PAIR_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  a.unit_cost = 96;  // 192: 360 us instead of 350 for the skewed requests by head
+  a.unit_cost = 96;  // 8 x 8 requests, a token each: 40.4 us, with 48 or 160 41.1
   a.slice_pages = kSlice<D> / a.page;
   a.slice_rest = kSlice<D> % a.page;
   a.narrow = true;
