@@ -652,12 +652,16 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  *                      orders of magnitude: each is off by 2^-4 of itself at
  *                      most, where whole numbers are off by up to 2^-7 of the
  *                      row's largest).
- * b is the least byte with which the row's largest entry does not round beyond
- * the largest code, and every code is its entry's nearest (halves to even), so
- * codes do not depend on the device. b = 255: the row had a NaN or an infinity;
- * it holds NaN. (No other row has codes that are not numbers; what e4m3's two
- * such codes count as in a row that a caller made is not defined.) The scales
- * are powers of two: a stored value is a bf16 number.
+ * b is the least byte with which the row's largest |x| is
+ *     below 127.5 2^(b - 127) for PAIR_CACHE_I8,
+ *     below 464 2^(b - 127)   for PAIR_CACHE_E4M3
+ * (what is below rounds to the largest code at most; what is equal takes the
+ * byte above, in e4m3 too, where 464 itself would round to 448), and every code
+ * is its entry's nearest (halves to even), so codes do not depend on the device.
+ * b = 255: the row had a NaN or an infinity; it holds NaN. (No other row has
+ * codes that are not numbers; what e4m3's two such codes count as in a row that
+ * a caller made is not defined.) The scales are powers of two: a stored value is
+ * a bf16 number.
  */
 typedef struct {
   void *codes;                 /* int8 or e4m3, strides in elements (bytes) */
