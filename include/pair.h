@@ -649,9 +649,11 @@ PAIR_API pair_status pair_attend_paged(int64_t T, int32_t R, int32_t Hq, int32_t
  *     PAIR_CACHE_I8    whole numbers from -127 to 127 (int8),
  *     PAIR_CACHE_E4M3  floating-point numbers of 4 exponent and 3 significand
  *                      bits, up to 448 (for rows whose entries differ by
- *                      orders of magnitude: each is off by 2^-4 of itself at
- *                      most, where whole numbers are off by up to 2^-7 of the
- *                      row's largest).
+ *                      orders of magnitude).
+ * An entry x is off by at most 2^-1 2^(b - 127) for PAIR_CACHE_I8 and by at most
+ * max(2^-4 |x|, 2^-10 2^(b - 127)) for PAIR_CACHE_E4M3: relative to the entry
+ * down to some 2^-14 of the row's largest one, absolute below, and entries below
+ * some 2^-18 of the largest one may become 0.
  * b is the least byte with which the row's largest |x| is
  *     below 127.5 2^(b - 127) for PAIR_CACHE_I8,
  *     below 464 2^(b - 127)   for PAIR_CACHE_E4M3

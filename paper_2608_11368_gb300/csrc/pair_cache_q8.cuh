@@ -58,10 +58,11 @@ __device__ __forceinline__ __nv_bfloat162 whole_to_bf16(uint32_t x) {
 }
 
 // The exponent byte of a row whose largest |x| has these bits: the least one with
-// which it is below 127.5 or 464, half a step above the largest code. A significand of 1 + m with E - 6 gives 64 (1 + m), at most 127 if it is
-// below 127.5; with E - 8 e4m3 gets 256 (1 + m), at most 448 if it is below 464. What is
-// not below carries into the exponent (464 too, which would round to 448: the bytes are
-// the contract, and the same comparison does for both formats).
+// which it is below 127.5 or 464, half a step above the largest code. A significand of
+// 1 + m with E - 6 gives 64 (1 + m), at most 127 if it is below 127.5; with E - 8 e4m3
+// gets 256 (1 + m), at most 448 if it is below 464. What is not below carries into the
+// exponent (464 too, which would round to 448: the bytes are the contract, and the same
+// comparison does for both formats).
 template <int F>
 __device__ __forceinline__ uint32_t exponent_of(uint32_t top) {
   constexpr uint32_t carry = F == kI8 ? 0x010000u : 0x180000u;

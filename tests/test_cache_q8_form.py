@@ -39,3 +39,28 @@ def test_least_exponent_is_the_headers(fmt):
         else:
             assert (np.abs(c - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10)).all()
         assert (np.abs(c) <= MOST[fmt]).all()
+
+
+def test_errors_are_within_the_headers_bounds():
+    """Entries from the row's largest down to 2^-40 of it, midpoints between codes among
+    them: each is off by at most what the header says, and by all of it somewhere."""
+    rng = np.random.default_rng(0)
+    text = header()
+    half = 2.0 ** int(re.search(r"at most 2\^(-\d+) 2\^\(b - 127\) for PAIR_CACHE_I8",
+                                text).group(1))
+    m = re.search(r"at most max\(2\^(-\d+) \|x\|, 2\^(-\d+) 2\^\(b - 127\)\) for PAIR_CACHE_E4M3",
+                  text)
+    part, step = (2.0 ** int(x) for x in m.groups())
+    x = rng.choice([-1.0, 1.0], (400, 64)) * 2.0 ** -rng.uniform(0, 40, (400, 64))
+    x[:200] = np.ldexp(rng.integers(1, 64, (200, 64)) / 2.0, -rng.integers(0, 24, (200, 64)))
+    x *= 2.0 ** rng.integers(-30, 30, (400, 1))
+    for fmt in sorted(NAMES):
+        c, b = rollout.store_q8(x, fmt)
+        unit = 2.0 ** (b - 127.0)[:, None] * np.ones_like(x)
+        off = np.abs(rollout.values_q8(c, b) - x)
+        bound = half * unit if fmt == "i8" else np.maximum(part * np.abs(x), step * unit)
+        assert (off <= bound).all()
+        assert off.max() > 0 and (off > 0.9 * bound).any()
+    for row, back in (([1.0, 2.0 ** -18], [1.0, 0.0]),  # 1 is 256 2^-8: codes down to 2^-17
+                      ([1.0, 2.0 ** -17], [1.0, 2.0 ** -17])):
+        assert rollout.values_q8(*rollout.store_q8(np.array([row]), "e4m3"))[0].tolist() == back
