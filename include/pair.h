@@ -710,13 +710,19 @@ PAIR_API pair_status pair_cache_read_q8(int64_t T, int32_t Hkv, int32_t D, const
 
 /*
  * pair_attend_paged_q8 -- pair_attend_paged over caches in 8 bits: the same
- * sums over the stored values, which are exact in the arithmetic, with the same
- * conventions, workspace (pair_attend_workspace_size for dt) and errors. dt is
+ * sums over the stored values, which are exact in the arithmetic (but for the
+ * range below), with the same conventions, workspace (pair_attend_workspace_size for dt) and errors. dt is
  * the type of q and out; nothing is asked of the exponent bytes' strides. A key
  * or value that holds NaN makes the rows that see it NaN, and no others.
  * Arithmetic: PAIR_BF16 as for pair_attend_paged. PAIR_F32: on the tensor cores
  * too, queries as sums of two fp16 numbers (22 bits, down to 2^-39 of a row's
  * largest entry) and weights of three bf16 ones (24 bits), sums in fp32.
+ * Range: a key or value may be taken as off by up to 2^-126 (kernel for many
+ * rows), and a key's part of an output, with the largest weight as 1 and before
+ * the division by their sum, is off by up to 2^-125 beside the rest: of account
+ * for values of 2^-100 and less, and keys of 2^-118 and less. Scores, and sums of
+ * values over keys with weights of up to 2^8, have to be fp32 numbers: values of
+ * 2^90 and more may leave that range.
  * max_new is of more use here than there: chunks of few rows have kernels for 8,
  * 16, 24 and 32 of them per key head, by what it says. Chunks of more go to the
  * tensor cores' kernel for many rows where D is 64 or 128 and pages are a
