@@ -471,7 +471,9 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
       }
     }
     // sc[i][j][c]: key 16 i + g + 8 (c / 2), row 8 j + 2 t + c % 2. In log2 units, relative
-    // to the row's reference, which is 0 at first.
+    // to the row's reference, which is 0 at first. The powers of two of key and query meet
+    // first: a large key under small queries, whose codes alone make products of up to
+    // 2^32, would leave fp32's range with one of them.
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const float k0 = __shfl_sync(0xffffffffu, ke, i * 16 + g);
@@ -481,7 +483,7 @@ __device__ __forceinline__ void few_segment(const Args &a, const Segment &s, Str
 #pragma unroll
         for (int c = 0; c < 4; c += 2) {  // two rows at once
           const float k = c ? k1 : k0;
-          const float2 y = fma2(mul2({sc[i][j][c], sc[i][j][c + 1]}, {k, k}), {cs[j][0], cs[j][1]},
+          const float2 y = fma2({sc[i][j][c], sc[i][j][c + 1]}, mul2({cs[j][0], cs[j][1]}, {k, k}),
                                 {-mx[j][0], -mx[j][1]});
           sc[i][j][c] = y.x, sc[i][j][c + 1] = y.y;
         }

@@ -103,3 +103,14 @@ def check(fmt, D, n, keys, values, dtype):
 @pytest.mark.parametrize("values", [(0, 1, 2, 10), (20, 129, 142), (130, 143, 200, 216)])
 def test_values_of_every_size(values, n, D, dtype, fmt):
     check(fmt, D, n, (ORDINARY,) * len(values), values, dtype)
+
+
+@pytest.mark.parametrize("fmt", sorted(CODES))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n", [1, 12, 16, 100])
+@pytest.mark.parametrize("keys", [(2, 10, 11, 60), (20, 129, 142), (130, 143, 200, 240)])
+def test_keys_of_every_size(keys, n, D, dtype, fmt):
+    """Large keys under queries that are as small: a score is what it is, although a product
+    of codes and the key's power of two alone would leave fp32's range."""
+    check(fmt, D, n, keys, (ORDINARY,) * len(keys), dtype)
