@@ -711,9 +711,10 @@ PAIR_API pair_status pair_cache_read_q8(int64_t T, int32_t Hkv, int32_t D, const
 /*
  * pair_attend_paged_q8 -- pair_attend_paged over caches in 8 bits: the same
  * sums over the stored values, which are exact in the arithmetic (but for the
- * range below), with the same conventions, workspace (pair_attend_workspace_size for dt) and errors. dt is
- * the type of q and out; nothing is asked of the exponent bytes' strides. A key
- * or value that holds NaN makes the rows that see it NaN, and no others.
+ * range below), with the same conventions, workspace (pair_attend_workspace_size
+ * for dt) and errors. dt is the type of q and out; nothing is asked of the
+ * exponent bytes' strides. A key or value that holds NaN makes the rows that see
+ * it NaN, and no others.
  * Arithmetic: PAIR_BF16 as for pair_attend_paged. PAIR_F32: on the tensor cores
  * too, queries as sums of two fp16 numbers (22 bits, down to 2^-39 of a row's
  * largest entry) and weights of three bf16 ones (24 bits), sums in fp32.
@@ -723,10 +724,13 @@ PAIR_API pair_status pair_cache_read_q8(int64_t T, int32_t Hkv, int32_t D, const
  * for values of 2^-100 and less, and keys of 2^-118 and less. Scores, and sums of
  * values over keys with weights of up to 2^8, have to be fp32 numbers: values of
  * 2^90 and more may leave that range.
- * max_new is of more use here than there: chunks of few rows have kernels for 8,
- * 16, 24 and 32 of them per key head, by what it says. Chunks of more go to the
- * tensor cores' kernel for many rows where D is 64 or 128 and pages are a
- * multiple of 8 tokens.
+ * max_new is of more use here than there: the kernel for few rows has a form for
+ * the most of them per key head that it admits, 8, 16, 24 or 32 in PAIR_BF16 with
+ * D 64 or 128, 8 or 16 in PAIR_F32, 16 in PAIR_BF16 with D 256 (chunks of more are
+ * worked on in pieces of so many). In PAIR_BF16 with D 64 or 128, over pages of a
+ * multiple of 8 tokens, chunks of more than 32 rows per key head go to the tcgen05
+ * kernel for many rows, unless a stride of the codes is below 16 or from 2^40 on;
+ * all others stay with the kernel for few.
  */
 PAIR_API pair_status pair_attend_paged_q8(int64_t T, int32_t R, int32_t Hq, int32_t Hkv, int32_t D,
                                           pair_dtype dt, const void *q, int64_t q_row,

@@ -678,7 +678,8 @@ constexpr int kPerSm = 2 * (Few<T, D, M>::kBytes + 1024) > 233472 ? 1
 // joined at its end: 442 us instead of 391 for the skewed requests). Every warp has a share
 // of the work of its own, or, where key heads come in fours, a CTA has one of four heads at
 // once: its warps then read the same tokens, whose heads lie side by side in a cache by
-// token (405 us -> 351). Three CTAs an SM for up to 8 rows (two: 419), two for more.
+// token (405 us -> 351). Three CTAs an SM for up to 8 rows of at most 256 bytes (two: 419),
+// two for more, one for 16 rows of 1024 bytes.
 template <typename T, int D, int F, int M>
 __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kernel(Args a) {
   using L = Few<T, D, M>;

@@ -114,3 +114,31 @@ def test_keys_of_every_size(keys, n, D, dtype, fmt):
     """Large keys under queries that are as small: a score is what it is, although a product
     of codes and the key's power of two alone would leave fp32's range."""
     check(fmt, D, n, keys, (ORDINARY,) * len(keys), dtype)
+
+
+@pytest.mark.parametrize("dtype,D,page,rows,names", [
+    (torch.bfloat16, 128, 16, 100, ["attend_q8_many"]),
+    (torch.bfloat16, 64, 8, 33, ["attend_q8_many"]),
+    (torch.bfloat16, 128, 16, 32, ["attend_q8_few"]),
+    (torch.bfloat16, 128, 12, 100, ["attend_q8_few"]),
+    (torch.bfloat16, 256, 16, 100, ["attend_q8_few"]),
+    (torch.float32, 128, 16, 100, ["attend_q8_few"])])
+def test_which_kernel_a_chunk_goes_to(dtype, D, page, rows, names):
+    """As the header says it: by the type, the head size, the pages and the rows per key
+    head; a chunk that is alone has one launch and the joining pass."""
+    from paper_2608_11368_gb300 import binding as B
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    pages = -(-KV // page)
+    codes = torch.zeros((pages, page, 1, D), dtype=torch.int8, device="cuda")
+    exps = torch.zeros((pages, page, 1), dtype=torch.uint8, device="cuda")
+    q, err = torch.zeros((rows, 1, D), dtype=dtype, device="cuda"), i32([0])
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous()
+    B.pair_timing_enable(True)
+    try:
+        B.pair_attend_paged_q8(q, codes, exps, codes, exps, table, i32([KV]), i32([0, rows]),
+                               dev_err=err)
+        got = [n for n, _ in B.pair_timing_read()]
+    finally:
+        B.pair_timing_enable(False)
+    assert B.pair_status_sync(err) == 0
+    assert got == [*names, "attend_join"]
