@@ -703,8 +703,9 @@ def pair_attend_paged_q8(q, k_codes, k_exps, v_codes, v_exps, block_table, kv_le
                          stream=None):
     """pair_attend_paged over caches in 8 bits (see pair.h): codes [num_pages,
     page_size, Hkv, D] int8 or float8_e4m3fn, exponent bytes [num_pages,
-    page_size, Hkv] uint8 (views with other strides too). Returns (out [T, Hq, D],
-    lse [T, Hq] float32)."""
+    page_size, Hkv] uint8 (views with other strides too). max_new: the longest
+    chunk, where the host knows it; 0 takes the kernels for chunks of any length,
+    which are slower for short ones. Returns (out [T, Hq, D], lse [T, Hq] float32)."""
     T, Hq, D = q.shape
     dt, at, i32 = _pair_dtype(q, "q"), _index(q, "q"), torch.int32
     qp = _strided(q, "q", q.dtype, (T, Hq, D), q, at)

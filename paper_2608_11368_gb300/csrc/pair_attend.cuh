@@ -223,7 +223,8 @@ struct Segment {
 };
 
 // Walks a CTA's share, one segment per call. All arguments are uniform. Units are cut
-// between tiles of BN keys, of many requests between every S of them.
+// between tiles of BN keys, between every S of them if the request table has more than one
+// entry.
 template <int M, int BN, int S = 1>
 struct Walk {
   Share s;

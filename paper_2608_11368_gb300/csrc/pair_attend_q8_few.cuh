@@ -45,10 +45,12 @@ using q8::kI8;
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-// Work is cut between tiles of BN keys, of many requests between every kCut of them: a
-// token of one request over 700 keys takes 14.6 us, cut between every 128 keys 16.5; 128
+// Work is cut between tiles of BN keys, of more than one request between every kCut of them:
+// a token of one request over 700 keys takes 14.6 us, cut between every 128 keys 16.5; 128
 // requests of up to 640 keys in fp32 20.7, cut between all tiles 24.8 (more units fall into
-// pieces, which have to be joined), between every eight 25.8 (shares differ by more).
+// pieces, which have to be joined), between every eight 25.8 (shares differ by more). The
+// rule counts entries, idle ones too: a token over 700 keys beside 1 or 15 of them takes
+// 16.5, as two to eight such requests do; the finer cut was not measured there.
 constexpr int BN = 32, kCut = 4;
 // Keys that a warp works on at once: 16 where slices of 32 would leave an SM four warps.
 template <int D>
@@ -679,7 +681,9 @@ constexpr int kPerSm = 2 * (Few<T, D, M>::kBytes + 1024) > 233472 ? 1
 // of the work of its own, or, where key heads come in fours, a CTA has one of four heads at
 // once: its warps then read the same tokens, whose heads lie side by side in a cache by
 // token (405 us -> 351). Three CTAs an SM for up to 8 rows of at most 256 bytes (two: 419),
-// two for more, one for 16 rows of 1024 bytes.
+// two for more, one for 16 rows of 1024 bytes. The form for 32 rows, which a call takes that
+// does not know its longest chunk, serves single tokens too: the skewed requests 517 us
+// instead of 328, 16 x 16 with drafts 442 instead of 290.
 template <typename T, int D, int F, int M>
 __global__ void __launch_bounds__(kThreads, kPerSm<T, D, M>) attend_q8_few_kernel(Args a) {
   using L = Few<T, D, M>;

@@ -154,7 +154,7 @@ __device__ void look_over(const Args &a, Smem<D> &sm, Walk<M, BN> walk) {
 // 1.7e-3 if only the output were rounded; weights of 16 more bits would take the
 // second product twice, in the pipe that binds. Four chunks of 1025 to 2048 tokens
 // behind 1000 to 6144 (32/8 heads of 128, 0.52 TFLOP as the mean of two sets of
-// lengths): 397 us, 1.32 PFLOP/s, the tensor pipe 60 % active. Bound by shared
+// lengths): 391 us, 1.34 PFLOP/s, the tensor pipe 60 % active. Bound by shared
 // memory's reads (a product Q K^T of 64 cycles reads 8 KB at 128 bytes a cycle,
 // beside TMA's writes) and by the step's chain: products, scores out of TMEM,
 // maximum, exponentials, weights into TMEM.

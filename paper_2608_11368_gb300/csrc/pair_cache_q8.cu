@@ -163,8 +163,8 @@ template <typename T, int F>
 __device__ __forceinline__ void values(const uint32_t (&w)[8 / sizeof(T)], uint32_t b,
                                        uint32_t (&u)[8]) {
   if constexpr (F == kI8 && sizeof(T) == 2) {
-    // Codes over 64 by one multiply-add for two (to_bf16 in pair_cache_q8.cuh), times 2^(b
-    // - 121): in two factors where that is beyond bf16.
+    // Codes over 64 by one multiply-add for two (whole_to_bf16), times 2^(b - 121):
+    // in two factors where that is beyond bf16.
     const bool beyond = b > 248 && b != 255;
     const uint32_t f = b == 255 ? 0x7fc0u : (beyond ? b - 64 + 6 : b + 6) << 7;
 #pragma unroll
